@@ -320,6 +320,114 @@ ll_status ll_gdn_fwd_staged(const void* q, const void* k, const void* v, const f
                             void* workspace, size_t workspace_bytes, void* stream,
                             void* const* events);
 
+/* ---- Operators around a token mixer -----------------------------------------------------------
+ *
+ * The short causal convolution in front of a mixer, the selective state space scan (a mixer whose
+ * decay differs by channel and state) and the group norm of a mixer's output, with their backward
+ * passes and, for decoding, their form for one token.  Conventions, besides those at the top:
+ * Layout.   x, dt, the gates z, B and C may be columns of wider rows: each comes with the strides of
+ *           a sequence (batch) and of a token in elements, channels adjacent; strides are >= 0, a
+ *           token's below 2^24.  Everything else is dense.  Rows that start at a multiple of 16 bytes
+ *           are fastest, any start is accepted.  Parameters and their gradients, states of the scan
+ *           and statistics are float32; the rest has the storage dtype.
+ * Lengths.  lengths (int32, [B], device; NULL: all T) gives the tokens of each sequence; values are
+ *           taken into 0 .. T.  What stands after a sequence's end is never read into a result (it may
+ *           be NaN); outputs and gradients there are zeros, and final states are those at the end.
+ * States.   A call may continue a sequence from an initial state and leave the final one; both may be
+ *           the same buffer (overlap otherwise is not allowed).  NULL: zeros, or not wanted.
+ * Sums.     Sums over tokens are formed in an order that the sizes alone fix: no atomics.
+ * Arithmetic is float32 with one rounding at the end, whatever the storage dtype. */
+typedef enum { LL_ACT_NONE = 0, LL_ACT_SILU = 1 } ll_act;  /* SiLU: v / (1 + e^-v) */
+
+/* Short causal convolution of each channel, W = 2, 3 or 4 taps:
+ *   v_t = bias + sum_{j < W} weight[:, j] * x_(t - W + 1 + j),  y = act(v).
+ * x [B, T, D]; weight [D, W]; bias [D] or NULL; states [B, W - 1, D], the tokens before the first (oldest
+ * first) in the storage dtype; y [B, T, D]. */
+ll_status ll_causal_conv_fwd(const void* x, int64_t x_batch_stride, int64_t x_token_stride,
+                             const float* weight, const float* bias, const void* initial_state,
+                             void* final_state, const int32_t* lengths, void* y, int64_t B, int64_t T,
+                             int64_t D, int64_t W, int32_t act, int32_t dtype, void* stream);
+
+/* One token: x [B, D], y [B, D]; state [B, W - 1, D] is read and new_state written (the same buffer
+ * for decoding in place, another one to keep the old state). */
+ll_status ll_causal_conv_step(const void* x, int64_t x_batch_stride, const float* weight,
+                              const float* bias, const void* state, void* new_state, void* y, int64_t B,
+                              int64_t D, int64_t W, int32_t act, int32_t dtype, void* stream);
+
+/* Gradients: d_y [B, T, D] and d_final_state (NULL: zeros) give dx [B, T, D] (dense), dweight [D, W],
+ * dbias [D] and d_initial_state [B, W - 1, D] (NULL: not wanted).  The workspace is
+ * ll_causal_conv_bwd_workspace_size(...) bytes (0 for invalid arguments). */
+size_t ll_causal_conv_bwd_workspace_size(int32_t dtype, int64_t B, int64_t T, int64_t D, int64_t W);
+ll_status ll_causal_conv_bwd(const void* x, int64_t x_batch_stride, int64_t x_token_stride,
+                             const float* weight, const float* bias, const void* initial_state,
+                             const int32_t* lengths, const void* d_y, const void* d_final_state, void* dx,
+                             float* dweight, float* dbias, void* d_initial_state, int64_t B, int64_t T,
+                             int64_t D, int64_t W, int32_t act, int32_t dtype, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/* Inputs of the selective scan, for sequence b, token t, channel d and state n (channel d reads group
+ * d / (channels / groups) of B and C):
+ *   delta = softplus(dt + dt_bias)  (without softplus where delta_softplus is 0),
+ *   h_t = exp(delta A) h_(t-1) + delta x B,   y = (sum_n C h_t + D x) * silu(z).
+ * x, dt, z [batch, T, channels] (z may be NULL: no gate); A [channels, N] (the caller keeps it < 0);
+ * B, C [batch, T, groups, N]; D, dt_bias [channels], either may be NULL.  N <= 64. */
+typedef struct ll_scan_inputs {
+  const void *x, *dt, *z, *B, *C;
+  int64_t x_strides[2], dt_strides[2], z_strides[2], B_strides[2], C_strides[2];  /* batch, token */
+  const float *A, *D, *dt_bias;
+  const int32_t* lengths;
+  int64_t batch, T, channels, N, groups;
+  int32_t delta_softplus, dtype;
+} ll_scan_inputs;
+
+/* Bytes of workspace of the forward (backward = 0; may be 0: then the workspace may be NULL) or of the
+ * backward; bytes of the states that a forward leaves for the backward.  0 for invalid arguments. */
+size_t ll_selective_scan_workspace_size(int64_t B, int64_t T, int64_t D, int64_t N, int64_t groups,
+                                        int32_t backward);
+size_t ll_selective_scan_states_bytes(int64_t B, int64_t T, int64_t D, int64_t N);
+
+/* Forward: y [batch, T, channels] and the final state [batch, channels, N].  states (16-byte aligned,
+ * NULL for inference) receives the state before every 64th token (N <= 16; 32nd up to 32 states, 16th
+ * beyond), in the library's own layout, for ll_selective_scan_bwd on the same inputs. */
+ll_status ll_selective_scan_fwd(const ll_scan_inputs* in, const float* initial_state, void* y,
+                                float* final_state, float* states, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/* One token (T = 1, no lengths): state [batch, channels, N] is read and new_state written (the same
+ * buffer for decoding in place).  Token strides are not used. */
+ll_status ll_selective_scan_step(const ll_scan_inputs* in, const float* state, float* new_state, void* y,
+                                 void* stream);
+
+/* Gradients of the forward that left `states`, from d_y [batch, T, channels] and d_final_state (NULL:
+ * zeros): dx, ddt, dz [batch, T, channels] (dense; dz required with a gate), dA [channels, N],
+ * dB, dC [batch, T, groups, N], dD and ddt_bias [channels] and d_initial_state [batch, channels, N]
+ * (these three NULL: not wanted). */
+ll_status ll_selective_scan_bwd(const ll_scan_inputs* in, const float* states, const void* d_y,
+                                const float* d_final_state, void* dx, void* ddt, void* dz, float* dA,
+                                void* dB, void* dC, float* dD, float* ddt_bias, float* d_initial_state,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/* Group norm over channels-last rows x [N, S, C] with an activation, and a gate [N, S, C] or NULL:
+ *   u = (x - mean) / sqrt(var + eps) * weight + bias,   y = act(u), with a gate u * act(gate);
+ * mean and (biased) variance over the S tokens and the C / groups channels of a group.  S = 1
+ * normalises every token by itself (the heads of a mixer's output).  weight, bias [C] or NULL (1, 0).
+ * stats [N, groups, 2] (8-byte aligned; NULL: not wanted) receives mean and 1 / sqrt(var + eps) for
+ * the backward, which gives dx, dgate [N, S, C] (dense), dweight and dbias [C] (NULL: not wanted).
+ * The workspace is ll_group_norm_workspace_size(...) bytes (may be 0: then NULL is accepted). */
+size_t ll_group_norm_workspace_size(int32_t dtype, int64_t N, int64_t S, int64_t C, int64_t groups,
+                                    int32_t backward);
+ll_status ll_group_norm_fwd(const void* x, int64_t x_batch_stride, int64_t x_token_stride,
+                            const void* gate, int64_t gate_batch_stride, int64_t gate_token_stride,
+                            const float* weight, const float* bias, void* y, float* stats, int64_t N,
+                            int64_t S, int64_t C, int64_t groups, float eps, int32_t act, int32_t dtype,
+                            void* workspace, size_t workspace_bytes, void* stream);
+ll_status ll_group_norm_bwd(const void* x, int64_t x_batch_stride, int64_t x_token_stride,
+                            const void* gate, int64_t gate_batch_stride, int64_t gate_token_stride,
+                            const float* weight, const float* bias, const float* stats, const void* d_y,
+                            void* dx, void* dgate, float* dweight, float* dbias, int64_t N, int64_t S,
+                            int64_t C, int64_t groups, int32_t act, int32_t dtype, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
 /* Debug: writes out[t*T + s] = the Fenwick level l(t,s) that the forward kernels assign to the
  * pair (t, s) for chunk size C (Sec. 3.1; the intra/inter split of Eq. 5), and -1 for s > t.
  * `out` is device memory of T*T bytes.  Computed on the GPU by the same device functions the

@@ -58,7 +58,7 @@ struct ScanSplit {
   int64_t S = 1, len = 0;
 };
 int scan_state_blocks(int64_t N);            // blocks of 16 states a lane group holds: 1, 2 or 4
-int64_t scan_chunk(int64_t N);               // tokens between two saved states
+constexpr int kScanChunk = 16;               // tokens between two saved states
 int64_t scan_states_bytes(int64_t B, int64_t T, int64_t D, int64_t N);
 int64_t scan_fwd_workspace(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G);
 int64_t scan_bwd_workspace(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G);

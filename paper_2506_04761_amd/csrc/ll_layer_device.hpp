@@ -2,6 +2,8 @@
 // activations in fp32, and sums across the lanes of a wave.
 #pragma once
 
+#include <utility>
+
 #include "ll_device.hpp"
 
 namespace ll {
@@ -97,6 +99,12 @@ __device__ inline void wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// f(0), f(1), .. with the index as a compile-time constant (DPP controls need one).
+template <int... I, typename F>
+__device__ inline void unrolled(std::integer_sequence<int, I...>, F&& f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+
 template <int CTRL>
 __device__ inline float dpp_mov(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
@@ -108,31 +116,34 @@ __device__ inline float row_bcast(float v) {
   return dpp_mov<0x150 + M>(v);
 }
 
-// y + sum_i b_i h_i with b_i = lane M + i of each row of `b`: one v_fmac_f32_dpp a term, which the compiler
-// does not form by itself.  A register needs two wait states between its write and its use as a DPP
-// operand; the compiler does not see into the block, so it waits itself.
-template <int M>
-__device__ inline float dot4_bcast(float y, float b, const float* h) {
-  asm("s_nop 1\n\t"
-      "v_fmac_f32_dpp %0, %1, %2 row_newbcast:%6 row_mask:0xf bank_mask:0xf\n\t"
-      "v_fmac_f32_dpp %0, %1, %3 row_newbcast:%7 row_mask:0xf bank_mask:0xf\n\t"
-      "v_fmac_f32_dpp %0, %1, %4 row_newbcast:%8 row_mask:0xf bank_mask:0xf\n\t"
-      "v_fmac_f32_dpp %0, %1, %5 row_newbcast:%9 row_mask:0xf bank_mask:0xf"
-      : "+v"(y)
-      : "v"(b), "v"(h[0]), "v"(h[1]), "v"(h[2]), "v"(h[3]), "n"(M), "n"(M + 1), "n"(M + 2), "n"(M + 3));
-  return y;
-}
-
-// g_i + b_i v for four accumulators, b_i = lane M + i of each row of `b`.
-template <int M>
-__device__ inline void axpy4_bcast(float* g, float b, float v) {
-  asm("s_nop 1\n\t"
-      "v_fmac_f32_dpp %0, %4, %5 row_newbcast:%6 row_mask:0xf bank_mask:0xf\n\t"
-      "v_fmac_f32_dpp %1, %4, %5 row_newbcast:%7 row_mask:0xf bank_mask:0xf\n\t"
-      "v_fmac_f32_dpp %2, %4, %5 row_newbcast:%8 row_mask:0xf bank_mask:0xf\n\t"
-      "v_fmac_f32_dpp %3, %4, %5 row_newbcast:%9 row_mask:0xf bank_mask:0xf"
-      : "+v"(g[0]), "+v"(g[1]), "+v"(g[2]), "+v"(g[3])
-      : "v"(b), "v"(v), "n"(M), "n"(M + 1), "n"(M + 2), "n"(M + 3));
+// One token of a backward scan for four states: g_i += c_i dy, then sum_i b_i g_i and, with H, sum_i c_i h_i, where
+// b_i and c_i are lane M + i of each row of `b` and `c`: DPP operands, in multiply-adds that the compiler does not form
+// by itself.  A register needs two wait states between its write and its use as a DPP operand; the compiler does not
+// see into the block, so it waits itself.
+template <int M, bool H>
+__device__ inline void grad_token(float* g, float b, float c, float dy, const float* h, float& bg, float& ch) {
+#define LL_DPP(op, d, s, v, m) op " " d ", " s ", " v " row_newbcast:" m " row_mask:0xf bank_mask:0xf\n\t"
+  if (H) {
+    asm("s_nop 1\n\t"
+        LL_DPP("v_fmac_f32_dpp", "%0", "%7", "%8", "%13") LL_DPP("v_fmac_f32_dpp", "%1", "%7", "%8", "%14")
+        LL_DPP("v_fmac_f32_dpp", "%2", "%7", "%8", "%15") LL_DPP("v_fmac_f32_dpp", "%3", "%7", "%8", "%16")
+        LL_DPP("v_mul_f32_dpp", "%5", "%7", "%9", "%13") LL_DPP("v_mul_f32_dpp", "%4", "%6", "%0", "%13")
+        LL_DPP("v_fmac_f32_dpp", "%5", "%7", "%10", "%14") LL_DPP("v_fmac_f32_dpp", "%4", "%6", "%1", "%14")
+        LL_DPP("v_fmac_f32_dpp", "%5", "%7", "%11", "%15") LL_DPP("v_fmac_f32_dpp", "%4", "%6", "%2", "%15")
+        LL_DPP("v_fmac_f32_dpp", "%5", "%7", "%12", "%16") LL_DPP("v_fmac_f32_dpp", "%4", "%6", "%3", "%16")
+        : "+v"(g[0]), "+v"(g[1]), "+v"(g[2]), "+v"(g[3]), "=&v"(bg), "=&v"(ch)
+        : "v"(b), "v"(c), "v"(dy), "v"(h[0]), "v"(h[1]), "v"(h[2]), "v"(h[3]), "n"(M), "n"(M + 1), "n"(M + 2), "n"(M + 3));
+  } else {
+    asm("s_nop 1\n\t"
+        LL_DPP("v_fmac_f32_dpp", "%0", "%6", "%7", "%8") LL_DPP("v_fmac_f32_dpp", "%1", "%6", "%7", "%9")
+        LL_DPP("v_fmac_f32_dpp", "%2", "%6", "%7", "%10") LL_DPP("v_fmac_f32_dpp", "%3", "%6", "%7", "%11")
+        LL_DPP("v_mul_f32_dpp", "%4", "%5", "%0", "%8") LL_DPP("v_fmac_f32_dpp", "%4", "%5", "%1", "%9")
+        LL_DPP("v_fmac_f32_dpp", "%4", "%5", "%2", "%10") LL_DPP("v_fmac_f32_dpp", "%4", "%5", "%3", "%11")
+        : "+v"(g[0]), "+v"(g[1]), "+v"(g[2]), "+v"(g[3]), "=&v"(bg)
+        : "v"(b), "v"(c), "v"(dy), "n"(M), "n"(M + 1), "n"(M + 2), "n"(M + 3));
+    ch = 0.0f;
+  }
+#undef LL_DPP
 }
 
 // Sums over the 16 lanes of each row of 16 values: lane m of a row holds the total of v[m].  Halves of a row

@@ -3,21 +3,19 @@
 //   D_td = softplus(dt_td + bias_d),  a_tdn = exp(D_td A_dn),  h_tdn = a_tdn h_(t-1)dn + D_td x_td B_tn,
 //   y_td = (sum_n C_tn h_tdn + skip_d x_td) silu(z_td).
 //
-// Layout of a wave: 16 channels x 16 states (per block of 16 states).  Lane (r, c) = (lane / 16, lane % 16)
-// holds states 4r .. 4r+3 of channel c.  B and C are the same for all channels, so one register per
-// 4 tokens holds them with lane (r, m) = token m / 4, state 4r + m % 4, and a product takes its factor
-// as a row-broadcast operand (DPP) without an instruction for it.  Step sizes, inputs, gates and outputs
-// go through a wave's own LDS rows: loaded and finished as 16 tokens x 16 channels, four channels to
-// a lane, so that softplus and the gate are computed once for a token and channel.
+// Layout: a lane holds one channel and all its states in registers, so that no sum crosses lanes.  x, dt, z and y
+// are one element a lane and token, 64 adjacent channels to a wave, any alignment.  B and C, the same for all
+// channels of a group, are staged in LDS as fp32 rows of padded length and read at one address by all lanes (as
+// scalar operands they would halve the rate of the products that take them).
 //
-// Bound by the vector ALU: per token, channel and state one exp, the rate's product, the input's
-// product and two FMAs.  The states of a channel are a chain over tokens, and channels x sequences alone
-// rarely fill the card, so the length is split into S segments: a first kernel runs every segment but the
-// last by itself (the first from the initial state, the others from zero) without outputs, the second starts
-// each from the segments before it,
+// Bound by the vector ALU: per token, channel and state one exp (8 cycles of a wave), and the rate's product, the
+// input's product, the state's and the output's FMA (2 cycles each, with four waves on a SIMD; a lone wave issues
+// one in 8).  The states of a channel are a chain over tokens, and channels x sequences alone rarely make four
+// waves a SIMD, so the length is split into S segments, run twice: k_scan_fwd<OUT = false> runs every segment
+// but the last by itself (the first from the initial state, the others from zero) for its final state and its sum
+// of step sizes, k_scan_join turns these into the states that segments start from,
 //   h = exp(A sum D) h + (segment by itself),
-// and runs it with the outputs.  The second kernel's first segment starts from the first kernel's copy of the
-// initial state, so that the final state may be written over it.
+// and k_scan_fwd<OUT = true> runs them from there with the outputs.
 #include "ll_layer.hpp"
 #include "ll_layer_device.hpp"
 
@@ -25,9 +23,12 @@ namespace ll {
 
 namespace {
 
-constexpr int kTile = 16;      // tokens a wave stages at a time
-constexpr int kWaves = 4;      // waves of a workgroup: neighbouring blocks of 16 channels share cache lines
-constexpr int kBlock = 16 * kWaves;
+constexpr int kWaves = 4;            // waves of a workgroup: neighbouring channels of the same tokens
+constexpr int kBlock = 64 * kWaves;  // channels
+constexpr int kStep = 4;             // tokens that are loaded together
+
+constexpr int kQ = 4;                // states whose B and C are read from LDS together
+constexpr int kRows = 32;            // tokens whose B and C are staged together
 
 struct ScanDev {
   Rows x, dt, z, Bm, Cm;
@@ -36,10 +37,9 @@ struct ScanDev {
   float *h_final, *states, *seg_h, *seg_d;
   void* y;
   int64_t T, D, chunks;
-  int N, Dg, blocks, cblocks;  // states; channels of a group; workgroups of a group and of a sequence
-  int S, B;
-  int64_t len;            // tokens of a segment
-  int softplus, vec;      // vec: x, dt, z and y rows may be accessed four channels at a time
+  int N, G, Dg, blocks, cblocks;  // states; groups; channels of a group; workgroups of a group and of a sequence
+  int S, B, softplus;
+  int64_t len;                    // tokens of a segment
 };
 
 // Start of [.., segment or chunk, channel, padded state] records.
@@ -47,201 +47,212 @@ __device__ inline int64_t rec(int64_t b, int64_t s, int64_t S, int64_t D, int64_
   return ((b * S + s) * D + ch) * NP;
 }
 
-template <typename T, int NB, bool OUT, bool GATED>
-__global__ __launch_bounds__(64 * kWaves) void k_scan_fwd(ScanDev p) {
-  constexpr int NP = 16 * NB;
-  typedef typename VecN<T, 4>::type V4;
-  __shared__ float2 s_du[kWaves][kTile][16];
-  __shared__ float s_y[kWaves][kTile][16];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane >> 4, c = lane & 15;
+__device__ inline int64_t live_tokens(const int32_t* lengths, int64_t b, int64_t T) {
+  if (!lengths) return T;
+  const int64_t n = lengths[b];
+  return n < 0 ? 0 : (n > T ? T : n);
+}
 
+template <int NP>
+__device__ inline void load_state(const float* q, float* h) {
+#pragma unroll
+  for (int n = 0; n < NP; n += 4) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(q + n);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[n + i] = v[i];
+  }
+}
+template <int NP>
+__device__ inline void save_state(float* q, const float* h) {
+#pragma unroll
+  for (int n = 0; n < NP; n += 4) *reinterpret_cast<f32x4*>(q + n) = f32x4{h[n], h[n + 1], h[n + 2], h[n + 3]};
+}
+
+template <typename T, int NB, bool OUT, bool GATED>
+__global__ __launch_bounds__(64 * kWaves, NB == 1 ? 4 : (NB == 2 ? 2 : 1)) void k_scan_fwd(ScanDev p) {
+  constexpr int NP = 16 * NB, CH = kScanChunk;
+  constexpr int W = OUT ? 2 * NP : NP, STAGE = kRows * W / 256;  // values of a token's row; of a tile and thread
+  __shared__ float s_row[2][kRows][W];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   int64_t id = blockIdx.x;
   const int cb = int(id % p.cblocks);
   id /= p.cblocks;
   const int segs = OUT ? p.S : p.S - 1;  // nothing follows the last segment
   const int seg = int(id % segs), b = int(id / segs);
-  const int g = cb / p.blocks, c0 = (cb % p.blocks) * kBlock + wave * 16;
-  if (c0 >= p.Dg) return;
-  const int nch = p.Dg - c0 < 16 ? p.Dg - c0 : 16;       // channels of this wave
-  const int64_t ch0 = int64_t(g) * p.Dg + c0;
-  const int64_t ch = ch0 + (c < nch ? c : nch - 1);      // spare lanes repeat the last channel
+  const int g = cb / p.blocks, c0 = (cb % p.blocks) * kBlock + wave * 64;
+  const bool mine = c0 + lane < p.Dg;  // spare lanes repeat the group's last channel and store nothing
+  const int c = mine ? lane : p.Dg - 1 - c0;  // may be negative: a spare wave
+  const int64_t ch0 = int64_t(g) * p.Dg + c0, ch = ch0 + c;
 
-  float A2[NB][4], h[NB][4];
-  auto save = [&](float* base, int s) {
-    float* q = base + rec(b, s, p.S, p.D, ch, NP) + 4 * r;
+  float A2[NP], h[NP];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-      *reinterpret_cast<f32x4*>(q + 16 * nb) = f32x4{h[nb][0], h[nb][1], h[nb][2], h[nb][3]};
-  };
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int n = nb * 16 + 4 * r + i;
-      A2[nb][i] = n < p.N ? p.A[ch * p.N + n] * kLog2e : 0.0f;
-      h[nb][i] = p.h0 && seg == 0 && (!OUT || p.S == 1) && n < p.N ? p.h0[(int64_t(b) * p.D + ch) * p.N + n] : 0.0f;
-    }
-  if (!OUT && seg == 0 && p.h0 && c < nch) save(p.seg_h, p.S - 1);
-  if (OUT && seg == 0 && p.S > 1 && p.h0) {
-    const float* q = p.seg_h + rec(b, p.S - 1, p.S, p.D, ch, NP) + 4 * r;
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) h[nb][i] = q[16 * nb + i];
+  for (int n = 0; n < NP; ++n) {
+    A2[n] = n < p.N ? p.A[ch * p.N + n] * kLog2e : 0.0f;
+    h[n] = 0.0f;
   }
-  if (OUT) {
-#pragma unroll 4
-    for (int s = 0; s < seg; ++s) {
-      const float d = p.seg_d[(int64_t(b) * p.S + s) * p.D + ch];
-      const float* q = p.seg_h + rec(b, s, p.S, p.D, ch, NP) + 4 * r;
+  if (OUT && p.S > 1) {
+    load_state<NP>(p.seg_h + rec(b, seg, p.S, p.D, ch, NP), h);
+  } else if (seg == 0 && p.h0) {
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(q + 16 * nb);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h[nb][i] = fmaf(fast_exp2(A2[nb][i] * d), h[nb][i], v[i]);
-      }
-    }
+    for (int n = 0; n < NP; ++n) h[n] = n < p.N ? p.h0[(int64_t(b) * p.D + ch) * p.N + n] : 0.0f;
   }
+  const float bias = p.dt_bias ? p.dt_bias[ch] : 0.0f, skip = OUT && p.skip ? p.skip[ch] : 0.0f;
 
   const int64_t t_begin = int64_t(seg) * p.len, t_end = t_begin + p.len < p.T ? t_begin + p.len : p.T;
-  int64_t live = p.T;  // tokens from here on are no inputs
-  if (p.lengths) {
-    live = p.lengths[b];
-    live = live < 0 ? 0 : (live > p.T ? p.T : live);
-  }
-  // staging: lane = token lane / 4 of the tile, channels 4 (lane % 4) .. + 3
-  const int ts = lane >> 2, cs = 4 * (lane & 3);
-  const int mine = nch - cs < 0 ? 0 : (nch - cs > 4 ? 4 : nch - cs);
-  const T* xp = static_cast<const T*>(p.x.p) + b * p.x.sb + ch0;
-  const T* dp = static_cast<const T*>(p.dt.p) + b * p.dt.sb + ch0;
-  const T* zp = static_cast<const T*>(p.z.p) + b * p.z.sb + ch0;
-  constexpr bool gated = OUT && GATED;
-  T* yp = static_cast<T*>(p.y) + int64_t(b) * p.T * p.D + ch0;
-  const T* Bp = static_cast<const T*>(p.Bm.p) + b * p.Bm.sb + int64_t(g) * p.N;
-  const T* Cp = static_cast<const T*>(p.Cm.p) + b * p.Cm.sb + int64_t(g) * p.N;
-  float bias[4], skip[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    bias[i] = p.dt_bias && i < mine ? p.dt_bias[ch0 + cs + i] : 0.0f;
-    skip[i] = OUT && p.skip && i < mine ? p.skip[ch0 + cs + i] : 0.0f;
-  }
+  const int64_t live = live_tokens(p.lengths, b, p.T), end = live < t_end ? live : t_end;
+  // uniform addresses of the next token to be fetched, to be run; a lane adds its channel
+  const T* xp = static_cast<const T*>(p.x.p) + b * p.x.sb + t_begin * p.x.st + ch0;
+  const T* dp = static_cast<const T*>(p.dt.p) + b * p.dt.sb + t_begin * p.dt.st + ch0;
+  const T* zp = static_cast<const T*>(p.z.p) + b * p.z.sb + t_begin * p.z.st + ch0;
+  T* yp = static_cast<T*>(p.y) + (int64_t(b) * p.T + t_begin) * p.D + ch0;
+  const int count = __builtin_amdgcn_readfirstlane(end > t_begin ? int(end - t_begin) : 0);  // tokens to run
 
-  V4 xr = {}, dr = {}, zr = {};
-  T br[NB][4], cr[NB][4];
-  const int64_t end = live < t_end ? live : t_end;
-  // The inputs of a tile; rows from the end of the sequence on repeat its last and are masked when used.
-  auto fetch = [&](int64_t t0) {
-    const int left = end - t0 < kTile ? int(end - t0) : kTile;
-    if (left <= 0) return;
-    const int row = ts < left ? ts : left - 1;
-    xr = load_row4<T>(xp + t0 * p.x.st, row, p.x.st, cs, nch, p.vec);
-    dr = load_row4<T>(dp + t0 * p.dt.st, row, p.dt.st, cs, nch, p.vec);
-    if (gated) zr = load_row4<T>(zp + t0 * p.z.st, row, p.z.st, cs, nch, p.vec);
+  // a tile's rows: thread i of the workgroup holds values i, i + 256, ..
+  T stage[STAGE];
+  const T* Bp = static_cast<const T*>(p.Bm.p) + b * p.Bm.sb + t_begin * p.Bm.st + int64_t(g) * p.N;
+  const T* Cp = static_cast<const T*>(p.Cm.p) + b * p.Cm.sb + t_begin * p.Cm.st + int64_t(g) * p.N;
+  auto fetch_rows = [&](int t0) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int rj = 4 * j + (c >> 2) < left ? 4 * j + (c >> 2) : left - 1;
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const int n = nb * 16 + 4 * r + (c & 3) < p.N ? nb * 16 + 4 * r + (c & 3) : 0;
-        br[nb][j] = load_at<T>(Bp + t0 * p.Bm.st, rj, p.Bm.st, n);
-        if (OUT) cr[nb][j] = load_at<T>(Cp + t0 * p.Cm.st, rj, p.Cm.st, n);
-      }
+    for (int k = 0; k < STAGE; ++k) {
+      const int e = threadIdx.x + 256 * k, t = t0 + e / W, n = e % NP;
+      const bool is_c = OUT && e % W >= NP;
+      const T* q = is_c ? Cp : Bp;
+      stage[k] = t < count && n < p.N ? q[int64_t(t) * (is_c ? p.Cm.st : p.Bm.st) + n] : from_f32<T>(0.0f);
     }
   };
 
+  T xr[kStep], dr[kStep], zr[kStep];
+  int ahead = 0;  // tokens fetched; behind the end the last one is fetched again, and masked when used
+  auto fetch = [&] {
+#pragma unroll
+    for (int k = 0; k < kStep; ++k) {
+      xr[k] = load_at<T>(xp, 0, 0, c);
+      dr[k] = load_at<T>(dp, 0, 0, c);
+      if (GATED) zr[k] = load_at<T>(zp, 0, 0, c);
+      const bool more = ++ahead < count;
+      xp += more ? p.x.st : 0;
+      dp += more ? p.dt.st : 0;
+      if (GATED) zp += more ? p.z.st : 0;
+    }
+  };
   float dsum = 0.0f;
-  if (t_begin < t_end) fetch(t_begin);
-  for (int64_t t0 = t_begin; t0 < t_end; t0 += kTile) {
-    if (OUT && p.states && (t0 - t_begin) % (64 / NB) == 0 && c < nch) {
-      float* q = p.states + rec(b, t0 / (64 / NB), p.chunks, p.D, ch, NP) + 4 * r;
+  // kStep tokens from t on, whose rows are at `rows`.  A step size of zero leaves the states as they are, and rows
+  // behind the end are zeros.
+  auto run = [&](const float (*rows)[W], int t) {
+    float x[kStep], d[kStep], gate[kStep], y[kStep];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-        *reinterpret_cast<f32x4*>(q + 16 * nb) = f32x4{h[nb][0], h[nb][1], h[nb][2], h[nb][3]};
+    for (int k = 0; k < kStep; ++k) {
+      x[k] = to_f32(xr[k]);
+      d[k] = to_f32(dr[k]) + bias;
+      gate[k] = GATED ? to_f32(zr[k]) : 0.0f;
     }
-    const V4 xk = xr, zk = zr;
-    const bool in = ts < end - t0;
-    {
-      float2 du[4];
+    if (t + kStep < count) fetch();
+    if (p.softplus) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float d = to_f32(T(dr[i])) + bias[i];
-        if (p.softplus) d = softplusf(d);
-        d = in ? d : 0.0f;  // a token that is no input leaves the states as they are
-        du[i] = make_float2(d, in ? d * to_f32(T(xk[i])) : 0.0f);
-      }
-      wave_sync();
-      float4* q = reinterpret_cast<float4*>(&s_du[wave][ts][cs]);
-      q[0] = make_float4(du[0].x, du[0].y, du[1].x, du[1].y);
-      q[1] = make_float4(du[2].x, du[2].y, du[3].x, du[3].y);
-      wave_sync();
+      for (int k = 0; k < kStep; ++k) d[k] = softplusf(d[k]);
     }
-    float Bv[NB][4], Cv[NB][4];
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
+    for (int k = 0; k < kStep; ++k)
+      if (t + k >= count) d[k] = x[k] = 0.0f;
+    // kQ states at a time, the next ones' B and C on their way (registers are for the states: no more are)
+    auto read = [&](int i, f32x4 (*v)[2]) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bool ok = 4 * j + (c >> 2) < end - t0 && nb * 16 + 4 * r + (c & 3) < p.N;
-        Bv[nb][j] = ok ? to_f32(br[nb][j]) : 0.0f;
-        if (OUT) Cv[nb][j] = ok ? to_f32(cr[nb][j]) : 0.0f;
+      for (int j = 0; j < kQ / 4; ++j) {
+        v[j][0] = *reinterpret_cast<const f32x4*>(&rows[0][0] + i / NP * W + i % NP + 4 * j);
+        if (OUT) v[j][1] = *reinterpret_cast<const f32x4*>(&rows[0][0] + i / NP * W + NP + i % NP + 4 * j);
       }
-    if (t0 + kTile < t_end) fetch(t0 + kTile);
-
+    };
+    f32x4 now[kQ / 4][2], next[kQ / 4][2];
+    read(0, now);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float yt[4];
-      auto step = [&](auto K) {
-        constexpr int k = decltype(K)::value;
-        const float2 du = s_du[wave][4 * j + k][c];
-        if (!OUT) dsum += du.x;
-        float y = 0.0f;
+    for (int k = 0; k < kStep; ++k) {
+      const float u = d[k] * x[k];
+      if (!OUT) dsum += d[k];
+      y[k] = skip * x[k];
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          auto state = [&](auto I) {
-            constexpr int i = decltype(I)::value;
-            const float a = fast_exp2(du.x * A2[nb][i]);
-            h[nb][i] = fmaf(a, h[nb][i], row_bcast<4 * k + i>(Bv[nb][j]) * du.y);
-          };
-          state(std::integral_constant<int, 0>{});
-          state(std::integral_constant<int, 1>{});
-          state(std::integral_constant<int, 2>{});
-          state(std::integral_constant<int, 3>{});
-          if (OUT) y = dot4_bcast<4 * k>(y, Cv[nb][j], h[nb]);
+      for (int q = 0; q < NP; q += kQ) {
+        if (k * NP + q + kQ < kStep * NP) read(k * NP + q + kQ, next);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < kQ; ++i) {
+          h[q + i] = fmaf(fast_exp2(d[k] * A2[q + i]), h[q + i], now[i / 4][0][i % 4] * u);
+          if (OUT) y[k] = fmaf(now[i / 4][1][i % 4], h[q + i], y[k]);
         }
-        yt[k] = y;
-      };
-      step(std::integral_constant<int, 0>{});
-      step(std::integral_constant<int, 1>{});
-      step(std::integral_constant<int, 2>{});
-      step(std::integral_constant<int, 3>{});
-      if (OUT) s_y[wave][4 * j + r][c] = sum_rows4(yt[0], yt[1], yt[2], yt[3]);
-    }
-    if (OUT) {
-      wave_sync();
-      const float4 v = *reinterpret_cast<const float4*>(&s_y[wave][ts][cs]);
-      float o[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        o[i] = fmaf(skip[i], to_f32(T(xk[i])), o[i]);
-        if (gated) o[i] *= silu(to_f32(T(zk[i])));
-        o[i] = in ? o[i] : 0.0f;
+        for (int j = 0; j < kQ / 4; ++j) now[j][0] = next[j][0], now[j][1] = next[j][1];
       }
-      store_row4<T>(yp + t0 * p.D, ts, p.D, cs, o, ts < t_end - t0 ? mine : 0, p.vec);
+      if (GATED) y[k] *= silu(gate[k]);
+      asm volatile("" : "+v"(y[k]));  // the sums are formed here, not where they are stored: every state would stay alive
+    }
+    if (OUT && mine) {
+#pragma unroll
+      for (int k = 0; k < kStep; ++k)
+        if (t + k < count) (yp + k * p.D)[c] = from_f32<T>(y[k]);
+    }
+    yp += kStep * p.D;
+  };
+  auto save = [&](int64_t t) {
+    if (OUT && p.states && t % CH == 0 && mine) save_state<NP>(p.states + rec(b, t / CH, p.chunks, p.D, ch, NP), h);
+  };
+  const bool works = c0 < p.Dg;  // a spare wave only helps to stage
+  fetch_rows(0);
+  if (works && count > 0) fetch();
+  for (int t0 = 0; t0 < count; t0 += kRows) {
+    float(*rows)[W] = s_row[t0 / kRows & 1];
+#pragma unroll
+    for (int k = 0; k < STAGE; ++k) (&rows[0][0])[threadIdx.x + 256 * k] = to_f32(stage[k]);
+    __syncthreads();  // the rows are there; and every wave has left the other buffer, which is written next
+    if (t0 + kRows < count) fetch_rows(t0 + kRows);
+    if (!works) continue;
+    const int n = count - t0 < kRows ? count - t0 : kRows;
+    for (int t = 0; t < n; t += kStep) {
+      save(t_begin + t0 + t);
+      run(rows + t, t0 + t);
     }
   }
-
   if (OUT) {
-    if (seg == p.S - 1 && p.h_final && c < nch) {
+    yp = static_cast<T*>(p.y) + int64_t(b) * p.T * p.D + ch0;
+    if (mine)
+      for (int64_t t = t_begin + count; t < t_end; ++t) {
+        yp[t * p.D + c] = from_f32<T>(0.0f);
+        save(t);
+      }
+    if (seg == p.S - 1 && p.h_final && mine) {
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int n = nb * 16 + 4 * r + i;
-          if (n < p.N) p.h_final[(int64_t(b) * p.D + ch) * p.N + n] = h[nb][i];
-        }
+      for (int n = 0; n < NP; ++n)
+        if (n < p.N) p.h_final[(int64_t(b) * p.D + ch) * p.N + n] = h[n];
     }
-  } else if (c < nch) {
-    save(p.seg_h, seg);
-    if (r == 0) p.seg_d[(int64_t(b) * p.S + seg) * p.D + ch] = dsum;
+  } else if (mine) {
+    save_state<NP>(p.seg_h + rec(b, seg, p.S, p.D, ch, NP), h);
+    p.seg_d[(int64_t(b) * p.S + seg) * p.D + ch] = dsum;
+  }
+}
+
+// In place: a segment's own final state becomes the state that it starts from.
+__global__ __launch_bounds__(256) void k_scan_join(ScanDev p, int NP, int64_t total) {
+  constexpr int U = 32;  // segments whose loads are in flight together
+  const int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (id >= total) return;
+  const int64_t per = p.D * NP, b = id / per, e = id - b * per, ch = e / NP;
+  const int n = int(e - ch * NP);
+  const float A2 = n < p.N ? p.A[ch * p.N + n] * kLog2e : 0.0f;
+  float h = p.h0 && n < p.N ? p.h0[(b * p.D + ch) * p.N + n] : 0.0f;
+  float* q = p.seg_h + b * p.S * per + e;
+  const float* d = p.seg_d + b * p.S * p.D + ch;
+  for (int s = 0; s < p.S; s += U) {
+    float v[U], w[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int sk = s + k < p.S - 1 ? s + k : 0;  // the last segment has no record of its own
+      v[k] = q[sk * per];
+      w[k] = d[sk * p.D];
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (s + k < p.S) {
+        q[(s + k) * per] = h;
+        h = s + k == 0 ? v[0] : fmaf(fast_exp2(A2 * w[k]), h, v[k]);  // the first ran from the initial state
+      }
   }
 }
 
@@ -296,16 +307,17 @@ __global__ __launch_bounds__(256) void k_scan_step(StepDev p) {
   }
 }
 
-int elem(int dtype) { return dtype == 1 ? 2 : 4; }
-
-// Segments: enough waves to hold two on every SIMD, in segments of 256 tokens and more.
+// Segments: enough waves for four on every SIMD, of 8 tokens and more; for eight where segments stay longer than
+// 128 tokens (439 against 447 us at T = 8192, 4 x 2048 channels, 835 against 864 at T = 65536, 2048 channels; the
+// states of segments are written and read twice, which costs short ones more than it gives).
 ScanSplit split(int64_t B, int64_t T, int64_t D, int64_t G) {
-  const int64_t waves = B * G * ceil_div(D / G, kBlock) * kWaves;
+  const int64_t waves = B * G * ceil_div(D / G, 64);
   ScanSplit s;
-  int64_t want = waves >= 1024 ? 1 : ceil_div(2048, waves);
-  const int64_t most = ceil_div(T, 256);
+  int64_t want = waves >= 4096 ? 1 : ceil_div(4096, waves);
+  if (want > 1 && T / want >= 256) want = ceil_div(8192, waves);
+  const int64_t most = ceil_div(T, 8);
   if (want > most) want = most;
-  s.len = ceil_div(ceil_div(T, want), 64) * 64;
+  s.len = ceil_div(ceil_div(T, want), kStep) * kStep;
   s.S = ceil_div(T, s.len);
   return s;
 }
@@ -315,56 +327,56 @@ int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
 }  // namespace
 
 int scan_state_blocks(int64_t N) { return N <= 16 ? 1 : (N <= 32 ? 2 : 4); }
-int64_t scan_chunk(int64_t N) { return 64 / scan_state_blocks(N); }
 int64_t scan_states_bytes(int64_t B, int64_t T, int64_t D, int64_t N) {
-  return B * ceil_div(T, scan_chunk(N)) * D * 16 * scan_state_blocks(N) * 4;
+  return B * ceil_div(T, kScanChunk) * D * 16 * scan_state_blocks(N) * 4;
 }
-int64_t scan_fwd_workspace(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) {
-  const ScanSplit s = split(B, T, D, G);
-  if (s.S == 1) return 0;
-  return align256(B * s.S * D * 16 * scan_state_blocks(N) * 4) + align256(B * s.S * D * 4);
+namespace {
+struct FwdLayout {
+  ScanSplit split;
+  int64_t seg_d, total;  // the segments' states come first
+};
+FwdLayout layout(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) {
+  const int64_t NP = 16 * scan_state_blocks(N);
+  FwdLayout l;
+  l.split = split(B, T, D, G);
+  l.seg_d = l.split.S > 1 ? align256(B * l.split.S * D * NP * 4) : 0;
+  l.total = l.seg_d + (l.split.S > 1 ? align256(B * l.split.S * D * 4) : 0);
+  return l;
 }
 
-template <typename T>
-static hipError_t run_fwd(const ScanDev& p, int nb, hipStream_t st) {
-  const int64_t per = int64_t(p.cblocks) * p.B;
-  const dim3 first(unsigned(per * (p.S - 1))), second(unsigned(per * p.S)), threads(64 * kWaves);
+template <typename T, int NB>
+hipError_t run_fwd(const ScanDev& p, hipStream_t st) {
+  constexpr int NP = 16 * NB;
+  const int64_t per = int64_t(p.cblocks) * p.B, join = p.B * p.D * NP;
   if (p.S > 1) {
-    if (nb == 1) k_scan_fwd<T, 1, false, false><<<first, threads, 0, st>>>(p);
-    else if (nb == 2) k_scan_fwd<T, 2, false, false><<<first, threads, 0, st>>>(p);
-    else k_scan_fwd<T, 4, false, false><<<first, threads, 0, st>>>(p);
+    k_scan_fwd<T, NB, false, false><<<dim3(unsigned(per * (p.S - 1))), 64 * kWaves, 0, st>>>(p);
+    k_scan_join<<<dim3(unsigned(ceil_div(join, 256))), 256, 0, st>>>(p, NP, join);
   }
-  if (p.z.p) {
-    if (nb == 1) k_scan_fwd<T, 1, true, true><<<second, threads, 0, st>>>(p);
-    else if (nb == 2) k_scan_fwd<T, 2, true, true><<<second, threads, 0, st>>>(p);
-    else k_scan_fwd<T, 4, true, true><<<second, threads, 0, st>>>(p);
-  } else {
-    if (nb == 1) k_scan_fwd<T, 1, true, false><<<second, threads, 0, st>>>(p);
-    else if (nb == 2) k_scan_fwd<T, 2, true, false><<<second, threads, 0, st>>>(p);
-    else k_scan_fwd<T, 4, true, false><<<second, threads, 0, st>>>(p);
-  }
+  const dim3 grid(unsigned(per * p.S));
+  if (p.z.p) k_scan_fwd<T, NB, true, true><<<grid, 64 * kWaves, 0, st>>>(p);
+  else k_scan_fwd<T, NB, true, false><<<grid, 64 * kWaves, 0, st>>>(p);
   return hipGetLastError();
 }
+}  // namespace
+
+int64_t scan_fwd_workspace(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) { return layout(B, T, D, N, G).total; }
 
 hipError_t launch_scan_fwd(const ScanArgs& a, hipStream_t st) {
-  const int nb = scan_state_blocks(a.N), e = elem(a.dtype);
-  const ScanSplit s = split(a.B, a.T, a.D, a.G);
+  const int nb = scan_state_blocks(a.N);
+  const FwdLayout l = layout(a.B, a.T, a.D, a.N, a.G);
   ScanDev p = {};
   p.x = a.x, p.dt = a.dt, p.z = a.z, p.Bm = a.Bm, p.Cm = a.Cm;
   p.A = a.A, p.skip = a.skip, p.dt_bias = a.dt_bias, p.h0 = a.h0, p.lengths = a.lengths;
   p.h_final = a.h_final, p.states = a.states, p.y = a.y;
-  p.T = a.T, p.D = a.D, p.chunks = ceil_div(a.T, scan_chunk(a.N));
-  p.N = int(a.N), p.Dg = int(a.D / a.G);
+  p.T = a.T, p.D = a.D, p.chunks = ceil_div(a.T, kScanChunk);
+  p.N = int(a.N), p.G = int(a.G), p.Dg = int(a.D / a.G);
   p.blocks = int(ceil_div(p.Dg, kBlock)), p.cblocks = int(p.blocks * a.G);
-  p.S = int(s.S), p.B = int(a.B), p.len = s.len;
+  p.S = int(l.split.S), p.B = int(a.B), p.len = l.split.len;
   p.softplus = a.softplus;
-  p.vec = p.Dg % 4 == 0 && rows_aligned(a.x, e, 4) && rows_aligned(a.dt, e, 4) &&
-          (!a.z.p || rows_aligned(a.z, e, 4)) && rows_aligned(Rows{a.y, a.T * a.D, a.D}, e, 4);
-  if (s.S > 1) {
-    p.seg_h = static_cast<float*>(a.workspace);
-    p.seg_d = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + align256(a.B * s.S * a.D * 16 * nb * 4));
-  }
-  return a.dtype == 1 ? run_fwd<__bf16>(p, nb, st) : run_fwd<float>(p, nb, st);
+  char* ws = static_cast<char*>(a.workspace);
+  p.seg_h = reinterpret_cast<float*>(ws), p.seg_d = reinterpret_cast<float*>(ws + l.seg_d);
+  if (a.dtype == 1) return nb == 1 ? run_fwd<__bf16, 1>(p, st) : (nb == 2 ? run_fwd<__bf16, 2>(p, st) : run_fwd<__bf16, 4>(p, st));
+  return nb == 1 ? run_fwd<float, 1>(p, st) : (nb == 2 ? run_fwd<float, 2>(p, st) : run_fwd<float, 4>(p, st));
 }
 
 hipError_t launch_scan_step(const ScanArgs& a, hipStream_t st) {

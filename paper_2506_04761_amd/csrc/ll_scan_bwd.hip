@@ -4,13 +4,19 @@
 //   dA_n = sum_t D_t q_tn,   dB_tn = sum_d g_tdn D_td x_td,   dC_tn = sum_d dy_td h_tdn,
 // where dy is the gradient before the gate: d_y silu(z).
 //
-// The layout of lanes, and the split of the length into segments, are the forward's: k_scan_rev runs every
-// segment backwards by itself (carry G = a g, from zero), k_scan_bwd starts each from the carries of the
-// segments after it.  It needs the states too: from the state saved before every chunk it first runs the
-// chunk forwards, keeping the state before each tile of 8 tokens in LDS, then takes the tiles last to first,
-// forming a tile's rates and states again in registers.  A wave holds two blocks of 16 channels, so that
-// the sums over channels (dB, dC) are half added before lanes are; the four waves of a workgroup are added
-// in LDS, workgroups by k_scan_bc.
+// The split of the length into segments is the forward's: k_scan_rev runs every segment backwards by itself (carry
+// G = a g, from zero; lanes and staging as in k_scan_fwd), k_scan_join_rev turns these into the carries that segments
+// start from, and k_scan_bwd runs them from there.
+//
+// k_scan_bwd has to add over channels as well as over states, so it spreads both over lanes: lane (r, c) =
+// (lane / 16, lane % 16) holds states 4r .. 4r+3 of channel c, for two blocks of 16 channels one after the other, so
+// that the sums over channels (dB, dC) are half added before lanes are.  B and C are the same for all channels: one
+// register per 4 tokens holds them with lane (r, m) = token m / 4, state 4r + m % 4, and a product takes its factor
+// as a row-broadcast (DPP) operand.  Step sizes, inputs and dy pass through LDS, 16 tokens x 32 channels to a wave,
+// eight channels of a token to a lane, and the sums over states come back the same way.  A chunk of 16 tokens starts
+// from the state that the forward saved before it: it is run once for the states before its tiles of 4 tokens, then
+// the tiles are taken last to first, forming rates and states again in registers.  The four waves of a workgroup are added in
+// LDS, workgroups by k_scan_bc.
 #include "ll_layer.hpp"
 #include "ll_layer_device.hpp"
 
@@ -18,12 +24,15 @@ namespace ll {
 
 namespace {
 
-constexpr int kTile = 8;          // tokens of a tile
+constexpr int kChunk = kScanChunk;
+constexpr int kTile = 4;          // tokens whose rates and states are in registers
 constexpr int kWaves = 4;
 constexpr int kCG = 2;            // blocks of 16 channels of a wave
 constexpr int kWaveCh = 16 * kCG;
 constexpr int kBlock = kWaveCh * kWaves;
-constexpr int kRevTile = 16;
+constexpr int kRevBlock = 256;    // channels of a workgroup of k_scan_rev
+constexpr int kStep = 4;          // tokens that k_scan_rev loads together
+constexpr int kRows = 32;         // tokens whose C it stages together
 constexpr float kLn2 = 0.6931471805599453f;
 
 struct BwdDev {
@@ -33,8 +42,8 @@ struct BwdDev {
   const void* dy;
   void *dx, *ddt, *dz, *dB, *dC;
   float *seg_g, *seg_d, *part_bc, *part, *dh0;
-  int64_t T, D, chunks, T4, len;  // T4: groups of four tokens, padded to whole tiles
-  int N, G, Dg, blocks, cblocks, rev_blocks, rev_cblocks, S, B;
+  int64_t T, D, chunks, T4, len, flen;  // T4: groups of four tokens, padded to whole chunks; tokens of a (fine) segment
+  int N, G, Dg, blocks, cblocks, rev_blocks, rev_cblocks, S, F, R, B;  // segments, fine segments, R fine ones to a segment
   int softplus, vec;
 };
 
@@ -48,140 +57,163 @@ __device__ inline int64_t live_tokens(const int32_t* lengths, int64_t b, int64_t
   return n < 0 ? 0 : (n > T ? T : n);
 }
 
-template <int... I, typename F>
-__device__ inline void unrolled(std::integer_sequence<int, I...>, F&& f) {
-  (f(std::integral_constant<int, I>{}), ...);
-}
-
-// A segment backwards by itself: lanes and staging as in the forward kernel.
+// A fine segment backwards by itself.
 template <typename T, int NB, bool GATED>
-__global__ __launch_bounds__(256) void k_scan_rev(BwdDev p) {
-  constexpr int NP = 16 * NB;
-  typedef typename VecN<T, 4>::type V4;
-  __shared__ float2 s_dy[kWaves][kRevTile][16];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane >> 4, c = lane & 15;
+__global__ __launch_bounds__(256, NB == 1 ? 4 : (NB == 2 ? 2 : 1)) void k_scan_rev(BwdDev p) {
+  constexpr int NP = 16 * NB, STAGE = kRows * NP / 256;
+  __shared__ float s_row[2][kRows][NP];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   int64_t id = blockIdx.x;
   const int cb = int(id % p.rev_cblocks);
   id /= p.rev_cblocks;
-  const int seg = 1 + int(id % (p.S - 1)), b = int(id / (p.S - 1));  // nothing comes before segment 0
-  const int g = cb / p.rev_blocks, c0 = (cb % p.rev_blocks) * 64 + wave * 16;
-  if (c0 >= p.Dg) return;
-  const int nch = p.Dg - c0 < 16 ? p.Dg - c0 : 16;
-  const int64_t ch0 = int64_t(g) * p.Dg + c0, ch = ch0 + (c < nch ? c : nch - 1);
-  float A2[NB][4], G[NB][4];
+  const int seg = 1 + int(id % (p.F - 1)), b = int(id / (p.F - 1));  // nothing comes before segment 0
+  const int g = cb / p.rev_blocks, c0 = (cb % p.rev_blocks) * kRevBlock + wave * 64;
+  const bool mine = c0 + lane < p.Dg;         // spare lanes repeat the group's last channel and store nothing
+  const int c = mine ? lane : p.Dg - 1 - c0;  // may be negative: a spare wave, which only helps to stage
+  const int64_t ch0 = int64_t(g) * p.Dg + c0, ch = ch0 + c;
+  float A2[NP], G[NP];
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int n = nb * 16 + 4 * r + i;
-      A2[nb][i] = n < p.N ? p.A[ch * p.N + n] * kLog2e : 0.0f;
-      G[nb][i] = seg == p.S - 1 && p.dh_final && n < p.N ? p.dh_final[(int64_t(b) * p.D + ch) * p.N + n] : 0.0f;
-    }
-  const int64_t t_begin = int64_t(seg) * p.len, t_end = t_begin + p.len < p.T ? t_begin + p.len : p.T;
+  for (int n = 0; n < NP; ++n) {
+    A2[n] = n < p.N ? p.A[ch * p.N + n] * kLog2e : 0.0f;
+    G[n] = seg == p.F - 1 && p.dh_final && n < p.N ? p.dh_final[(int64_t(b) * p.D + ch) * p.N + n] : 0.0f;
+  }
+  const float bias = p.dt_bias ? p.dt_bias[ch] : 0.0f;
+  const int64_t t_begin = int64_t(seg) * p.flen, t_end = t_begin + p.flen < p.T ? t_begin + p.flen : p.T;
   const int64_t live = live_tokens(p.lengths, b, p.T), end = live < t_end ? live : t_end;
-  const int ts = lane >> 2, cs = 4 * (lane & 3);
-  const int mine = nch - cs < 0 ? 0 : (nch - cs > 4 ? 4 : nch - cs);
-  const T* dp = static_cast<const T*>(p.dt.p) + b * p.dt.sb + ch0;
-  const T* zp = static_cast<const T*>(p.z.p) + b * p.z.sb + ch0;
-  const T* gp = static_cast<const T*>(p.dy) + int64_t(b) * p.T * p.D + ch0;
-  const T* Cp = static_cast<const T*>(p.Cm.p) + b * p.Cm.sb + int64_t(g) * p.N;
-  float bias[4];
+  const int count = __builtin_amdgcn_readfirstlane(end > t_begin ? int(end - t_begin) : 0);
+  // token i, counted from the end
+  const T* dp = static_cast<const T*>(p.dt.p) + b * p.dt.sb + (end - 1) * p.dt.st + ch0;
+  const T* zp = static_cast<const T*>(p.z.p) + b * p.z.sb + (end - 1) * p.z.st + ch0;
+  const T* gp = static_cast<const T*>(p.dy) + (int64_t(b) * p.T + end - 1) * p.D + ch0;
+  const T* Cp = static_cast<const T*>(p.Cm.p) + b * p.Cm.sb + (end - 1) * p.Cm.st + int64_t(g) * p.N;
+  T stage[STAGE];
+  auto fetch_rows = [&](int i0) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) bias[i] = p.dt_bias && i < mine ? p.dt_bias[ch0 + cs + i] : 0.0f;
-  V4 dr = {}, zr = {}, gr = {};
-  T cr[NB][4];
-  auto fetch = [&](int64_t t0) {
-    const int left = end - t0 < kRevTile ? int(end - t0) : kRevTile;
-    if (left <= 0) return;
-    const int row = ts < left ? ts : left - 1;
-    dr = load_row4<T>(dp + t0 * p.dt.st, row, p.dt.st, cs, nch, p.vec);
-    gr = load_row4<T>(gp + t0 * p.D, row, p.D, cs, nch, p.vec);
-    if (GATED) zr = load_row4<T>(zp + t0 * p.z.st, row, p.z.st, cs, nch, p.vec);
+    for (int k = 0; k < STAGE; ++k) {
+      const int e = threadIdx.x + 256 * k, i = i0 + e / NP, n = e % NP;
+      stage[k] = i < count && n < p.N ? (Cp - int64_t(i) * p.Cm.st)[n] : from_f32<T>(0.0f);
+    }
+  };
+  T dr[kStep], zr[kStep], gr[kStep];
+  int ahead = 0;  // tokens fetched; before the first that one is fetched again, and masked when used
+  auto fetch = [&] {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int rj = 4 * j + (c >> 2) < left ? 4 * j + (c >> 2) : left - 1;
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const int n = nb * 16 + 4 * r + (c & 3) < p.N ? nb * 16 + 4 * r + (c & 3) : 0;
-        cr[nb][j] = load_at<T>(Cp + t0 * p.Cm.st, rj, p.Cm.st, n);
-      }
+    for (int k = 0; k < kStep; ++k) {
+      dr[k] = load_at<T>(dp, 0, 0, c);
+      gr[k] = load_at<T>(gp, 0, 0, c);
+      if (GATED) zr[k] = load_at<T>(zp, 0, 0, c);
+      const bool more = ++ahead < count;
+      dp -= more ? p.dt.st : 0;
+      gp -= more ? p.D : 0;
+      if (GATED) zp -= more ? p.z.st : 0;
     }
   };
   float dsum = 0.0f;
-  const int64_t last = t_begin + (t_end - 1 - t_begin) / kRevTile * kRevTile;
-  fetch(last);
-  for (int64_t t0 = last; t0 >= t_begin; t0 -= kRevTile) {
-    {
-      const bool in = ts < end - t0;
-      float2 v[4];
+  auto run = [&](const float (*rows)[NP], int i0) {
+    float d[kStep], e[kStep];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float d = to_f32(T(dr[i])) + bias[i], e = to_f32(T(gr[i]));
-        if (p.softplus) d = softplusf(d);
-        if (GATED) e *= silu(to_f32(T(zr[i])));
-        v[i] = make_float2(in ? d : 0.0f, in ? e : 0.0f);
-      }
-      wave_sync();
-      float4* q = reinterpret_cast<float4*>(&s_dy[wave][ts][cs]);
-      q[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
-      q[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
-      wave_sync();
+    for (int k = 0; k < kStep; ++k) {
+      d[k] = to_f32(dr[k]) + bias;
+      e[k] = to_f32(gr[k]);
+      if (GATED) e[k] *= silu(to_f32(zr[k]));
     }
-    float Cv[NB][4];
+    if (i0 + kStep < count) fetch();
+    if (p.softplus) {
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
+      for (int k = 0; k < kStep; ++k) d[k] = softplusf(d[k]);
+    }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bool ok = 4 * j + (c >> 2) < end - t0 && nb * 16 + 4 * r + (c & 3) < p.N;
-        Cv[nb][j] = ok ? to_f32(cr[nb][j]) : 0.0f;
+    for (int k = 0; k < kStep; ++k)
+      if (i0 + k >= count) d[k] = e[k] = 0.0f;
+    f32x4 now = *reinterpret_cast<const f32x4*>(&rows[0][0]), next = now;
+#pragma unroll
+    for (int k = 0; k < kStep; ++k) {
+      dsum += d[k];
+#pragma unroll
+      for (int q = 0; q < NP; q += 4) {
+        if (k * NP + q + 4 < kStep * NP) next = *reinterpret_cast<const f32x4*>(&rows[0][0] + k * NP + q + 4);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) G[q + i] = fmaf(now[i], e[k], G[q + i]) * fast_exp2(d[k] * A2[q + i]);
+        now = next;
       }
-    if (t0 > t_begin) fetch(t0 - kRevTile);
+    }
+  };
+  const bool works = c0 < p.Dg;
+  fetch_rows(0);
+  if (works && count > 0) fetch();
+  for (int i0 = 0; i0 < count; i0 += kRows) {
+    float(*rows)[NP] = s_row[i0 / kRows & 1];
 #pragma unroll
-    for (int j = 3; j >= 0; --j)
-      unrolled(std::make_integer_sequence<int, 4>{}, [&](auto K) {
-        constexpr int k = 3 - decltype(K)::value;
-        const float2 v = s_dy[wave][4 * j + k][c];
-        dsum += v.x;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          axpy4_bcast<4 * k>(G[nb], Cv[nb][j], v.y);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) G[nb][i] *= fast_exp2(v.x * A2[nb][i]);
-        }
-      });
+    for (int k = 0; k < STAGE; ++k) (&rows[0][0])[threadIdx.x + 256 * k] = to_f32(stage[k]);
+    __syncthreads();
+    if (i0 + kRows < count) fetch_rows(i0 + kRows);
+    if (!works) continue;
+    const int n = count - i0 < kRows ? count - i0 : kRows;
+    for (int i = 0; i < n; i += kStep) run(rows + i, i0 + i);
   }
-  if (c < nch) {
-    float* q = p.seg_g + rec(b, seg, p.S, p.D, ch, NP) + 4 * r;
+  if (mine) {
+    float* q = p.seg_g + rec(b, seg, p.F, p.D, ch, NP);
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-      *reinterpret_cast<f32x4*>(q + 16 * nb) = f32x4{G[nb][0], G[nb][1], G[nb][2], G[nb][3]};
-    if (r == 0) p.seg_d[(int64_t(b) * p.S + seg) * p.D + ch] = dsum;
+    for (int n = 0; n < NP; n += 4) *reinterpret_cast<f32x4*>(q + n) = f32x4{G[n], G[n + 1], G[n + 2], G[n + 3]};
+    p.seg_d[(int64_t(b) * p.F + seg) * p.D + ch] = dsum;
+  }
+}
+
+// In place: a segment's own carry becomes the carry that it starts from (at its last token).
+__global__ __launch_bounds__(256) void k_scan_join_rev(BwdDev p, int NP, int64_t total) {
+  constexpr int U = 32;  // segments whose loads are in flight together
+  const int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (id >= total) return;
+  const int64_t per = p.D * NP, b = id / per, e = id - b * per, ch = e / NP;
+  const int n = int(e - ch * NP);
+  const float A2 = n < p.N ? p.A[ch * p.N + n] * kLog2e : 0.0f;
+  float g = p.dh_final && n < p.N ? p.dh_final[(b * p.D + ch) * p.N + n] : 0.0f;
+  float* q = p.seg_g + b * p.F * per + e;
+  const float* d = p.seg_d + b * p.F * p.D + ch;
+  for (int s = p.F - 1; s >= 0; s -= U) {
+    float v[U], w[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int sk = s - k > 0 ? s - k : p.F - 1;  // the first segment has no record of its own
+      v[k] = q[sk * per];
+      w[k] = d[sk * p.D];
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (s - k >= 0) {
+        q[(s - k) * per] = g;
+        g = s - k == p.F - 1 ? v[0] : fmaf(fast_exp2(A2 * w[k]), g, v[k]);  // the last ran from the final gradient
+      }
   }
 }
 
 template <typename T, int NB, bool GATED>
 __global__ __launch_bounds__(256, 2) void k_scan_bwd(BwdDev p) {
   constexpr int NP = 16 * NB;
-  constexpr int CH = 64 / NB;          // tokens of a chunk
-  constexpr int TILES = CH / kTile;
-  constexpr bool OVER = NB == 1;       // a tile's sums may take the place of its staged inputs
-  typedef typename VecN<T, 4>::type V4;
-  __shared__ f32x4 s_h[kWaves][TILES - 1][kCG][NB][64];   // states before tiles 1, 2, ..
-  __shared__ float2 s_du[kWaves][kTile][kWaveCh];         // step size, step size times input
-  __shared__ float s_dy[kWaves][kTile][kWaveCh];
-  __shared__ float2 s_sum[OVER ? 1 : kWaves][kTile][kWaveCh];
-  __shared__ float s_out[OVER ? 1 : kWaves][kTile][kWaveCh];
-  __shared__ float s_bc[2][kWaves][4][64];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane >> 4, c = lane & 15;
+  constexpr int TILES = kChunk / kTile;
+  constexpr bool OVER = NB == 1;  // a tile's sums may take the place of its staged inputs
+  typedef typename VecN<T, 8>::type V8;
+  // rows padded for lanes that write one token each
+  __shared__ float2 s_du[kWaves][kChunk][kWaveCh + 2];  // step size, step size times input; then sums of B g, of A2 q
+  __shared__ float s_dy[kWaves][kChunk][kWaveCh + 4];   // dy; then sums of C h
+  __shared__ float2 s_sum[OVER ? 1 : kWaves][kChunk][kWaveCh + 2];
+  __shared__ float s_out[OVER ? 1 : kWaves][kChunk][kWaveCh + 4];
+  __shared__ float s_row[2][2][kChunk][NP];             // B and C of a chunk
+  __shared__ f32x4 s_h[kWaves][TILES - 1][kCG][64];  // states before tiles 1, 2, ..
+  __shared__ float s_bc[2][kWaves][2 * TILES][64];
+  __shared__ float s_par[kWaves][2][kWaveCh];        // bias, skip
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane >> 4, c = lane & 15;
 
   int64_t id = blockIdx.x;
   const int cb = int(id % p.cblocks);
   id /= p.cblocks;
   const int seg = int(id % p.S), b = int(id / p.S);
   const int grp = cb / p.blocks, c0 = (cb % p.blocks) * kBlock + wave * kWaveCh;
-  const int nch = p.Dg - c0 < 0 ? 0 : (p.Dg - c0 > kWaveCh ? kWaveCh : p.Dg - c0);  // may be none: the wave only meets barriers
+  const int nch = p.Dg - c0 < 0 ? 0 : (p.Dg - c0 > kWaveCh ? kWaveCh : p.Dg - c0);  // may be none: the wave adds zeros
   const int64_t ch0 = int64_t(grp) * p.Dg + c0;
 
+  const int fine = (seg + 1) * p.R < p.F ? (seg + 1) * p.R - 1 : p.F - 1;  // the segment's last fine one
   // Spare lanes and states have rate, state and gradient zero, so that they add nothing to any sum.
   float A2[kCG][NB][4], g[kCG][NB][4], dA[kCG][NB][4];
 #pragma unroll
@@ -193,29 +225,17 @@ __global__ __launch_bounds__(256, 2) void k_scan_bwd(BwdDev p) {
         const int n = nb * 16 + 4 * r + i, cc = 16 * k + c;
         const bool ok = cc < nch && n < p.N;
         A2[k][nb][i] = ok ? p.A[(ch0 + cc) * p.N + n] * kLog2e : 0.0f;
-        g[k][nb][i] = ok && seg == p.S - 1 && p.dh_final ? p.dh_final[(int64_t(b) * p.D + ch0 + cc) * p.N + n] : 0.0f;
+        g[k][nb][i] = 0.0f;
+        if (ok && p.F > 1) g[k][nb][i] = p.seg_g[rec(b, fine, p.F, p.D, ch0 + cc, NP) + n];
+        else if (ok && p.dh_final) g[k][nb][i] = p.dh_final[(int64_t(b) * p.D + ch0 + cc) * p.N + n];
         dA[k][nb][i] = 0.0f;
-      }
-  for (int s = p.S - 1; s > seg; --s)
-#pragma unroll
-    for (int k = 0; k < kCG; ++k)
-      if (16 * k + c < nch) {
-        const int64_t ch = ch0 + 16 * k + c;
-        const float d = p.seg_d[(int64_t(b) * p.S + s) * p.D + ch];
-        const float* q = p.seg_g + rec(b, s, p.S, p.D, ch, NP) + 4 * r;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          const f32x4 v = *reinterpret_cast<const f32x4*>(q + 16 * nb);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) g[k][nb][i] = fmaf(fast_exp2(A2[k][nb][i] * d), g[k][nb][i], v[i]);
-        }
       }
 
   const int64_t t_begin = int64_t(seg) * p.len, t_end = t_begin + p.len < p.T ? t_begin + p.len : p.T;
   const int64_t live = live_tokens(p.lengths, b, p.T), end = live < t_end ? live : t_end;
-  // staging: lane = token lane / 8 of the tile, channels 4 (lane % 8) .. + 3
-  const int ts = lane >> 3, cs = 4 * (lane & 7);
-  const int mine = nch - cs < 0 ? 0 : (nch - cs > 4 ? 4 : nch - cs);
+  // staging: lane (r, c) = channels 8 r .. 8 r + 7 of token c of the chunk
+  const int ts = c, cs = 8 * r;
+  const int own = nch - cs < 0 ? 0 : (nch - cs > 8 ? 8 : nch - cs);
   const int64_t base = int64_t(b) * p.T * p.D + ch0;
   const T* xp = static_cast<const T*>(p.x.p) + b * p.x.sb + ch0;
   const T* dp = static_cast<const T*>(p.dt.p) + b * p.dt.sb + ch0;
@@ -223,234 +243,232 @@ __global__ __launch_bounds__(256, 2) void k_scan_bwd(BwdDev p) {
   const T* gp = static_cast<const T*>(p.dy) + base;
   const T* Bp = static_cast<const T*>(p.Bm.p) + b * p.Bm.sb + int64_t(grp) * p.N;
   const T* Cp = static_cast<const T*>(p.Cm.p) + b * p.Cm.sb + int64_t(grp) * p.N;
-  float bias[4], skip[4], dskip[4], dbias[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    bias[i] = p.dt_bias && i < mine ? p.dt_bias[ch0 + cs + i] : 0.0f;
-    skip[i] = p.skip && i < mine ? p.skip[ch0 + cs + i] : 0.0f;
-    dskip[i] = dbias[i] = 0.0f;
+  if (lane < kWaveCh) {
+    s_par[wave][0][lane] = p.dt_bias && lane < nch ? p.dt_bias[ch0 + lane] : 0.0f;
+    s_par[wave][1][lane] = p.skip && lane < nch ? p.skip[ch0 + lane] : 0.0f;
   }
-  V4 xr = {}, dr = {}, zr = {}, gr = {};
-  T br[NB][2], cr[NB][2];
-  // A tile's inputs; `all`: those of the backward too.  Rows from the end of the sequence on repeat its last
-  // and are masked when used.
-  auto fetch = [&](int64_t t0, bool all) {
-    const int left = end - t0 < kTile ? int(end - t0) : kTile;
-    if (left <= 0 || nch == 0) return;
-    const int row = ts < left ? ts : left - 1;
-    xr = load_row4<T>(xp + t0 * p.x.st, row, p.x.st, cs, nch, p.vec);
-    dr = load_row4<T>(dp + t0 * p.dt.st, row, p.dt.st, cs, nch, p.vec);
-    if (all) {
-      gr = load_row4<T>(gp + t0 * p.D, row, p.D, cs, nch, p.vec);
-      if (GATED) zr = load_row4<T>(zp + t0 * p.z.st, row, p.z.st, cs, nch, p.vec);
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int rj = 4 * j + (c >> 2) < left ? 4 * j + (c >> 2) : left - 1;
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        const int n = nb * 16 + 4 * r + (c & 3) < p.N ? nb * 16 + 4 * r + (c & 3) : 0;
-        br[nb][j] = load_at<T>(Bp + t0 * p.Bm.st, rj, p.Bm.st, n);
-        if (all) cr[nb][j] = load_at<T>(Cp + t0 * p.Cm.st, rj, p.Cm.st, n);
-      }
-    }
+  float dparam = 0.0f;  // lane (r, m): the sum of dskip (m < 8) or dbias of channel 8 r + m % 8
+  // p.vec: the rows' channels are whole vectors of eight, at their alignment; own is 0 or 8
+  auto load8 = [&](const T* q, int row, int64_t stride) {
+    const char* at = reinterpret_cast<const char*>(q) + (unsigned(row) * unsigned(stride) + unsigned(cs)) * unsigned(sizeof(T));
+    return load_n<T, 8>(reinterpret_cast<const T*>(at), own, p.vec);
   };
-  // whether this lane's entry of B and C (token 4 j + c / 4 of the tile, state nb 16 + 4 r + c % 4) is an input
-  auto used = [&](int64_t t0, int nb, int j) { return 4 * j + (c >> 2) < end - t0 && nb * 16 + 4 * r + (c & 3) < p.N; };
-  auto step_size = [&](float v) { return p.softplus ? softplusf(v) : v; };
-  auto stage_du = [&](bool in, float* delta) {
-    float u[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool ok = in && i < mine;
-      delta[i] = ok ? step_size(to_f32(T(dr[i])) + bias[i]) : 0.0f;
-      u[i] = ok ? delta[i] * to_f32(T(xr[i])) : 0.0f;
-    }
-    float4* q = reinterpret_cast<float4*>(&s_du[wave][ts][cs]);
-    q[0] = make_float4(delta[0], u[0], delta[1], u[1]);
-    q[1] = make_float4(delta[2], u[2], delta[3], u[3]);
-  };
-  auto load_states = [&](int64_t chunk, int k, int nb) {
-    const int cc = 16 * k + c;
-    return cc < nch ? *reinterpret_cast<const f32x4*>(p.states + rec(b, chunk, p.chunks, p.D, ch0 + cc, NP) + 16 * nb + 4 * r)
-                    : f32x4{0, 0, 0, 0};
+  auto store8 = [&](void* q, int64_t t0, const float* f) {
+    char* at = reinterpret_cast<char*>(static_cast<T*>(q) + base + t0 * p.D) +
+               (unsigned(ts) * unsigned(p.D) + unsigned(cs)) * unsigned(sizeof(T));
+    store_n<T, 8>(reinterpret_cast<T*>(at), f, own, p.vec);
   };
 
-  int buf = 0;
-  const int64_t last_chunk = (t_end - 1) / CH, first_chunk = t_begin / CH;
-  fetch(last_chunk * CH, false);
-  for (int64_t chunk = last_chunk; chunk >= first_chunk; --chunk) {
-    const int64_t tc = chunk * CH;
-    const int tiles = int((t_end - tc < CH ? t_end - tc : CH) + kTile - 1) / kTile;
-    f32x4 h0[kCG][NB];
+  V8 xr = {}, dr = {}, zr = {}, gr = {};
+  T bc[2 * NB];  // the workgroup's B and C of a chunk: value e = threadIdx.x + 256 i of [B or C][token][state]
+  f32x4 hr[kCG][NB];
+#pragma unroll
+  for (int k = 0; k < kCG; ++k)
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) hr[k][nb] = f32x4{0, 0, 0, 0};  // what a wave without channels works on
+  // A chunk's inputs and the states before it.  Rows from the end of the sequence on repeat its last and are
+  // masked when used.
+  auto fetch = [&](int64_t chunk) {
+    const int64_t t0 = chunk * kChunk;
+    const int left = end - t0 < kChunk ? int(end - t0) : kChunk;
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i) {
+      const int e = threadIdx.x + 256 * i, t = e / NP % kChunk, n = e % NP;
+      const bool is_c = i >= NB;
+      bc[i] = t < left && n < p.N ? load_at<T>((is_c ? Cp : Bp) + t0 * (is_c ? p.Cm.st : p.Bm.st), t, is_c ? p.Cm.st : p.Bm.st, n)
+                                  : from_f32<T>(0.0f);
+    }
+    if (nch == 0) return;
+    const float* hp = p.states + rec(b, chunk, p.chunks, p.D, ch0, NP);
 #pragma unroll
     for (int k = 0; k < kCG; ++k)
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) h0[k][nb] = load_states(chunk, k, nb);
-    // forwards: the states before tiles 1, 2, ..
-    for (int tile = 0; tile + 1 < tiles; ++tile) {
-      const int64_t t0 = tc + tile * kTile;
-      float delta[4], Bv[NB][2];
-      wave_sync();
-      stage_du(ts < end - t0, delta);
-      wave_sync();
-#pragma unroll
       for (int nb = 0; nb < NB; ++nb)
+        if (16 * k + c < nch) hr[k][nb] = *reinterpret_cast<const f32x4*>(reinterpret_cast<const char*>(hp) + unsigned((16 * k + c) * NP + 16 * nb + 4 * r) * 4);
+    if (left <= 0) return;
+    const int row = ts < left ? ts : left - 1;
+    xr = load8(xp + t0 * p.x.st, row, p.x.st);
+    dr = load8(dp + t0 * p.dt.st, row, p.dt.st);
+    gr = load8(gp + t0 * p.D, row, p.D);
+    if (GATED) zr = load8(zp + t0 * p.z.st, row, p.z.st);
+  };
+  auto stage_rows = [&](int buf) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) Bv[nb][j] = used(t0, nb, j) ? to_f32(br[nb][j]) : 0.0f;
-      fetch(t0 + kTile, tile + 2 == tiles);
-      if (nch > 0) {
+    for (int i = 0; i < 2 * NB; ++i) (&s_row[buf][0][0][0])[threadIdx.x + 256 * i] = to_f32(bc[i]);
+  };
+
+  int buf = 0;
+  const int64_t last_chunk = (t_end - 1) / kChunk, first_chunk = t_begin / kChunk;
+  fetch(last_chunk);
+  stage_rows(0);
+  __syncthreads();
+  for (int64_t chunk = last_chunk; chunk >= first_chunk; --chunk) {
+    const int64_t t0 = chunk * kChunk;
+    const bool in = ts < end - t0;
+    const V8 xk = xr, dk = dr, zk = zr, gk = gr;
+    wave_sync();
 #pragma unroll
-        for (int k = 0; k < kCG; ++k)
-          unrolled(std::make_integer_sequence<int, kTile>{}, [&](auto K) {
-            constexpr int t = decltype(K)::value;
-            const float2 du = s_du[wave][t][16 * k + c];
+    for (int i = 0; i < 8; i += 2) {
+      float d[2], u[2], e[2];
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-              unrolled(std::make_integer_sequence<int, 4>{}, [&](auto I) {
-                constexpr int i = decltype(I)::value;
-                h0[k][nb][i] = fmaf(fast_exp2(du.x * A2[k][nb][i]), h0[k][nb][i],
-                                    row_bcast<4 * (t & 3) + i>(Bv[nb][t >> 2]) * du.y);
-              });
-          });
-#pragma unroll
-        for (int k = 0; k < kCG; ++k)
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) s_h[wave][tile][k][nb][lane] = h0[k][nb];
+      for (int j = 0; j < 2; ++j) {
+        const bool ok = in && i + j < own;
+        d[j] = to_f32(T(dk[i + j])) + s_par[wave][0][cs + i + j];
+        if (p.softplus) d[j] = softplusf(d[j]);
+        e[j] = to_f32(T(gk[i + j]));
+        if (GATED) e[j] *= silu(to_f32(T(zk[i + j])));
+        u[j] = ok ? d[j] * to_f32(T(xk[i + j])) : 0.0f;
+        d[j] = ok ? d[j] : 0.0f;
+        e[j] = ok ? e[j] : 0.0f;
       }
+      *reinterpret_cast<float4*>(&s_du[wave][ts][cs + i]) = make_float4(d[0], u[0], d[1], u[1]);
+      *reinterpret_cast<float2*>(&s_dy[wave][ts][cs + i]) = make_float2(e[0], e[1]);
     }
-    if (tiles == 1) fetch(tc, true);
-    // backwards
-    for (int tile = tiles - 1; tile >= 0; --tile) {
-      const int64_t t0 = tc + tile * kTile;
-      const bool in = ts < end - t0;
-      float delta[4], dyg[4];
-      const V4 xk = xr, dk = dr, zk = zr, gk = gr;
-      wave_sync();
-      stage_du(in, delta);
+    wave_sync();
+    f32x4 first[kCG][NB];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        dyg[i] = to_f32(T(gk[i]));
-        if (GATED) dyg[i] *= silu(to_f32(T(zk[i])));
-        dyg[i] = in && i < mine ? dyg[i] : 0.0f;
-      }
-      *reinterpret_cast<float4*>(&s_dy[wave][ts][cs]) = make_float4(dyg[0], dyg[1], dyg[2], dyg[3]);
-      wave_sync();
-      float Bv[NB][2], Cv[NB][2];
+    for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          Bv[nb][j] = used(t0, nb, j) ? to_f32(br[nb][j]) : 0.0f;
-          Cv[nb][j] = used(t0, nb, j) ? to_f32(cr[nb][j]) : 0.0f;
-        }
-      if (tile > 0) fetch(t0 - kTile, true);
-      else if (chunk > first_chunk) fetch(tc - CH, false);
+      for (int k = 0; k < kCG; ++k) first[k][nb] = hr[k][nb];
+    const int rb = int(last_chunk - chunk) & 1;
+    // lane (r, m)'s B or C of a tile: token m / 4, state 4 r + m % 4
+    auto row4 = [&](int which, int tile, int nb) { return s_row[rb][which][4 * tile + (c >> 2)][16 * nb + 4 * r + (c & 3)]; };
+    if (chunk > first_chunk) fetch(chunk - 1);
 
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        float db[2][16], dc[2][16];
-        if (nch > 0) {
+    for (int nb = 0; nb < NB; ++nb) {
+      // forwards through all tiles but the last, for the states between them
+      {
+#pragma unroll
+        for (int k = 0; k < kCG; ++k) {
+          f32x4 h = first[k][nb];
+#pragma unroll
+          for (int tile = 0; tile + 1 < TILES; ++tile) {
+            const float Bv = row4(0, tile, nb);
+            float2 du[kTile];
+#pragma unroll
+            for (int t = 0; t < kTile; ++t) du[t] = s_du[wave][kTile * tile + t][16 * k + c];
+            unrolled(std::make_integer_sequence<int, kTile>{}, [&](auto K) {
+              constexpr int t = decltype(K)::value;
+              unrolled(std::make_integer_sequence<int, 4>{}, [&](auto I) {
+                constexpr int i = decltype(I)::value;
+                h[i] = fmaf(fast_exp2(du[t].x * A2[k][nb][i]), h[i], row_bcast<4 * t + i>(Bv) * du[t].y);
+              });
+            });
+            s_h[wave][tile][k][lane] = h;
+          }
+        }
+      }
+      // backwards, tile by tile
+#pragma unroll
+      for (int tile = TILES - 1; tile >= 0; --tile) {
+        const float Bv = row4(0, tile, nb), Cv = row4(1, tile, nb);
+        float db[16], dc[16];
+        {
           unrolled(std::make_integer_sequence<int, kCG>{}, [&](auto KK) {
             constexpr int k = decltype(KK)::value;
             __builtin_amdgcn_sched_barrier(0);
-            float a[kTile][4], h[kTile + 1][4];
-            const f32x4 hs = tile > 0 ? s_h[wave][tile > 0 ? tile - 1 : 0][k][nb][lane] : load_states(chunk, k, nb);
+            float a[kTile][4], h[kTile + 1][4], dy[kTile];
+            float2 du[kTile];
+            const f32x4 hs = tile > 0 ? s_h[wave][tile > 0 ? tile - 1 : 0][k][lane] : first[k][nb];
+#pragma unroll
+            for (int t = 0; t < kTile; ++t) {
+              du[t] = s_du[wave][kTile * tile + t][16 * k + c];
+              dy[t] = s_dy[wave][kTile * tile + t][16 * k + c];
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) h[0][i] = hs[i];
             unrolled(std::make_integer_sequence<int, kTile>{}, [&](auto K) {
               constexpr int t = decltype(K)::value;
-              const float2 du = s_du[wave][t][16 * k + c];
               unrolled(std::make_integer_sequence<int, 4>{}, [&](auto I) {
                 constexpr int i = decltype(I)::value;
-                a[t][i] = fast_exp2(du.x * A2[k][nb][i]);
-                h[t + 1][i] = fmaf(a[t][i], h[t][i], row_bcast<4 * (t & 3) + i>(Bv[nb][t >> 2]) * du.y);
+                a[t][i] = fast_exp2(du[t].x * A2[k][nb][i]);
+                h[t + 1][i] = fmaf(a[t][i], h[t][i], row_bcast<4 * t + i>(Bv) * du[t].y);
               });
             });
+            __builtin_amdgcn_sched_barrier(0);
+            float sx[4], sq[4], sy[4];
+            unrolled(std::make_integer_sequence<int, 4>{}, [&](auto K) {
+              constexpr int t = 3 - decltype(K)::value;
+              grad_token<4 * t, GATED>(g[k][nb], Bv, Cv, dy[t], h[t + 1], sx[t], sy[t]);
+              float q;
 #pragma unroll
-            for (int j = 1; j >= 0; --j) {
-              __builtin_amdgcn_sched_barrier(0);  // no work of another half tile in flight: registers are full
-              float sx[4], sq[4], sy[4];
-              unrolled(std::make_integer_sequence<int, 4>{}, [&](auto K) {
-                constexpr int m = 3 - decltype(K)::value;
-                const int t = 4 * j + m;
-                const float2 du = s_du[wave][t][16 * k + c];
-                const float dy = s_dy[wave][t][16 * k + c];
-                axpy4_bcast<4 * m>(g[k][nb], Cv[nb][j], dy);
-                sx[m] = dot4_bcast<4 * m>(0.0f, Bv[nb][j], g[k][nb]);
-                sy[m] = GATED ? dot4_bcast<4 * m>(0.0f, Cv[nb][j], h[t + 1]) : 0.0f;
-                float q = 0.0f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  db[j][4 * m + i] = k == 0 ? du.y * g[k][nb][i] : fmaf(du.y, g[k][nb][i], db[j][4 * m + i]);
-                  dc[j][4 * m + i] = k == 0 ? dy * h[t + 1][i] : fmaf(dy, h[t + 1][i], dc[j][4 * m + i]);
-                  g[k][nb][i] *= a[t][i];
-                  const float gh = g[k][nb][i] * h[t][i];
-                  dA[k][nb][i] = fmaf(du.x, gh, dA[k][nb][i]);
-                  q = fmaf(A2[k][nb][i], gh, q);
-                }
-                sq[m] = q;
-              });
-              // the four tokens' inputs have been read: their sums may stand there
-              float2 v = make_float2(sum_rows4(sx[0], sx[1], sx[2], sx[3]), sum_rows4(sq[0], sq[1], sq[2], sq[3]));
-              float y = GATED ? sum_rows4(sy[0], sy[1], sy[2], sy[3]) : 0.0f;
-              if (OVER) {
-                wave_sync();
-                s_du[wave][4 * j + r][16 * k + c] = v;
-                s_dy[wave][4 * j + r][16 * k + c] = y;
-              } else {
-                if (nb > 0) {
-                  const float2 o = s_sum[OVER ? 0 : wave][4 * j + r][16 * k + c];
-                  v.x += o.x, v.y += o.y;
-                  y += s_out[OVER ? 0 : wave][4 * j + r][16 * k + c];
-                }
-                s_sum[OVER ? 0 : wave][4 * j + r][16 * k + c] = v;
-                s_out[OVER ? 0 : wave][4 * j + r][16 * k + c] = y;
+              for (int i = 0; i < 4; ++i) {
+                db[4 * t + i] = k == 0 ? du[t].y * g[k][nb][i] : fmaf(du[t].y, g[k][nb][i], db[4 * t + i]);
+                dc[4 * t + i] = k == 0 ? dy[t] * h[t + 1][i] : fmaf(dy[t], h[t + 1][i], dc[4 * t + i]);
+                g[k][nb][i] *= a[t][i];
+                const float gh = g[k][nb][i] * h[t][i];
+                dA[k][nb][i] = fmaf(du[t].x, gh, dA[k][nb][i]);
+                q = i == 0 ? A2[k][nb][i] * gh : fmaf(A2[k][nb][i], gh, q);
               }
+              sq[t] = q;
+            });
+            // formed here, not where they are used (the compiler would keep all their terms until then)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(dA[k][nb][i]));
+#pragma unroll
+            for (int i = 0; i < 16; ++i) asm volatile("" : "+v"(db[i]), "+v"(dc[i]));
+            // row r of the sums is token r of the tile
+            float2 v = make_float2(sum_rows4(sx[0], sx[1], sx[2], sx[3]), sum_rows4(sq[0], sq[1], sq[2], sq[3]));
+            float y = GATED ? sum_rows4(sy[0], sy[1], sy[2], sy[3]) : 0.0f;
+            const int t = kTile * tile + r;
+            if (OVER) {  // the wave has read the tile's inputs
+              wave_sync();
+              s_du[wave][t][16 * k + c] = v;
+              s_dy[wave][t][16 * k + c] = y;
+            } else {
+              if (nb > 0) {
+                const float2 o = s_sum[OVER ? 0 : wave][t][16 * k + c];
+                v.x += o.x, v.y += o.y;
+                y += s_out[OVER ? 0 : wave][t][16 * k + c];
+              }
+              s_sum[OVER ? 0 : wave][t][16 * k + c] = v;
+              s_out[OVER ? 0 : wave][t][16 * k + c] = y;
             }
           });
+          __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
-        // sums over the channels: lanes of a row, then the waves
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          s_bc[buf][wave][j][lane] = nch > 0 ? sum_lanes16(db[j]) : 0.0f;
-          s_bc[buf][wave][2 + j][lane] = nch > 0 ? sum_lanes16(dc[j]) : 0.0f;
-        }
-        __syncthreads();  // the other buffer is free: all waves have passed the barrier after its sums were read
-        {
-          const float v = (s_bc[buf][0][wave][lane] + s_bc[buf][1][wave][lane]) +
-                          (s_bc[buf][2][wave][lane] + s_bc[buf][3][wave][lane]);
-          const int64_t t4 = t0 / 4 + (wave & 1);
-          p.part_bc[((((int64_t(wave >> 1) * p.B + b) * p.cblocks + cb) * p.T4 + t4) * NB + nb) * 64 + lane] = v;
-        }
-        buf ^= 1;
+        // the sums over this wave's channels, lane (r, m): token m / 4 of the tile, state 4 r + m % 4
+        s_bc[buf][wave][tile][lane] = sum_lanes16(db);
+        s_bc[buf][wave][TILES + tile][lane] = sum_lanes16(dc);
       }
-      // outputs, four channels of a token to a lane
-      wave_sync();
-      if (mine > 0 && ts < t_end - t0) {
-        const float4 w0 = *reinterpret_cast<const float4*>(OVER ? &s_du[wave][ts][cs] : &s_sum[OVER ? 0 : wave][ts][cs]);
-        const float4 w1 = *reinterpret_cast<const float4*>(OVER ? &s_du[wave][ts][cs + 2] : &s_sum[OVER ? 0 : wave][ts][cs + 2]);
-        const float4 w2 = *reinterpret_cast<const float4*>(OVER ? &s_dy[wave][ts][cs] : &s_out[OVER ? 0 : wave][ts][cs]);
-        const float sx[4] = {w0.x, w0.z, w1.x, w1.z}, sq[4] = {w0.y, w0.w, w1.y, w1.w}, sy[4] = {w2.x, w2.y, w2.z, w2.w};
-        float ox[4], od[4], oz[4];
+      if (nb == NB - 1 && chunk > first_chunk) stage_rows(rb ^ 1);
+      __syncthreads();  // the other buffers are free: all waves have passed this barrier after they were read
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x = to_f32(T(xk[i])), zf = GATED ? to_f32(T(zk[i])) : 0.0f;
-          ox[i] = in ? fmaf(delta[i], sx[i], skip[i] * dyg[i]) : 0.0f;
-          float dd = fmaf(x, sx[i], kLn2 * sq[i]);
-          if (p.softplus) dd *= sigmoidf(to_f32(T(dk[i])) + bias[i]);
-          od[i] = in ? dd : 0.0f;
-          if (GATED) oz[i] = in ? to_f32(T(gk[i])) * fmaf(skip[i], x, sy[i]) * silu_grad(zf, sigmoidf(zf)) : 0.0f;
-          dskip[i] += in ? dyg[i] * x : 0.0f;
-          dbias[i] += od[i];
-        }
-        const int64_t at = base + t0 * p.D;
-        store_row4<T>(static_cast<T*>(p.dx) + at, ts, p.D, cs, ox, mine, p.vec);
-        store_row4<T>(static_cast<T*>(p.ddt) + at, ts, p.D, cs, od, mine, p.vec);
-        if (GATED) store_row4<T>(static_cast<T*>(p.dz) + at, ts, p.D, cs, oz, mine, p.vec);
+      for (int i = 0; i < 2 * TILES / kWaves; ++i) {
+        const int e = wave * (2 * TILES / kWaves) + i, which = e / TILES, tile = e % TILES;
+        const float v = (s_bc[buf][0][e][lane] + s_bc[buf][1][e][lane]) + (s_bc[buf][2][e][lane] + s_bc[buf][3][e][lane]);
+        (p.part_bc + ((((int64_t(which) * p.B + b) * p.cblocks + cb) * p.T4 + t0 / 4 + tile) * NB + nb) * 64)[lane] = v;
       }
+      buf ^= 1;
     }
+    // outputs, eight channels of a token to a lane
+    wave_sync();
+    float sums[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sums[i] = 0.0f;
+    if (own > 0 && ts < t_end - t0) {
+      float ox[8], od[8], oz[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float2 s = OVER ? s_du[wave][ts][cs + i] : s_sum[OVER ? 0 : wave][ts][cs + i];
+        const float sy = OVER ? s_dy[wave][ts][cs + i] : s_out[OVER ? 0 : wave][ts][cs + i];
+        const float x = to_f32(T(xk[i])), v = to_f32(T(dk[i])) + s_par[wave][0][cs + i], skip = s_par[wave][1][cs + i];
+        const float dout = to_f32(T(gk[i])), z = GATED ? to_f32(T(zk[i])) : 0.0f, sg = GATED ? sigmoidf(z) : 1.0f;
+        const float dy = GATED ? dout * (z * sg) : dout;
+        ox[i] = in ? fmaf(p.softplus ? softplusf(v) : v, s.x, skip * dy) : 0.0f;
+        float dd = fmaf(x, s.x, kLn2 * s.y);
+        if (p.softplus) dd *= sigmoidf(v);
+        od[i] = in ? dd : 0.0f;
+        if (GATED) oz[i] = in ? dout * fmaf(skip, x, sy) * silu_grad(z, sg) : 0.0f;
+        sums[i] = in ? dy * x : 0.0f;
+        sums[8 + i] = od[i];
+      }
+      store8(p.dx, t0, ox);
+      store8(p.ddt, t0, od);
+      if (GATED) store8(p.dz, t0, oz);
+    }
+    dparam += sum_lanes16(sums);
   }
 
   // the segment's sums over tokens: dA, dskip, dbias; and before token 0 the state's gradient
@@ -468,18 +486,7 @@ __global__ __launch_bounds__(256, 2) void k_scan_bwd(BwdDev p) {
           if (seg == 0 && p.dh0 && n < p.N) p.dh0[(int64_t(b) * p.D + ch) * p.N + n] = g[k][nb][i];
         }
     }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-#pragma unroll
-    for (int m = 8; m < 64; m <<= 1) {
-      dskip[i] += __shfl_xor(dskip[i], m);
-      dbias[i] += __shfl_xor(dbias[i], m);
-    }
-    if (ts == 0 && i < mine) {
-      row[p.D * NP + ch0 + cs + i] = dskip[i];
-      row[p.D * (NP + 1) + ch0 + cs + i] = dbias[i];
-    }
-  }
+  if ((c & 7) < own) row[p.D * (NP + (c >> 3)) + ch0 + cs + (c & 7)] = dparam;
 }
 
 // dB and dC from the workgroups' sums over channels: a lane adds a group's workgroups.
@@ -511,22 +518,28 @@ __global__ __launch_bounds__(256) void k_scan_bc(BwdDev p, int64_t total) {
 int elem(int dtype) { return dtype == 1 ? 2 : 4; }
 int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
 
-// Segments: two workgroups on every compute unit.
+// Segments: two workgroups of k_scan_bwd on every compute unit; split further for k_scan_rev, to four waves on
+// every SIMD.
 struct BwdLayout {
-  int64_t S, len, T4, seg_g, seg_d, bc, part, total;
+  int64_t S, len, F, flen, R, T4, seg_g, seg_d, bc, part, total;
 };
 BwdLayout layout(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) {
   BwdLayout l;
-  const int64_t NP = 16 * scan_state_blocks(N), wgs = B * G * ceil_div(D / G, kBlock);
-  int64_t want = ceil_div(512, wgs);
-  const int64_t most = ceil_div(T, 64);
-  if (want > most) want = most;
-  l.len = ceil_div(ceil_div(T, want), 64) * 64;
+  const int64_t NP = 16 * scan_state_blocks(N), wgs = B * G * ceil_div(D / G, kBlock), most = ceil_div(T, kChunk);
+  const int64_t rev = B * G * ceil_div(D / G, 64);
+  int64_t want = ceil_div(512, wgs), fine = ceil_div(4096, rev);
+  want = want > most ? most : want;
+  fine = fine > most ? most : fine;
+  fine = fine < want ? want : fine;
+  l.flen = ceil_div(ceil_div(T, fine), kChunk) * kChunk;
+  l.R = ceil_div(ceil_div(T, want), l.flen);
+  l.len = l.R * l.flen;
   l.S = ceil_div(T, l.len);
-  l.T4 = ceil_div(T, kTile) * (kTile / 4);
+  l.F = ceil_div(T, l.flen);
+  l.T4 = ceil_div(T, kChunk) * (kChunk / 4);
   l.seg_g = 0;
-  l.seg_d = l.seg_g + (l.S > 1 ? align256(B * l.S * D * NP * 4) : 0);
-  l.bc = l.seg_d + (l.S > 1 ? align256(B * l.S * D * 4) : 0);
+  l.seg_d = l.seg_g + (l.F > 1 ? align256(B * l.F * D * NP * 4) : 0);
+  l.bc = l.seg_d + (l.F > 1 ? align256(B * l.F * D * 4) : 0);
   l.part = l.bc + align256(2 * wgs * l.T4 * NP * 4 * 4);
   l.total = l.part + align256(B * l.S * D * (NP + 2) * 4);
   return l;
@@ -534,8 +547,11 @@ BwdLayout layout(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) {
 
 template <typename T, int NB, bool GATED>
 void go_main(const BwdDev& p, hipStream_t st) {
-  if (p.S > 1)
-    k_scan_rev<T, NB, GATED><<<dim3(unsigned(int64_t(p.rev_cblocks) * p.B * (p.S - 1))), 256, 0, st>>>(p);
+  if (p.F > 1) {
+    const int64_t join = int64_t(p.B) * p.D * 16 * NB;
+    k_scan_rev<T, NB, GATED><<<dim3(unsigned(int64_t(p.rev_cblocks) * p.B * (p.F - 1))), 256, 0, st>>>(p);
+    k_scan_join_rev<<<dim3(unsigned(ceil_div(join, 256))), 256, 0, st>>>(p, 16 * NB, join);
+  }
   k_scan_bwd<T, NB, GATED><<<dim3(unsigned(int64_t(p.cblocks) * p.B * p.S)), 256, 0, st>>>(p);
 }
 
@@ -550,7 +566,10 @@ hipError_t go(const BwdDev& p, hipStream_t st) {
 
 }  // namespace
 
-int64_t scan_bwd_workspace(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) { return layout(B, T, D, N, G).total; }
+int64_t scan_bwd_workspace(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) {
+  const int64_t own = layout(B, T, D, N, G).total, fwd = scan_fwd_workspace(B, T, D, N, G);
+  return own > fwd ? own : fwd;  // one workspace serves both
+}
 
 hipError_t launch_scan_bwd(const ScanArgs& a, const ScanGrads& g, hipStream_t st) {
   const int nb = scan_state_blocks(a.N), e = elem(a.dtype);
@@ -563,14 +582,14 @@ hipError_t launch_scan_bwd(const ScanArgs& a, const ScanGrads& g, hipStream_t st
   char* ws = static_cast<char*>(a.workspace);
   p.seg_g = reinterpret_cast<float*>(ws + l.seg_g), p.seg_d = reinterpret_cast<float*>(ws + l.seg_d);
   p.part_bc = reinterpret_cast<float*>(ws + l.bc), p.part = reinterpret_cast<float*>(ws + l.part);
-  p.T = a.T, p.D = a.D, p.chunks = ceil_div(a.T, scan_chunk(a.N)), p.T4 = l.T4, p.len = l.len;
+  p.T = a.T, p.D = a.D, p.chunks = ceil_div(a.T, kScanChunk), p.T4 = l.T4, p.len = l.len, p.flen = l.flen;
   p.N = int(a.N), p.G = int(a.G), p.Dg = int(a.D / a.G);
   p.blocks = int(ceil_div(p.Dg, kBlock)), p.cblocks = int(p.blocks * a.G);
-  p.rev_blocks = int(ceil_div(p.Dg, 64)), p.rev_cblocks = int(p.rev_blocks * a.G);
-  p.S = int(l.S), p.B = int(a.B), p.softplus = a.softplus;
+  p.rev_blocks = int(ceil_div(p.Dg, kRevBlock)), p.rev_cblocks = int(p.rev_blocks * a.G);
+  p.S = int(l.S), p.F = int(l.F), p.R = int(l.R), p.B = int(a.B), p.softplus = a.softplus;
   const Rows flat[4] = {{g.dy, 0, a.D}, {g.dx, 0, a.D}, {g.ddt, 0, a.D}, {g.dz, 0, a.D}};
-  p.vec = p.Dg % 4 == 0 && rows_aligned(a.x, e, 4) && rows_aligned(a.dt, e, 4) && (!a.z.p || rows_aligned(a.z, e, 4));
-  for (const Rows& r : flat) p.vec = p.vec && rows_aligned(r, e, 4);
+  p.vec = p.Dg % 8 == 0 && rows_aligned(a.x, e, 16 / e) && rows_aligned(a.dt, e, 16 / e) && (!a.z.p || rows_aligned(a.z, e, 16 / e));
+  for (const Rows& r : flat) p.vec = p.vec && rows_aligned(r, e, 16 / e);
   hipError_t err;
   if (a.dtype == 1) err = nb == 1 ? go<__bf16, 1>(p, st) : (nb == 2 ? go<__bf16, 2>(p, st) : go<__bf16, 4>(p, st));
   else err = nb == 1 ? go<float, 1>(p, st) : (nb == 2 ? go<float, 2>(p, st) : go<float, 4>(p, st));

@@ -95,9 +95,9 @@ def test_scan_checks_return_before_launch():
 
 def test_scan_sizes():
     states, ws = lib.ll_selective_scan_states_bytes, lib.ll_selective_scan_workspace_size
-    # the state of 16 (padded) float32 values before every 64th token
-    assert states(2, 65, 8, 5) == 2 * 2 * 8 * 16 * 4 and states(1, 64, 8, 16) == 8 * 16 * 4
-    assert states(1, 64, 8, 17) == 2 * 8 * 32 * 4 and states(1, 64, 8, 64) == 4 * 8 * 64 * 4
+    # the state of 16 (padded) float32 values before every 16th token
+    assert states(2, 65, 8, 5) == 2 * 5 * 8 * 16 * 4 and states(1, 16, 8, 16) == 8 * 16 * 4
+    assert states(1, 64, 8, 17) == 4 * 8 * 32 * 4 and states(1, 64, 8, 64) == 4 * 8 * 64 * 4
     assert states(1, 64, 8, 65) == 0 and states(1, 0, 8, 16) == 0
     assert ws(1, 64, 64, 16, 1, 0) == 0 and ws(1, 64, 64, 16, 1, 1) > 0 and ws(1, 8192, 64, 16, 1, 0) > 0
     assert ws(1, 64, 64, 16, 3, 1) == 0 and ws(0, 64, 64, 16, 1, 1) == 0

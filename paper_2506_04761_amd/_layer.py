@@ -23,8 +23,9 @@ NormGrads = namedtuple("NormGrads", "x weight bias gate")
 
 
 class _ScanInputs(ctypes.Structure):
+    # ll_scan_inputs; its pairs of strides are single fields here, for one constructor call
     _fields_ = ([(n, _vp) for n in ("x", "dt", "z", "B", "C")]
-                + [(n + "_strides", _i64 * 2) for n in ("x", "dt", "z", "B", "C")]
+                + [(n + "_" + axis, _i64) for n in ("x", "dt", "z", "B", "C") for axis in ("batch", "token")]
                 + [(n, _vp) for n in ("A", "D", "dt_bias", "lengths")]
                 + [(n, _i64) for n in ("batch", "T", "channels", "N", "groups")]
                 + [("delta_softplus", _i32), ("dtype", _i32)])
@@ -54,15 +55,17 @@ _declare("ll_group_norm_bwd", [_vp, _i64, _i64] * 2 + [_vp] * 8 + [_i64] * 4 + [
 # ------------------------------------------------------------------------------------ checks
 
 def _rows(t, name, dtype, shape):
-    """Checks columns of wider rows: adjacent channels, any strides of the other axes."""
+    """Checks columns of wider rows: adjacent channels, any strides of the other axes, which it returns."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.stride(-1) != 1 and t.shape[-1] != 1:
+    strides = t.stride()
+    if strides[-1] != 1 and shape[-1] != 1:
         raise ValueError(f"{name} must have adjacent channels (a last stride of 1)")
+    return strides
 
 
 def _opt(t, name, dtype, shape):
@@ -184,35 +187,30 @@ def ll_causal_conv_bwd(x, weight, bias, d_y, act=LL_ACT_SILU, initial_state=None
 # ------------------------------------------------------------------------------------ selective scan
 
 def _scan_inputs(x, dt, A, Bm, Cm, D, z, dt_bias, delta_softplus, lengths, step):
-    """The checked inputs of a scan call, and its sizes.  With `step`, tensors of one token ([B, ...])."""
+    """The checked inputs of a scan call.  With `step`, tensors of one token ([B, ...])."""
     lead = _dims(x, "x", 2 if step else 3)
     nb, ch = lead[0], lead[-1]
-    T = 1 if step else lead[1]
     N = _dims(A, "A", 2)[1]
     dtype = x.dtype
-    _rows(x, "x", dtype, lead)
-    _rows(dt, "dt", dtype, lead)
-    if z is not None:
-        _rows(z, "z", dtype, lead)
+    xs, ds = _rows(x, "x", dtype, lead), _rows(dt, "dt", dtype, lead)
+    zs = (0, 0, 1) if z is None else _rows(z, "z", dtype, lead)
     _check(A, "A", torch.float32, (ch, N))
     # [.., N] for one group, [.., groups, N] for several
     groups = 1 if Bm.dim() == len(lead) else Bm.shape[-2]
     shape = (*lead[:-1], N) if Bm.dim() == len(lead) else (*lead[:-1], groups, N)
-    for t, name in ((Bm, "B"), (Cm, "C")):
-        _rows(t, name, dtype, shape)
-        if len(shape) > len(lead) and t.stride(-2) != N and groups > 1:
-            raise ValueError(f"{name} must have adjacent groups")
-    _opt(D, "D", torch.float32, (ch,))
-    _opt(dt_bias, "dt_bias", torch.float32, (ch,))
-    _lengths(lengths, nb)
-    s = _ScanInputs(x.data_ptr(), dt.data_ptr(), _ptr(z), Bm.data_ptr(), Cm.data_ptr())
-    for t, to in ((x, s.x_strides), (dt, s.dt_strides), (z, s.z_strides), (Bm, s.B_strides), (Cm, s.C_strides)):
-        if t is not None:
-            to[0], to[1] = t.stride(0), 0 if step else t.stride(1)
-    s.A, s.D, s.dt_bias, s.lengths = A.data_ptr(), _ptr(D), _ptr(dt_bias), _ptr(lengths)
-    s.batch, s.T, s.channels, s.N, s.groups = nb, T, ch, N, groups
-    s.delta_softplus, s.dtype = int(bool(delta_softplus)), _dtype_code(x)
-    return s
+    bs, cs = _rows(Bm, "B", dtype, shape), _rows(Cm, "C", dtype, shape)
+    if groups > 1 and (bs[-2] != N or cs[-2] != N):
+        raise ValueError("B and C must have adjacent groups")
+    if D is not None:
+        _check(D, "D", torch.float32, (ch,))
+    if dt_bias is not None:
+        _check(dt_bias, "dt_bias", torch.float32, (ch,))
+    if lengths is not None:
+        _lengths(lengths, nb)
+    T = 1 if step else lead[1]
+    return _ScanInputs(x.data_ptr(), dt.data_ptr(), _ptr(z), Bm.data_ptr(), Cm.data_ptr(), xs[0], xs[1], ds[0], ds[1],
+                       zs[0], zs[1], bs[0], bs[1], cs[0], cs[1], A.data_ptr(), _ptr(D), _ptr(dt_bias), _ptr(lengths), nb,
+                       T, ch, N, groups, 1 if delta_softplus else 0, _dtype_code(x))
 
 
 def ll_selective_scan_workspace(x, B, backward=False):

@@ -2,7 +2,7 @@
 //   v_td = b_d + sum_{j < W} w_dj e_(t+j)d,  e = (the W - 1 tokens before the first, x),  y = act(v).
 //
 // Bound by memory: a token and channel are read and written once (backward: x and dy read, dx written).
-// A lane owns 16 bytes of adjacent channels and walks a run of tokens with the W - 1 tokens before it in
+// A lane owns 8 bytes of adjacent channels and walks a run of tokens with the W - 1 tokens before it in
 // registers, so that a token is read again only by the run after it.
 #include "ll_layer.hpp"
 #include "ll_layer_device.hpp"
@@ -11,7 +11,7 @@ namespace ll {
 
 namespace {
 
-constexpr int kMaxW = 4;
+constexpr int kVecBytes = 8;   // of adjacent channels to a lane
 
 struct ConvDev {
   Rows x;
@@ -27,7 +27,7 @@ struct ConvDev {
   int64_t T, D, total;  // total: threads that have work
   int64_t ncv, runs;    // channel vectors; runs of tokens of a sequence
   int run;              // tokens of a run
-  int act, vec;
+  int act, vec, pvec;   // pvec: a lane's taps and biases are 16-byte aligned
 };
 
 __device__ inline int64_t live_tokens(const int32_t* lengths, int64_t b, int64_t T) {
@@ -36,14 +36,15 @@ __device__ inline int64_t live_tokens(const int32_t* lengths, int64_t b, int64_t
   return n < 0 ? 0 : (n > T ? T : n);
 }
 
-template <typename T, int W, int V>
+template <int W, int V>
 __device__ inline void load_taps(const ConvDev& p, int64_t d0, int n, float (&w)[W][V], float (&bias)[V]) {
+  float t[V * W];
+  load_params<V * W>(p.weight + d0 * W, n * W, 0.0f, p.pvec, t);
+  load_params<V>(p.bias ? p.bias + d0 : nullptr, n, 0.0f, p.pvec, bias);
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    bias[i] = p.bias && i < n ? p.bias[d0 + i] : 0.0f;
+  for (int i = 0; i < V; ++i)
 #pragma unroll
-    for (int j = 0; j < W; ++j) w[j][i] = i < n ? p.weight[(d0 + i) * W + j] : 0.0f;
-  }
+    for (int j = 0; j < W; ++j) w[j][i] = t[i * W + j];
 }
 
 // Token t of sequence b as V floats; t < 0 comes from the state, t >= live and spare channels are zero.
@@ -61,7 +62,7 @@ __device__ inline void token(const ConvDev& p, int64_t b, int64_t t, int64_t liv
 
 template <typename T, int W>
 __global__ __launch_bounds__(256) void k_conv_fwd(ConvDev p) {
-  constexpr int V = 16 / sizeof(T), U = 4;
+  constexpr int V = kVecBytes / sizeof(T), U = 4;
   const int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x;
   if (id >= p.total) return;
   const int64_t cv = id % p.ncv, run = id / p.ncv % p.runs, b = id / p.ncv / p.runs;
@@ -70,7 +71,7 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvDev p) {
   const int64_t t0 = run * p.run, t1 = t0 + p.run < p.T ? t0 + p.run : p.T;
   const int64_t live = live_tokens(p.lengths, b, p.T);
   float w[W][V], bias[V];
-  load_taps<T, W, V>(p, d0, n, w, bias);
+  load_taps<W, V>(p, d0, n, w, bias);
   float e[W - 1 + U][V];
 #pragma unroll
   for (int j = 0; j < W - 1; ++j) token<T, W, V>(p, b, t0 - (W - 1) + j, live, d0, n, e[j]);
@@ -133,7 +134,7 @@ __global__ __launch_bounds__(256) void k_conv_fwd(ConvDev p) {
 
 template <typename T, int W>
 __global__ __launch_bounds__(256) void k_conv_step(ConvDev p) {
-  constexpr int V = 16 / sizeof(T);
+  constexpr int V = kVecBytes / sizeof(T);
   const int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x;
   if (id >= p.total) return;
   const int64_t cv = id % p.ncv, b = id / p.ncv, d0 = cv * V;
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(256) void k_conv_step(ConvDev p) {
   float w[W][V], bias[V], e[W][V], o[V];
 #pragma unroll
   for (int j = 0; j < W; ++j) token<T, W, V>(p, b, j - (W - 1), 1, d0, n, e[j]);
-  load_taps<T, W, V>(p, d0, n, w, bias);
+  load_taps<W, V>(p, d0, n, w, bias);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     float v = bias[i];
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(256) void k_conv_step(ConvDev p) {
 // sums; the workgroup's four runs are added in LDS, and k_colsum adds the workgroups.
 template <typename T, int W>
 __global__ __launch_bounds__(256) void k_conv_bwd(ConvDev p) {
-  constexpr int V = 16 / sizeof(T);
+  constexpr int V = kVecBytes / sizeof(T);
   __shared__ float s_sum[4][64][V + 1];
   const int lane = threadIdx.x & 63, strip = threadIdx.x >> 6;
   int64_t id = blockIdx.x;
@@ -181,7 +182,7 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvDev p) {
     const int64_t t0 = run * p.run, t1 = t0 + p.run < p.T ? t0 + p.run : p.T;
     const int64_t live = live_tokens(p.lengths, b, p.T);
     float w[W][V], bias[V], e[W][V], dv[W][V];
-    load_taps<T, W, V>(p, d0, n, w, bias);
+    load_taps<W, V>(p, d0, n, w, bias);
 #pragma unroll
     for (int j = 0; j < W; ++j) {
       if (j > 0) token<T, W, V>(p, b, t0 - W + j, live, d0, n, e[j]);
@@ -192,7 +193,7 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvDev p) {
     const T* xp = static_cast<const T*>(p.x.p) + b * p.x.sb + d0;
     const T* dfp = p.dfinal ? static_cast<const T*>(p.dfinal) + b * (W - 1) * p.D + d0 : nullptr;
     typedef typename VecN<T, V>::type Vec;
-    constexpr int U = 4;
+    constexpr int U = 2;
     Vec xr[U], gr[U];
     const int64_t last = t1 + W - 1;  // one past the last dv that the run needs
     auto fetch = [&](int64_t t) {
@@ -305,8 +306,8 @@ int run_length(int64_t B, int64_t T, int64_t ncv, int most) {
 }
 
 bool conv_vec(const ConvArgs& a) {
-  const int e = elem(a.dtype), V = 16 / e;
-  auto flat = [&](const void* q) { return !q || reinterpret_cast<uintptr_t>(q) % 16 == 0; };
+  const int e = elem(a.dtype), V = kVecBytes / e;
+  auto flat = [&](const void* q) { return !q || reinterpret_cast<uintptr_t>(q) % kVecBytes == 0; };
   return a.D % V == 0 && rows_aligned(a.x, e, V) && flat(a.y) && flat(a.state) && flat(a.new_state);
 }
 
@@ -314,7 +315,8 @@ ConvDev conv_dev(const ConvArgs& a, int most) {
   ConvDev p = {};
   p.x = a.x, p.weight = a.weight, p.bias = a.bias, p.state = a.state, p.new_state = a.new_state;
   p.lengths = a.lengths, p.y = a.y, p.T = a.T, p.D = a.D, p.act = a.act, p.vec = conv_vec(a);
-  p.ncv = ceil_div(a.D, 16 / elem(a.dtype));
+  p.pvec = p.vec && reinterpret_cast<uintptr_t>(a.weight) % 16 == 0 && reinterpret_cast<uintptr_t>(a.bias) % 16 == 0;
+  p.ncv = ceil_div(a.D, kVecBytes / elem(a.dtype));
   p.run = run_length(a.B, a.T, p.ncv, most);
   p.runs = ceil_div(a.T, p.run);
   p.total = p.ncv * p.runs * a.B;
@@ -349,7 +351,7 @@ void go_bwd(const ConvDev& p, int W, unsigned grid, hipStream_t st) {
 }  // namespace
 
 int64_t conv_bwd_workspace(int64_t B, int64_t T, int64_t D, int64_t W, int dtype) {
-  const int64_t runs = ceil_div(T, run_length(B, T, ceil_div(D, 16 / elem(dtype)), kBwdRun));
+  const int64_t runs = ceil_div(T, run_length(B, T, ceil_div(D, kVecBytes / elem(dtype)), kBwdRun));
   return B * ceil_div(runs, 4) * (W + 1) * D * 4;
 }
 
@@ -376,7 +378,7 @@ hipError_t launch_conv_step(const ConvArgs& a, hipStream_t st) {
 
 hipError_t launch_conv_bwd(const ConvArgs& a, const ConvGrads& g, hipStream_t st) {
   ConvDev p = conv_dev(a, kBwdRun);
-  auto flat = [&](const void* q) { return !q || reinterpret_cast<uintptr_t>(q) % 16 == 0; };
+  auto flat = [&](const void* q) { return !q || reinterpret_cast<uintptr_t>(q) % kVecBytes == 0; };
   p.vec = p.vec && flat(g.dy) && flat(g.dfinal) && flat(g.dx) && flat(g.dinit);
   p.dy = g.dy, p.dfinal = g.dfinal, p.dx = g.dx, p.dinit = g.dinit, p.part = static_cast<float*>(g.workspace);
   const int64_t rows = a.B * ceil_div(p.runs, 4);

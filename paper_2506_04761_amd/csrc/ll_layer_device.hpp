@@ -44,6 +44,22 @@ __device__ inline void store_n(T* p, const float* f, int n, bool vec) {
   }
 }
 
+// N adjacent parameters at p, or `value` without any; the first n are inputs, the others zero.  `vec`: 16-byte aligned.
+template <int N>
+__device__ inline void load_params(const float* p, int n, float value, bool vec, float* f) {
+  if (p && vec && n == N && N % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(p + i);
+#pragma unroll
+      for (int j = 0; j < 4 && i + j < N; ++j) f[i + j] = v[j];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = i < n ? (p ? p[i] : value) : 0.0f;
+  }
+}
+
 // Four adjacent channels c .. c + 3 of row `row` of a tile at `base` (the same for all lanes: a uniform address
 // plus a lane's 32-bit offset), for channels below nch: those beyond repeat channels of the tile, so that every
 // address is one of the tile's own.

@@ -25,7 +25,7 @@ struct NormDev {
   float* part;         // backward: [rows, 2, C] partial sums of du xh and du; slab forward: [N, chunks, ncv, 2]
   float* coef;         // slab backward: [N, G, 2]
   int64_t N, S, C, per, chunks, ncv;  // per: rows form, workgroups over the rows; slab, tokens of a chunk
-  int G, cg, act, vec;
+  int G, cg, act, vec, pvec;  // pvec: weight and bias are 16-byte aligned
   int slots, bpr, rpw;  // rows form: lanes of a row, workgroups of a row, rows of a workgroup
   float eps;
 };
@@ -33,7 +33,7 @@ struct NormDev {
 __device__ inline float act_of(float v, int act) { return act ? silu(v) : v; }
 __device__ inline float act_grad(float v, int act) { return act ? silu_grad(v, sigmoidf(v)) : 1.0f; }
 
-// Sum over LG adjacent lanes (LG = 256: the workgroup), in every lane.
+// Sum over LG adjacent lanes (LG = 256: a strip of the workgroup), in every lane.
 template <int LG>
 __device__ inline float group_sum(float v, float* s) {
   if (LG > 1) v += dpp_mov<0xB1>(v);   // quad_perm 1,0,3,2
@@ -52,19 +52,21 @@ __device__ inline float group_sum(float v, float* s) {
     __syncthreads();
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
     __syncthreads();
+    s += threadIdx.x >> 8 << 2;
     v = (s[0] + s[1]) + (s[2] + s[3]);
   }
   return v;
 }
 
 // What a thread of the rows form works on: vectors lane, lane + LG, .. of one group, in rows first, first + step, ..
-template <int V, int LG>
+// A workgroup is `strips` strips of 256 threads, each a row of its own (or rpw small ones).
 struct RowPlan {
-  int g, lane;
-  int64_t first, step;
+  int g, lane, strip;
+  int64_t part, first, step;
   bool on;
-  __device__ RowPlan(const NormDev& p) {
-    int slot = threadIdx.x, row = 0;
+  __device__ RowPlan(const NormDev& p, int LG, int strips) {
+    strip = threadIdx.x >> 8;
+    int slot = threadIdx.x & 255, row = 0;
     if (p.bpr > 1) {
       slot += int(blockIdx.x % p.bpr) * 256;
     } else {
@@ -75,8 +77,9 @@ struct RowPlan {
     on = row < p.rpw && slot < p.slots;
     g = on ? slot / LG : 0;
     lane = slot % LG;
-    first = blk * p.rpw + row;
-    step = p.per * p.rpw;
+    part = blk * p.rpw + row;
+    first = (blk * strips + strip) * p.rpw + row;
+    step = p.per * strips * p.rpw;
   }
 };
 
@@ -84,7 +87,7 @@ template <typename T, int V, int LG, int PV>
 __global__ __launch_bounds__(256) void k_norm_rows(NormDev p) {
   typedef typename VecN<T, V>::type Vec;
   __shared__ float s[4];
-  const RowPlan<V, LG> q(p);
+  const RowPlan q(p, LG, 1);
   if (LG <= 64 && !q.on) return;
   float w[PV][V], bi[PV][V];
   int off[PV], n[PV];
@@ -93,11 +96,8 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormDev p) {
     const int c = (q.lane + k * LG) * V;  // within the group
     n[k] = c < p.cg ? (p.cg - c < V ? p.cg - c : V) : 0;
     off[k] = q.g * p.cg + (n[k] ? c : 0);
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      w[k][i] = i < n[k] && p.weight ? p.weight[off[k] + i] : (i < n[k] ? 1.0f : 0.0f);
-      bi[k][i] = i < n[k] && p.bias ? p.bias[off[k] + i] : 0.0f;
-    }
+    load_params<V>(p.weight ? p.weight + off[k] : nullptr, n[k], 1.0f, p.pvec, w[k]);
+    load_params<V>(p.bias ? p.bias + off[k] : nullptr, n[k], 0.0f, p.pvec, bi[k]);
   }
   const float inv = 1.0f / float(p.cg);
   const bool gated = p.z.p;
@@ -149,43 +149,47 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormDev p) {
   }
 }
 
-// Gradients of one vector: x centred and scaled to xh in place; returns du and, with a gate, dz.
+// Gradients of one vector: x centred and scaled to xh in place; returns du (in place of dy if asked) and, with a
+// gate, dz.
 template <int V>
 __device__ inline void norm_du(const NormDev& p, bool gated, float mean, float rstd, const float* w, const float* b,
                                const float* dy, const float* z, float* xh, float* du, float* dz) {
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     xh[i] = (xh[i] - mean) * rstd;
-    const float u = fmaf(xh[i], w[i], b[i]);
+    const float u = fmaf(xh[i], w[i], b[i]), d = dy[i];
     if (gated) {
       const float sg = p.act ? sigmoidf(z[i]) : 1.0f;
-      du[i] = dy[i] * (p.act ? z[i] * sg : z[i]);
-      dz[i] = dy[i] * u * (p.act ? silu_grad(z[i], sg) : 1.0f);
+      du[i] = d * (p.act ? z[i] * sg : z[i]);
+      dz[i] = d * u * (p.act ? silu_grad(z[i], sg) : 1.0f);
     } else {
-      du[i] = dy[i] * act_grad(u, p.act);
+      du[i] = d * act_grad(u, p.act);
     }
   }
 }
 
+// Strips of a backward workgroup: four of one vector a lane, fewer of more (registers).
+template <int PV>
+constexpr int kBwdStrips = 4 / PV;
+
 template <typename T, int V, int LG, int PV>
-__global__ __launch_bounds__(256) void k_norm_rows_bwd(NormDev p) {
+__global__ __launch_bounds__(256 * kBwdStrips<PV>) void k_norm_rows_bwd(NormDev p) {
   typedef typename VecN<T, V>::type Vec;
-  __shared__ float s[4];
-  const RowPlan<V, LG> q(p);
-  if (LG <= 64 && !q.on) return;
+  constexpr int STRIPS = kBwdStrips<PV>;
+  __shared__ float s[4 * STRIPS];
+  __shared__ float s_sum[STRIPS > 1 ? STRIPS - 1 : 1][V][256];
+  const RowPlan q(p, LG, STRIPS);
   float w[PV][V], bi[PV][V], dw[PV][V], db[PV][V];
   int off[PV], n[PV];
 #pragma unroll
   for (int k = 0; k < PV; ++k) {
     const int c = (q.lane + k * LG) * V;
-    n[k] = c < p.cg ? (p.cg - c < V ? p.cg - c : V) : 0;
+    n[k] = q.on && c < p.cg ? (p.cg - c < V ? p.cg - c : V) : 0;
     off[k] = q.g * p.cg + (n[k] ? c : 0);
+    load_params<V>(p.weight ? p.weight + off[k] : nullptr, n[k], 1.0f, p.pvec, w[k]);
+    load_params<V>(p.bias ? p.bias + off[k] : nullptr, n[k], 0.0f, p.pvec, bi[k]);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      w[k][i] = i < n[k] && p.weight ? p.weight[off[k] + i] : (i < n[k] ? 1.0f : 0.0f);
-      bi[k][i] = i < n[k] && p.bias ? p.bias[off[k] + i] : 0.0f;
-      dw[k][i] = db[k][i] = 0.0f;
-    }
+    for (int i = 0; i < V; ++i) dw[k][i] = db[k][i] = 0.0f;
   }
   const float inv = 1.0f / float(p.cg);
   const bool gated = p.z.p;
@@ -202,23 +206,29 @@ __global__ __launch_bounds__(256) void k_norm_rows_bwd(NormDev p) {
     }
   };
   fetch(q.first);
-  for (int64_t r = q.first; r < p.N; r += q.step) {
-    float x[PV][V], du[PV][V], s1 = 0.0f, s2 = 0.0f;
+  const int64_t rounds = (p.N + q.step - 1) / q.step;  // the same for all threads: sums over strips meet barriers
+  for (int64_t i0 = 0; i0 < rounds; ++i0) {
+    const int64_t r = q.first + i0 * q.step;
+    const bool row = r < p.N;
+    float x[PV][V], du[PV][V], z[PV][V], s1 = 0.0f, s2 = 0.0f;
     const float mean = st.x, rstd = st.y;
 #pragma unroll
-    for (int k = 0; k < PV; ++k) {
-      float z[V], dy[V], dz[V];
+    for (int k = 0; k < PV; ++k)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         x[k][i] = to_f32(T(xr[k][i]));
-        dy[i] = to_f32(T(gr[k][i]));
-        z[i] = gated ? to_f32(T(zr[k][i])) : 0.0f;
+        du[k][i] = to_f32(T(gr[k][i]));
+        z[k][i] = gated ? to_f32(T(zr[k][i])) : 0.0f;
       }
-      norm_du<V>(p, gated, mean, rstd, w[k], bi[k], dy, z, x[k], du[k], dz);
-      if (gated) store_n<T, V>(static_cast<T*>(p.dz) + r * p.C + off[k], dz, n[k], p.vec);
+    fetch(r + q.step);
+#pragma unroll
+    for (int k = 0; k < PV; ++k) {
+      float dz[V];
+      norm_du<V>(p, gated, mean, rstd, w[k], bi[k], du[k], z[k], x[k], du[k], dz);
+      if (gated) store_n<T, V>(static_cast<T*>(p.dz) + r * p.C + off[k], dz, row ? n[k] : 0, p.vec);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        if (i >= n[k]) du[k][i] = 0.0f, x[k][i] = 0.0f;
+        if (i >= n[k] || !row) du[k][i] = 0.0f, x[k][i] = 0.0f;
         db[k][i] += du[k][i];
         dw[k][i] = fmaf(du[k][i], x[k][i], dw[k][i]);
         du[k][i] *= w[k][i];
@@ -226,7 +236,6 @@ __global__ __launch_bounds__(256) void k_norm_rows_bwd(NormDev p) {
         s2 = fmaf(du[k][i], x[k][i], s2);
       }
     }
-    fetch(r + q.step);
     s1 = group_sum<LG>(s1, s) * inv;
     s2 = group_sum<LG>(s2, s) * inv;
 #pragma unroll
@@ -234,15 +243,28 @@ __global__ __launch_bounds__(256) void k_norm_rows_bwd(NormDev p) {
       float o[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) o[i] = rstd * ((du[k][i] - s1) - x[k][i] * s2);
-      store_n<T, V>(static_cast<T*>(p.dx) + r * p.C + off[k], o, n[k], p.vec);
+      store_n<T, V>(static_cast<T*>(p.dx) + r * p.C + off[k], o, row ? n[k] : 0, p.vec);
     }
   }
-  if (p.part && q.on) {
-    float* out = p.part + q.first * 2 * p.C;  // one row of partial sums for each row of the grid
+  if (!p.part) return;
+  // one row of partial sums for the workgroup's strips
+  float* out = p.part + q.part * 2 * p.C;
+  const int at = threadIdx.x & 255;
 #pragma unroll
-    for (int k = 0; k < PV; ++k) {
-      store_n<float, V>(out + off[k], dw[k], n[k], false);
-      store_n<float, V>(out + p.C + off[k], db[k], n[k], false);
+  for (int k = 0; k < 2 * PV; ++k) {
+    float(&v)[V] = k < PV ? dw[k % PV] : db[k % PV];
+    __syncthreads();
+    if (q.strip > 0) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) s_sum[q.strip > 0 ? q.strip - 1 : 0][i][at] = v[i];
+    }
+    __syncthreads();
+    if (q.strip == 0) {
+#pragma unroll
+      for (int j = 0; j < STRIPS - 1; ++j)
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] += s_sum[j][i][at];
+      store_n<float, V>(out + (k < PV ? 0 : p.C) + off[k % PV], v, n[k % PV], false);
     }
   }
 }
@@ -350,11 +372,8 @@ __global__ __launch_bounds__(256) void k_norm_slab_join(NormDev p, int V) {
 
 template <int V>
 __device__ inline void slab_params(const NormDev& p, const SlabPlan& q, float* w, float* b) {
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    w[i] = p.weight ? p.weight[q.cv * V + i] : 1.0f;
-    b[i] = p.bias ? p.bias[q.cv * V + i] : 0.0f;
-  }
+  load_params<V>(p.weight ? p.weight + q.cv * V : nullptr, V, 1.0f, p.pvec, w);
+  load_params<V>(p.bias ? p.bias + q.cv * V : nullptr, V, 0.0f, p.pvec, b);
 }
 
 template <typename T, int V>
@@ -513,17 +532,18 @@ RowShape row_shape(int64_t cg, int V) {
   return r;
 }
 
-// Workgroups over the rows: enough to fill the card several times over, each with rows to keep its
-// channels' weights and sums for.
-int64_t row_blocks(int64_t rows, int rpw, int bpr) {
-  const int64_t all = ceil_div(rows, rpw), want = ceil_div(4096, bpr);
+// Workgroups over the rows.  Forward: up to 16384, of two rows and more (65536 rows of 2048 bf16 with a gate: 146 us,
+// 4096 workgroups 165, 2048, which end in a part of a round, 185).  Backward: 256, of four strips, one to a compute
+// unit; each leaves a row of sums.
+int64_t row_blocks(int64_t rows, int rpw, int bpr, int most, int least) {
+  const int64_t all = ceil_div(rows, rpw * least), want = ceil_div(most, bpr);
   return all < want ? all : want;
 }
 
 // Tokens of a chunk of the slab form, for about 1024 workgroups.
 int64_t slab_chunk(int64_t N, int64_t S, int64_t ncv) {
   const int64_t lanes = ncv < 256 ? ncv : 256, strips = 256 / lanes, cblocks = ceil_div(ncv, lanes);
-  int64_t chunks = ceil_div(2048, N * cblocks);
+  int64_t chunks = ceil_div(1024, N * cblocks);
   const int64_t least = 8 * strips;
   int64_t per = ceil_div(S, chunks);
   return per < least ? least : per;
@@ -543,9 +563,9 @@ void go_rows(const NormDev& p, int PV, unsigned grid, bool bwd, hipStream_t st) 
     else if (LG >= 64 && PV == 2) k_norm_rows<T, V, LG, LG >= 64 ? 2 : 1><<<grid, 256, 0, st>>>(p);
     else k_norm_rows<T, V, LG, LG >= 64 ? 4 : 1><<<grid, 256, 0, st>>>(p);
   } else {
-    if (PV == 1) k_norm_rows_bwd<T, V, LG, 1><<<grid, 256, 0, st>>>(p);
-    else if (LG >= 64 && PV == 2) k_norm_rows_bwd<T, V, LG, LG >= 64 ? 2 : 1><<<grid, 256, 0, st>>>(p);
-    else k_norm_rows_bwd<T, V, LG, LG >= 64 ? 4 : 1><<<grid, 256, 0, st>>>(p);
+    if (PV == 1) k_norm_rows_bwd<T, V, LG, 1><<<grid, 256 * kBwdStrips<1>, 0, st>>>(p);
+    else if (LG >= 64 && PV == 2) k_norm_rows_bwd<T, V, LG, LG >= 64 ? 2 : 1><<<grid, 256 * kBwdStrips<LG >= 64 ? 2 : 1>, 0, st>>>(p);
+    else k_norm_rows_bwd<T, V, LG, LG >= 64 ? 4 : 1><<<grid, 256 * kBwdStrips<LG >= 64 ? 4 : 1>, 0, st>>>(p);
   }
 }
 
@@ -593,8 +613,7 @@ NormPlan plan(int64_t N, int64_t S, int64_t C, int64_t G, int V, bool bwd) {
     q.slots = int(slots);
     q.bpr = int(slots > 256 ? ceil_div(slots, 256) : 1);
     q.rpw = int(slots > 256 ? 1 : 256 / slots);
-    q.per = row_blocks(N, q.rpw, q.bpr);
-    if (bwd) q.per = q.per < ceil_div(1024, q.bpr) ? q.per : ceil_div(1024, q.bpr);
+    q.per = row_blocks(N, bwd ? q.rpw * (4 / q.rows.PV) : q.rpw, q.bpr, bwd ? 256 * q.rows.PV : 16384, bwd ? 1 : 2);
     q.total = bwd ? q.per * q.rpw * 2 * C * 4 : 0;
     return q;
   }
@@ -612,6 +631,7 @@ hipError_t launch(const NormArgs& a, const NormGrads* g, hipStream_t st) {
   const int V = p.vec ? 16 / elem(a.dtype) : 1;
   const NormPlan q = plan(a.N, a.S, a.C, a.G, V, g != nullptr);
   if (V == 1) p.vec = 1;  // one element at a time: always aligned
+  p.pvec = reinterpret_cast<uintptr_t>(a.weight) % 16 == 0 && reinterpret_cast<uintptr_t>(a.bias) % 16 == 0;
   p.x = a.x, p.z = a.z, p.weight = a.weight, p.bias = a.bias, p.y = a.y, p.stats = a.stats;
   p.N = a.N, p.S = a.S, p.C = a.C, p.G = int(a.G), p.cg = int(a.C / a.G), p.act = a.act, p.eps = a.eps;
   p.per = q.per, p.chunks = q.chunks, p.ncv = q.ncv, p.slots = q.slots, p.bpr = q.bpr, p.rpw = q.rpw;

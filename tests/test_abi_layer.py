@@ -54,9 +54,11 @@ def _inputs(**kw):
         setattr(s, n, 4096)
     s.batch, s.T, s.channels, s.N, s.groups, s.delta_softplus, s.dtype = 2, 8, 64, 16, 1, 1, 1
     for k, v in kw.items():
-        if isinstance(v, tuple):
-            v = (ctypes.c_int64 * 2)(*v)
-        setattr(s, k, v)
+        if k.endswith("_strides"):
+            name = k[:-len("_strides")]
+            setattr(s, name + "_batch", v[0]), setattr(s, name + "_token", v[1])
+        else:
+            setattr(s, k, v)
     return s
 
 
@@ -99,7 +101,7 @@ def test_scan_sizes():
     assert states(2, 65, 8, 5) == 2 * 5 * 8 * 16 * 4 and states(1, 16, 8, 16) == 8 * 16 * 4
     assert states(1, 64, 8, 17) == 4 * 8 * 32 * 4 and states(1, 64, 8, 64) == 4 * 8 * 64 * 4
     assert states(1, 64, 8, 65) == 0 and states(1, 0, 8, 16) == 0
-    assert ws(1, 64, 64, 16, 1, 0) == 0 and ws(1, 64, 64, 16, 1, 1) > 0 and ws(1, 8192, 64, 16, 1, 0) > 0
+    assert ws(1, 8, 64, 16, 1, 0) == 0 and ws(1, 64, 64, 16, 1, 1) > 0 and ws(1, 8192, 64, 16, 1, 0) > 0
     assert ws(1, 64, 64, 16, 3, 1) == 0 and ws(0, 64, 64, 16, 1, 1) == 0
 
 

@@ -60,32 +60,11 @@ __device__ inline void load_params(const float* p, int n, float value, bool vec,
   }
 }
 
-// Four adjacent channels c .. c + 3 of row `row` of a tile at `base` (the same for all lanes: a uniform address
-// plus a lane's 32-bit offset), for channels below nch: those beyond repeat channels of the tile, so that every
-// address is one of the tile's own.
-template <typename T>
-__device__ inline typename VecN<T, 4>::type load_row4(const T* base, int row, int64_t stride, int c, int nch, bool vec) {
-  typedef typename VecN<T, 4>::type V4;
-  const char* q = reinterpret_cast<const char*>(base);
-  const unsigned at = unsigned(row) * unsigned(stride);
-  if (vec) return *reinterpret_cast<const V4*>(q + (at + unsigned(c < nch ? c : 0)) * unsigned(sizeof(T)));
-  V4 v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    v[i] = *reinterpret_cast<const T*>(q + (at + unsigned(c + i < nch ? c + i : nch - 1)) * unsigned(sizeof(T)));
-  return v;
-}
+// Element n of row `row` at `base` (the same for all lanes: a uniform address plus a lane's 32-bit offset).
 template <typename T>
 __device__ inline T load_at(const T* base, int row, int64_t stride, int n) {
   return *reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + (unsigned(row) * unsigned(stride) + unsigned(n)) * unsigned(sizeof(T)));
 }
-// The first n of four channels of row `row` of a tile.
-template <typename T>
-__device__ inline void store_row4(T* base, int row, int64_t stride, int c, const float* f, int n, bool vec) {
-  char* q = reinterpret_cast<char*>(base) + (unsigned(row) * unsigned(stride) + unsigned(c)) * unsigned(sizeof(T));
-  store_n<T, 4>(reinterpret_cast<T*>(q), f, n, vec);
-}
-
 // 1 / (1 + e^-v); v_exp_f32 and v_rcp_f32 are each within 1 ulp.
 __device__ inline float sigmoidf(float v) { return __builtin_amdgcn_rcpf(1.0f + fast_exp2(-kLog2e * v)); }
 __device__ inline float silu(float v) { return v * sigmoidf(v); }

@@ -68,9 +68,10 @@ __device__ inline void save_state(float* q, const float* h) {
   for (int n = 0; n < NP; n += 4) *reinterpret_cast<f32x4*>(q + n) = f32x4{h[n], h[n + 1], h[n + 2], h[n + 3]};
 }
 
-template <typename T, int NB, bool OUT, bool GATED>
-__global__ __launch_bounds__(64 * kWaves, NB == 1 ? 4 : (NB == 2 ? 2 : 1)) void k_scan_fwd(ScanDev p) {
-  constexpr int NP = 16 * NB, CH = kScanChunk;
+// NP: states of a lane, N rounded up to one of a few sizes.
+template <typename T, int NP, bool OUT, bool GATED>
+__global__ __launch_bounds__(64 * kWaves, NP <= 16 ? 4 : (NP <= 24 ? 3 : (NP <= 32 ? 2 : 1))) void k_scan_fwd(ScanDev p) {
+  constexpr int CH = kScanChunk, RP = (NP + 15) / 16 * 16;  // states of a saved record
   constexpr int W = OUT ? 2 * NP : NP, STAGE = kRows * W / 256;  // values of a token's row; of a tile and thread
   __shared__ float s_row[2][kRows][W];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -192,7 +193,12 @@ __global__ __launch_bounds__(64 * kWaves, NB == 1 ? 4 : (NB == 2 ? 2 : 1)) void 
     yp += kStep * p.D;
   };
   auto save = [&](int64_t t) {
-    if (OUT && p.states && t % CH == 0 && mine) save_state<NP>(p.states + rec(b, t / CH, p.chunks, p.D, ch, NP), h);
+    if (OUT && p.states && t % CH == 0 && mine) {
+      float* q = p.states + rec(b, t / CH, p.chunks, p.D, ch, RP);
+      save_state<NP>(q, h);
+#pragma unroll
+      for (int n = NP; n < RP; n += 4) *reinterpret_cast<f32x4*>(q + n) = f32x4{0, 0, 0, 0};
+    }
   };
   const bool works = c0 < p.Dg;  // a spare wave only helps to stage
   fetch_rows(0);
@@ -331,12 +337,14 @@ int64_t scan_states_bytes(int64_t B, int64_t T, int64_t D, int64_t N) {
   return B * ceil_div(T, kScanChunk) * D * 16 * scan_state_blocks(N) * 4;
 }
 namespace {
+int lane_states(int64_t N) { return N <= 8 ? 8 : (N <= 16 ? 16 : (N <= 24 ? 24 : (N <= 32 ? 32 : 64))); }
+
 struct FwdLayout {
   ScanSplit split;
   int64_t seg_d, total;  // the segments' states come first
 };
 FwdLayout layout(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) {
-  const int64_t NP = 16 * scan_state_blocks(N);
+  const int64_t NP = lane_states(N);
   FwdLayout l;
   l.split = split(B, T, D, G);
   l.seg_d = l.split.S > 1 ? align256(B * l.split.S * D * NP * 4) : 0;
@@ -344,25 +352,34 @@ FwdLayout layout(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) {
   return l;
 }
 
-template <typename T, int NB>
+template <typename T, int NP>
 hipError_t run_fwd(const ScanDev& p, hipStream_t st) {
-  constexpr int NP = 16 * NB;
   const int64_t per = int64_t(p.cblocks) * p.B, join = p.B * p.D * NP;
   if (p.S > 1) {
-    k_scan_fwd<T, NB, false, false><<<dim3(unsigned(per * (p.S - 1))), 64 * kWaves, 0, st>>>(p);
+    k_scan_fwd<T, NP, false, false><<<dim3(unsigned(per * (p.S - 1))), 64 * kWaves, 0, st>>>(p);
     k_scan_join<<<dim3(unsigned(ceil_div(join, 256))), 256, 0, st>>>(p, NP, join);
   }
   const dim3 grid(unsigned(per * p.S));
-  if (p.z.p) k_scan_fwd<T, NB, true, true><<<grid, 64 * kWaves, 0, st>>>(p);
-  else k_scan_fwd<T, NB, true, false><<<grid, 64 * kWaves, 0, st>>>(p);
+  if (p.z.p) k_scan_fwd<T, NP, true, true><<<grid, 64 * kWaves, 0, st>>>(p);
+  else k_scan_fwd<T, NP, true, false><<<grid, 64 * kWaves, 0, st>>>(p);
   return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_fwd(const ScanDev& p, hipStream_t st) {
+  switch (lane_states(p.N)) {
+    case 8: return run_fwd<T, 8>(p, st);
+    case 16: return run_fwd<T, 16>(p, st);
+    case 24: return run_fwd<T, 24>(p, st);
+    case 32: return run_fwd<T, 32>(p, st);
+    default: return run_fwd<T, 64>(p, st);
+  }
 }
 }  // namespace
 
 int64_t scan_fwd_workspace(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) { return layout(B, T, D, N, G).total; }
 
 hipError_t launch_scan_fwd(const ScanArgs& a, hipStream_t st) {
-  const int nb = scan_state_blocks(a.N);
   const FwdLayout l = layout(a.B, a.T, a.D, a.N, a.G);
   ScanDev p = {};
   p.x = a.x, p.dt = a.dt, p.z = a.z, p.Bm = a.Bm, p.Cm = a.Cm;
@@ -375,8 +392,7 @@ hipError_t launch_scan_fwd(const ScanArgs& a, hipStream_t st) {
   p.softplus = a.softplus;
   char* ws = static_cast<char*>(a.workspace);
   p.seg_h = reinterpret_cast<float*>(ws), p.seg_d = reinterpret_cast<float*>(ws + l.seg_d);
-  if (a.dtype == 1) return nb == 1 ? run_fwd<__bf16, 1>(p, st) : (nb == 2 ? run_fwd<__bf16, 2>(p, st) : run_fwd<__bf16, 4>(p, st));
-  return nb == 1 ? run_fwd<float, 1>(p, st) : (nb == 2 ? run_fwd<float, 2>(p, st) : run_fwd<float, 4>(p, st));
+  return a.dtype == 1 ? run_fwd<__bf16>(p, st) : run_fwd<float>(p, st);
 }
 
 hipError_t launch_scan_step(const ScanArgs& a, hipStream_t st) {

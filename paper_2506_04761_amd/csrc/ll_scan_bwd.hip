@@ -307,21 +307,27 @@ __global__ __launch_bounds__(256, 2) void k_scan_bwd(BwdDev p) {
     const bool in = ts < end - t0;
     const V8 xk = xr, dk = dr, zk = zr, gk = gr;
     wave_sync();
+    float delta[8];
+    const bool all = own == 8 && in;
 #pragma unroll
     for (int i = 0; i < 8; i += 2) {
-      float d[2], u[2], e[2];
+      float u[2], e[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const bool ok = in && i + j < own;
-        d[j] = to_f32(T(dk[i + j])) + s_par[wave][0][cs + i + j];
-        if (p.softplus) d[j] = softplusf(d[j]);
+        float d = to_f32(T(dk[i + j])) + s_par[wave][0][cs + i + j];
+        if (p.softplus) d = softplusf(d);
         e[j] = to_f32(T(gk[i + j]));
         if (GATED) e[j] *= silu(to_f32(T(zk[i + j])));
-        u[j] = ok ? d[j] * to_f32(T(xk[i + j])) : 0.0f;
-        d[j] = ok ? d[j] : 0.0f;
-        e[j] = ok ? e[j] : 0.0f;
+        u[j] = d * to_f32(T(xk[i + j]));
+        delta[i + j] = d;
+        if (!all) {
+          const bool ok = in && i + j < own;
+          u[j] = ok ? u[j] : 0.0f;
+          delta[i + j] = ok ? d : 0.0f;
+          e[j] = ok ? e[j] : 0.0f;
+        }
       }
-      *reinterpret_cast<float4*>(&s_du[wave][ts][cs + i]) = make_float4(d[0], u[0], d[1], u[1]);
+      *reinterpret_cast<float4*>(&s_du[wave][ts][cs + i]) = make_float4(delta[i], u[0], delta[i + 1], u[1]);
       *reinterpret_cast<float2*>(&s_dy[wave][ts][cs + i]) = make_float2(e[0], e[1]);
     }
     wave_sync();
@@ -456,10 +462,9 @@ __global__ __launch_bounds__(256, 2) void k_scan_bwd(BwdDev p) {
         const float x = to_f32(T(xk[i])), v = to_f32(T(dk[i])) + s_par[wave][0][cs + i], skip = s_par[wave][1][cs + i];
         const float dout = to_f32(T(gk[i])), z = GATED ? to_f32(T(zk[i])) : 0.0f, sg = GATED ? sigmoidf(z) : 1.0f;
         const float dy = GATED ? dout * (z * sg) : dout;
-        ox[i] = in ? fmaf(p.softplus ? softplusf(v) : v, s.x, skip * dy) : 0.0f;
-        float dd = fmaf(x, s.x, kLn2 * s.y);
-        if (p.softplus) dd *= sigmoidf(v);
-        od[i] = in ? dd : 0.0f;
+        const float grad = p.softplus ? sigmoidf(v) : 1.0f;
+        ox[i] = in ? fmaf(delta[i], s.x, skip * dy) : 0.0f;
+        od[i] = in ? fmaf(x, s.x, kLn2 * s.y) * grad : 0.0f;
         if (GATED) oz[i] = in ? dout * fmaf(skip, x, sy) * silu_grad(z, sg) : 0.0f;
         sums[i] = in ? dy * x : 0.0f;
         sums[8 + i] = od[i];

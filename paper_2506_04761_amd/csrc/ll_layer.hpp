@@ -57,6 +57,18 @@ constexpr int kScanMaxN = 64;
 struct ScanSplit {
   int64_t S = 1, len = 0;
 };
+// The segments' records of one split scan, joined in place (see k_scan_join); `reverse`: from the last segment on.
+struct ScanJoin {
+  const float *A, *init;  // init [B, D, N], may be null: zeros
+  float* h;               // [B, S, D, NP]
+  const float* d;         // [B, S, D] sums of step sizes
+  int64_t B;
+  int S;
+  int64_t D;
+  int N, NP;
+  bool reverse;
+};
+hipError_t launch_scan_join(const ScanJoin& p, hipStream_t st);
 int scan_state_blocks(int64_t N);            // blocks of 16 states a lane group holds: 1, 2 or 4
 constexpr int kScanChunk = 16;               // tokens between two saved states
 int64_t scan_states_bytes(int64_t B, int64_t T, int64_t D, int64_t N);

@@ -23,12 +23,11 @@ namespace ll {
 
 namespace {
 
-constexpr int kWaves = 4;            // waves of a workgroup: neighbouring channels of the same tokens
-constexpr int kBlock = 64 * kWaves;  // channels
+constexpr int kWaves = 4;            // waves of a workgroup at most: neighbouring channels of the same tokens
 constexpr int kStep = 4;             // tokens that are loaded together
 
 constexpr int kQ = 4;                // states whose B and C are read from LDS together
-constexpr int kRows = 32;            // tokens whose B and C are staged together
+constexpr int kRows = 8;             // tokens, times the waves, whose B and C are staged together
 
 struct ScanDev {
   Rows x, dt, z, Bm, Cm;
@@ -38,6 +37,7 @@ struct ScanDev {
   void* y;
   int64_t T, D, chunks;
   int N, G, Dg, blocks, cblocks;  // states; groups; channels of a group; workgroups of a group and of a sequence
+  int waves;                      // of a workgroup
   int S, B, softplus;
   int64_t len;                    // tokens of a segment
 };
@@ -72,15 +72,16 @@ __device__ inline void save_state(float* q, const float* h) {
 template <typename T, int NP, bool OUT, bool GATED>
 __global__ __launch_bounds__(64 * kWaves, NP <= 16 ? 4 : (NP <= 24 ? 3 : (NP <= 32 ? 2 : 1))) void k_scan_fwd(ScanDev p) {
   constexpr int CH = kScanChunk, RP = (NP + 15) / 16 * 16;  // states of a saved record
-  constexpr int W = OUT ? 2 * NP : NP, STAGE = kRows * W / 256;  // values of a token's row; of a tile and thread
-  __shared__ float s_row[2][kRows][W];
+  constexpr int W = OUT ? 2 * NP : NP, STAGE = kRows * W / 64;  // values of a token's row; of a tile and thread
+  __shared__ float s_row[2][kRows * kWaves][W];
+  const int threads = 64 * p.waves, tile = kRows * p.waves;  // of this launch: tokens staged together
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   int64_t id = blockIdx.x;
   const int cb = int(id % p.cblocks);
   id /= p.cblocks;
   const int segs = OUT ? p.S : p.S - 1;  // nothing follows the last segment
   const int seg = int(id % segs), b = int(id / segs);
-  const int g = cb / p.blocks, c0 = (cb % p.blocks) * kBlock + wave * 64;
+  const int g = cb / p.blocks, c0 = (cb % p.blocks * p.waves + wave) * 64;
   const bool mine = c0 + lane < p.Dg;  // spare lanes repeat the group's last channel and store nothing
   const int c = mine ? lane : p.Dg - 1 - c0;  // may be negative: a spare wave
   const int64_t ch0 = int64_t(g) * p.Dg + c0, ch = ch0 + c;
@@ -108,14 +109,14 @@ __global__ __launch_bounds__(64 * kWaves, NP <= 16 ? 4 : (NP <= 24 ? 3 : (NP <= 
   T* yp = static_cast<T*>(p.y) + (int64_t(b) * p.T + t_begin) * p.D + ch0;
   const int count = __builtin_amdgcn_readfirstlane(end > t_begin ? int(end - t_begin) : 0);  // tokens to run
 
-  // a tile's rows: thread i of the workgroup holds values i, i + 256, ..
+  // a tile's rows: thread i of the workgroup holds values i, i + threads, ..
   T stage[STAGE];
   const T* Bp = static_cast<const T*>(p.Bm.p) + b * p.Bm.sb + t_begin * p.Bm.st + int64_t(g) * p.N;
   const T* Cp = static_cast<const T*>(p.Cm.p) + b * p.Cm.sb + t_begin * p.Cm.st + int64_t(g) * p.N;
   auto fetch_rows = [&](int t0) {
 #pragma unroll
     for (int k = 0; k < STAGE; ++k) {
-      const int e = threadIdx.x + 256 * k, t = t0 + e / W, n = e % NP;
+      const int e = threadIdx.x + threads * k, t = t0 + e / W, n = e % NP;
       const bool is_c = OUT && e % W >= NP;
       const T* q = is_c ? Cp : Bp;
       stage[k] = t < count && n < p.N ? q[int64_t(t) * (is_c ? p.Cm.st : p.Bm.st) + n] : from_f32<T>(0.0f);
@@ -203,14 +204,15 @@ __global__ __launch_bounds__(64 * kWaves, NP <= 16 ? 4 : (NP <= 24 ? 3 : (NP <= 
   const bool works = c0 < p.Dg;  // a spare wave only helps to stage
   fetch_rows(0);
   if (works && count > 0) fetch();
-  for (int t0 = 0; t0 < count; t0 += kRows) {
-    float(*rows)[W] = s_row[t0 / kRows & 1];
+  int buf = 0;
+  for (int t0 = 0; t0 < count; t0 += tile, buf ^= 1) {
+    float(*rows)[W] = s_row[buf];
 #pragma unroll
-    for (int k = 0; k < STAGE; ++k) (&rows[0][0])[threadIdx.x + 256 * k] = to_f32(stage[k]);
+    for (int k = 0; k < STAGE; ++k) (&rows[0][0])[threadIdx.x + threads * k] = to_f32(stage[k]);
     __syncthreads();  // the rows are there; and every wave has left the other buffer, which is written next
-    if (t0 + kRows < count) fetch_rows(t0 + kRows);
+    if (t0 + tile < count) fetch_rows(t0 + tile);
     if (!works) continue;
-    const int n = count - t0 < kRows ? count - t0 : kRows;
+    const int n = count - t0 < tile ? count - t0 : tile;
     for (int t = 0; t < n; t += kStep) {
       save(t_begin + t0 + t);
       run(rows + t, t0 + t);
@@ -234,31 +236,61 @@ __global__ __launch_bounds__(64 * kWaves, NP <= 16 ? 4 : (NP <= 24 ? 3 : (NP <= 
   }
 }
 
-// In place: a segment's own final state becomes the state that it starts from.
-__global__ __launch_bounds__(256) void k_scan_join(ScanDev p, int NP, int64_t total) {
-  constexpr int U = 32;  // segments whose loads are in flight together
-  const int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (id >= total) return;
-  const int64_t per = p.D * NP, b = id / per, e = id - b * per, ch = e / NP;
-  const int n = int(e - ch * NP);
-  const float A2 = n < p.N ? p.A[ch * p.N + n] * kLog2e : 0.0f;
-  float h = p.h0 && n < p.N ? p.h0[(b * p.D + ch) * p.N + n] : 0.0f;
-  float* q = p.seg_h + b * p.S * per + e;
-  const float* d = p.seg_d + b * p.S * p.D + ch;
-  for (int s = 0; s < p.S; s += U) {
-    float v[U], w[U];
+// In place: the records of segments (what each leaves by itself) become what each starts from,
+//   start_0 = init, start_1 = own_0 (the first ran from init), start_(s+1) = exp(A d_s) start_s + own_s.
+// A workgroup takes 64 adjacent (channel, state) chains; its RUNS rows of 64 threads take a run of segments each: first
+// a run's decay and own end, then, from the runs before it, its segments' starts.  Bound by reading and writing the
+// records.  RUNS = 1 reads them once and is for few segments or more workgroups than are resident at a time (131072
+// chains of 63 segments 20 us, RUNS = 16 30; 65536 chains of 63 segments 13.4 and 15.7).  RUNS = 16 has 16 times the
+// loads in flight (2048 chains of 39 segments 5 us, RUNS = 1 9.4; 32768 chains of 255 segments 22).
+template <int RUNS>
+__global__ __launch_bounds__(64 * RUNS) void k_scan_join(ScanJoin p) {
+  constexpr int AHEAD = RUNS == 1 ? 32 : 8;  // segments whose loads are in flight together
+  __shared__ float s_f[RUNS][64], s_v[RUNS][64];
+  const int run = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t per = p.D * p.NP, chains = (per + 63) / 64, b = blockIdx.x / chains, e = blockIdx.x % chains * 64 + lane;
+  const bool on = e < per;
+  const int64_t ch = on ? e / p.NP : 0;
+  const int n = on ? int(e - ch * p.NP) : 0;
+  const float A2 = on && n < p.N ? p.A[ch * p.N + n] * kLog2e : 0.0f;
+  const float init = on && p.init && n < p.N ? p.init[(b * p.D + ch) * p.N + n] : 0.0f;
+  float* q = p.h + b * p.S * per + (on ? e : 0);
+  const float* d = p.d + b * p.S * p.D + ch;
+  const int len = (p.S + RUNS - 1) / RUNS, s0 = run * len, s1 = s0 + len < p.S ? s0 + len : p.S;
+  auto at = [&](int s) { return int64_t(p.reverse ? p.S - 1 - s : s); };
+  float f = 1.0f, v = 0.0f;
+  for (int s = s0; RUNS > 1 && s < s1; s += AHEAD) {
+    float own[AHEAD], step[AHEAD];
 #pragma unroll
-    for (int k = 0; k < U; ++k) {
-      const int sk = s + k < p.S - 1 ? s + k : 0;  // the last segment has no record of its own
-      v[k] = q[sk * per];
-      w[k] = d[sk * p.D];
+    for (int k = 0; k < AHEAD; ++k) {
+      const bool in = s + k < s1 && s + k < p.S - 1;  // nothing follows the last segment: it has no record of its own
+      own[k] = in ? q[at(s + k) * per] : 0.0f;
+      step[k] = in ? d[at(s + k) * p.D] : 0.0f;
     }
 #pragma unroll
-    for (int k = 0; k < U; ++k)
-      if (s + k < p.S) {
-        q[(s + k) * per] = h;
-        h = s + k == 0 ? v[0] : fmaf(fast_exp2(A2 * w[k]), h, v[k]);  // the first ran from the initial state
-      }
+    for (int k = 0; k < AHEAD; ++k) {
+      const float a = s + k == 0 ? 0.0f : fast_exp2(A2 * step[k]);
+      v = s + k == 0 ? own[k] : fmaf(a, v, own[k]);
+      f *= a;
+    }
+  }
+  s_f[run][lane] = f, s_v[run][lane] = v;
+  __syncthreads();
+  float h = init;
+  for (int i = 0; i < run; ++i) h = i == 0 && s_f[0][lane] == 0.0f ? s_v[0][lane] : fmaf(s_f[i][lane], h, s_v[i][lane]);
+  for (int s = s0; s < s1; s += AHEAD) {
+    float own[AHEAD], step[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const bool in = s + k < s1 && s + k < p.S - 1;
+      own[k] = in ? q[at(s + k) * per] : 0.0f;
+      step[k] = in ? d[at(s + k) * p.D] : 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      if (on && s + k < s1) q[at(s + k) * per] = h;
+      h = s + k == 0 ? own[k] : fmaf(fast_exp2(A2 * step[k]), h, own[k]);
+    }
   }
 }
 
@@ -321,7 +353,7 @@ ScanSplit split(int64_t B, int64_t T, int64_t D, int64_t G) {
   ScanSplit s;
   int64_t want = waves >= 4096 ? 1 : ceil_div(4096, waves);
   if (want > 1 && T / want >= 256) want = ceil_div(8192, waves);
-  const int64_t most = ceil_div(T, 8);
+  const int64_t most = ceil_div(T, T > 4096 ? 16 : 8);
   if (want > most) want = most;
   s.len = ceil_div(ceil_div(T, want), kStep) * kStep;
   s.S = ceil_div(T, s.len);
@@ -331,6 +363,13 @@ ScanSplit split(int64_t B, int64_t T, int64_t D, int64_t G) {
 int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
 
 }  // namespace
+
+hipError_t launch_scan_join(const ScanJoin& p, hipStream_t st) {
+  const int64_t wgs = p.B * ceil_div(p.D * p.NP, 64);
+  if (p.S > 16 && wgs <= 512) k_scan_join<16><<<dim3(unsigned(wgs)), 1024, 0, st>>>(p);
+  else k_scan_join<1><<<dim3(unsigned(wgs)), 64, 0, st>>>(p);
+  return hipGetLastError();
+}
 
 int scan_state_blocks(int64_t N) { return N <= 16 ? 1 : (N <= 32 ? 2 : 4); }
 int64_t scan_states_bytes(int64_t B, int64_t T, int64_t D, int64_t N) {
@@ -354,14 +393,15 @@ FwdLayout layout(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) {
 
 template <typename T, int NP>
 hipError_t run_fwd(const ScanDev& p, hipStream_t st) {
-  const int64_t per = int64_t(p.cblocks) * p.B, join = p.B * p.D * NP;
+  const int64_t per = int64_t(p.cblocks) * p.B;
   if (p.S > 1) {
-    k_scan_fwd<T, NP, false, false><<<dim3(unsigned(per * (p.S - 1))), 64 * kWaves, 0, st>>>(p);
-    k_scan_join<<<dim3(unsigned(ceil_div(join, 256))), 256, 0, st>>>(p, NP, join);
+    k_scan_fwd<T, NP, false, false><<<dim3(unsigned(per * (p.S - 1))), 64 * p.waves, 0, st>>>(p);
+    const hipError_t e = launch_scan_join({p.A, p.h0, p.seg_h, p.seg_d, p.B, p.S, p.D, p.N, NP, false}, st);
+    if (e != hipSuccess) return e;
   }
   const dim3 grid(unsigned(per * p.S));
-  if (p.z.p) k_scan_fwd<T, NP, true, true><<<grid, 64 * kWaves, 0, st>>>(p);
-  else k_scan_fwd<T, NP, true, false><<<grid, 64 * kWaves, 0, st>>>(p);
+  if (p.z.p) k_scan_fwd<T, NP, true, true><<<grid, 64 * p.waves, 0, st>>>(p);
+  else k_scan_fwd<T, NP, true, false><<<grid, 64 * p.waves, 0, st>>>(p);
   return hipGetLastError();
 }
 
@@ -387,7 +427,8 @@ hipError_t launch_scan_fwd(const ScanArgs& a, hipStream_t st) {
   p.h_final = a.h_final, p.states = a.states, p.y = a.y;
   p.T = a.T, p.D = a.D, p.chunks = ceil_div(a.T, kScanChunk);
   p.N = int(a.N), p.G = int(a.G), p.Dg = int(a.D / a.G);
-  p.blocks = int(ceil_div(p.Dg, kBlock)), p.cblocks = int(p.blocks * a.G);
+  const int64_t waves = ceil_div(p.Dg, 64);  // of a group: as few workgroups as hold them, of equal size
+  p.blocks = int(ceil_div(waves, kWaves)), p.waves = int(ceil_div(waves, p.blocks)), p.cblocks = int(p.blocks * a.G);
   p.S = int(l.split.S), p.B = int(a.B), p.len = l.split.len;
   p.softplus = a.softplus;
   char* ws = static_cast<char*>(a.workspace);

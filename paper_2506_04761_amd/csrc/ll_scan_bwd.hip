@@ -5,7 +5,7 @@
 // where dy is the gradient before the gate: d_y silu(z).
 //
 // The split of the length into segments is the forward's: k_scan_rev runs every segment backwards by itself (carry
-// G = a g, from zero; lanes and staging as in k_scan_fwd), k_scan_join_rev turns these into the carries that segments
+// G = a g, from zero; lanes and staging as in k_scan_fwd), k_scan_join turns these into the carries that segments
 // start from, and k_scan_bwd runs them from there.
 //
 // k_scan_bwd has to add over channels as well as over states, so it spreads both over lanes: lane (r, c) =
@@ -29,10 +29,8 @@ constexpr int kTile = 4;          // tokens whose rates and states are in regist
 constexpr int kWaves = 4;
 constexpr int kCG = 2;            // blocks of 16 channels of a wave
 constexpr int kWaveCh = 16 * kCG;
-constexpr int kBlock = kWaveCh * kWaves;
-constexpr int kRevBlock = 256;    // channels of a workgroup of k_scan_rev
 constexpr int kStep = 4;          // tokens that k_scan_rev loads together
-constexpr int kRows = 32;         // tokens whose C it stages together
+constexpr int kRows = 8;          // tokens, times the waves, whose C it stages together
 constexpr float kLn2 = 0.6931471805599453f;
 
 struct BwdDev {
@@ -43,7 +41,7 @@ struct BwdDev {
   void *dx, *ddt, *dz, *dB, *dC;
   float *seg_g, *seg_d, *part_bc, *part, *dh0;
   int64_t T, D, chunks, T4, len, flen;  // T4: groups of four tokens, padded to whole chunks; tokens of a (fine) segment
-  int N, G, Dg, blocks, cblocks, rev_blocks, rev_cblocks, S, F, R, B;  // segments, fine segments, R fine ones to a segment
+  int N, G, Dg, blocks, cblocks, waves, rev_blocks, rev_cblocks, rev_waves, S, F, R, B;  // segments, fine segments, R fine ones to a segment
   int softplus, vec;
 };
 
@@ -60,14 +58,15 @@ __device__ inline int64_t live_tokens(const int32_t* lengths, int64_t b, int64_t
 // A fine segment backwards by itself.
 template <typename T, int NB, bool GATED>
 __global__ __launch_bounds__(256, NB == 1 ? 4 : (NB == 2 ? 2 : 1)) void k_scan_rev(BwdDev p) {
-  constexpr int NP = 16 * NB, STAGE = kRows * NP / 256;
-  __shared__ float s_row[2][kRows][NP];
+  constexpr int NP = 16 * NB, STAGE = kRows * NP / 64;
+  __shared__ float s_row[2][kRows * kWaves][NP];
+  const int threads = 64 * p.rev_waves, tile = kRows * p.rev_waves;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   int64_t id = blockIdx.x;
   const int cb = int(id % p.rev_cblocks);
   id /= p.rev_cblocks;
   const int seg = 1 + int(id % (p.F - 1)), b = int(id / (p.F - 1));  // nothing comes before segment 0
-  const int g = cb / p.rev_blocks, c0 = (cb % p.rev_blocks) * kRevBlock + wave * 64;
+  const int g = cb / p.rev_blocks, c0 = (cb % p.rev_blocks * p.rev_waves + wave) * 64;
   const bool mine = c0 + lane < p.Dg;         // spare lanes repeat the group's last channel and store nothing
   const int c = mine ? lane : p.Dg - 1 - c0;  // may be negative: a spare wave, which only helps to stage
   const int64_t ch0 = int64_t(g) * p.Dg + c0, ch = ch0 + c;
@@ -90,7 +89,7 @@ __global__ __launch_bounds__(256, NB == 1 ? 4 : (NB == 2 ? 2 : 1)) void k_scan_r
   auto fetch_rows = [&](int i0) {
 #pragma unroll
     for (int k = 0; k < STAGE; ++k) {
-      const int e = threadIdx.x + 256 * k, i = i0 + e / NP, n = e % NP;
+      const int e = threadIdx.x + threads * k, i = i0 + e / NP, n = e % NP;
       stage[k] = i < count && n < p.N ? (Cp - int64_t(i) * p.Cm.st)[n] : from_f32<T>(0.0f);
     }
   };
@@ -142,14 +141,15 @@ __global__ __launch_bounds__(256, NB == 1 ? 4 : (NB == 2 ? 2 : 1)) void k_scan_r
   const bool works = c0 < p.Dg;
   fetch_rows(0);
   if (works && count > 0) fetch();
-  for (int i0 = 0; i0 < count; i0 += kRows) {
-    float(*rows)[NP] = s_row[i0 / kRows & 1];
+  int buf = 0;
+  for (int i0 = 0; i0 < count; i0 += tile, buf ^= 1) {
+    float(*rows)[NP] = s_row[buf];
 #pragma unroll
-    for (int k = 0; k < STAGE; ++k) (&rows[0][0])[threadIdx.x + 256 * k] = to_f32(stage[k]);
+    for (int k = 0; k < STAGE; ++k) (&rows[0][0])[threadIdx.x + threads * k] = to_f32(stage[k]);
     __syncthreads();
-    if (i0 + kRows < count) fetch_rows(i0 + kRows);
+    if (i0 + tile < count) fetch_rows(i0 + tile);
     if (!works) continue;
-    const int n = count - i0 < kRows ? count - i0 : kRows;
+    const int n = count - i0 < tile ? count - i0 : tile;
     for (int i = 0; i < n; i += kStep) run(rows + i, i0 + i);
   }
   if (mine) {
@@ -157,34 +157,6 @@ __global__ __launch_bounds__(256, NB == 1 ? 4 : (NB == 2 ? 2 : 1)) void k_scan_r
 #pragma unroll
     for (int n = 0; n < NP; n += 4) *reinterpret_cast<f32x4*>(q + n) = f32x4{G[n], G[n + 1], G[n + 2], G[n + 3]};
     p.seg_d[(int64_t(b) * p.F + seg) * p.D + ch] = dsum;
-  }
-}
-
-// In place: a segment's own carry becomes the carry that it starts from (at its last token).
-__global__ __launch_bounds__(256) void k_scan_join_rev(BwdDev p, int NP, int64_t total) {
-  constexpr int U = 32;  // segments whose loads are in flight together
-  const int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (id >= total) return;
-  const int64_t per = p.D * NP, b = id / per, e = id - b * per, ch = e / NP;
-  const int n = int(e - ch * NP);
-  const float A2 = n < p.N ? p.A[ch * p.N + n] * kLog2e : 0.0f;
-  float g = p.dh_final && n < p.N ? p.dh_final[(b * p.D + ch) * p.N + n] : 0.0f;
-  float* q = p.seg_g + b * p.F * per + e;
-  const float* d = p.seg_d + b * p.F * p.D + ch;
-  for (int s = p.F - 1; s >= 0; s -= U) {
-    float v[U], w[U];
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
-      const int sk = s - k > 0 ? s - k : p.F - 1;  // the first segment has no record of its own
-      v[k] = q[sk * per];
-      w[k] = d[sk * p.D];
-    }
-#pragma unroll
-    for (int k = 0; k < U; ++k)
-      if (s - k >= 0) {
-        q[(s - k) * per] = g;
-        g = s - k == p.F - 1 ? v[0] : fmaf(fast_exp2(A2 * w[k]), g, v[k]);  // the last ran from the final gradient
-      }
   }
 }
 
@@ -209,7 +181,7 @@ __global__ __launch_bounds__(256, 2) void k_scan_bwd(BwdDev p) {
   const int cb = int(id % p.cblocks);
   id /= p.cblocks;
   const int seg = int(id % p.S), b = int(id / p.S);
-  const int grp = cb / p.blocks, c0 = (cb % p.blocks) * kBlock + wave * kWaveCh;
+  const int grp = cb / p.blocks, c0 = (cb % p.blocks * p.waves + wave) * kWaveCh;
   const int nch = p.Dg - c0 < 0 ? 0 : (p.Dg - c0 > kWaveCh ? kWaveCh : p.Dg - c0);  // may be none: the wave adds zeros
   const int64_t ch0 = int64_t(grp) * p.Dg + c0;
 
@@ -260,7 +232,10 @@ __global__ __launch_bounds__(256, 2) void k_scan_bwd(BwdDev p) {
   };
 
   V8 xr = {}, dr = {}, zr = {}, gr = {};
-  T bc[2 * NB];  // the workgroup's B and C of a chunk: value e = threadIdx.x + 256 i of [B or C][token][state]
+  // the workgroup's B and C of a chunk, [B or C][token][state]: thread i holds values i, i + threads, .. (a workgroup of
+  // fewer waves loads the rest when it stages them)
+  T bc[2 * NB];
+  const int threads = 64 * p.waves;
   f32x4 hr[kCG][NB];
 #pragma unroll
   for (int k = 0; k < kCG; ++k)
@@ -268,16 +243,18 @@ __global__ __launch_bounds__(256, 2) void k_scan_bwd(BwdDev p) {
     for (int nb = 0; nb < NB; ++nb) hr[k][nb] = f32x4{0, 0, 0, 0};  // what a wave without channels works on
   // A chunk's inputs and the states before it.  Rows from the end of the sequence on repeat its last and are
   // masked when used.
+  auto row_value = [&](int64_t chunk, int e) {
+    const int64_t t0 = chunk * kChunk;
+    const int t = e / NP % kChunk, n = e % NP;
+    const bool is_c = e >= kChunk * NP;
+    return t < end - t0 && n < p.N ? load_at<T>((is_c ? Cp : Bp) + t0 * (is_c ? p.Cm.st : p.Bm.st), t, is_c ? p.Cm.st : p.Bm.st, n)
+                                   : from_f32<T>(0.0f);
+  };
   auto fetch = [&](int64_t chunk) {
     const int64_t t0 = chunk * kChunk;
     const int left = end - t0 < kChunk ? int(end - t0) : kChunk;
 #pragma unroll
-    for (int i = 0; i < 2 * NB; ++i) {
-      const int e = threadIdx.x + 256 * i, t = e / NP % kChunk, n = e % NP;
-      const bool is_c = i >= NB;
-      bc[i] = t < left && n < p.N ? load_at<T>((is_c ? Cp : Bp) + t0 * (is_c ? p.Cm.st : p.Bm.st), t, is_c ? p.Cm.st : p.Bm.st, n)
-                                  : from_f32<T>(0.0f);
-    }
+    for (int i = 0; i < 2 * NB; ++i) bc[i] = row_value(chunk, threadIdx.x + threads * i);
     if (nch == 0) return;
     const float* hp = p.states + rec(b, chunk, p.chunks, p.D, ch0, NP);
 #pragma unroll
@@ -292,15 +269,17 @@ __global__ __launch_bounds__(256, 2) void k_scan_bwd(BwdDev p) {
     gr = load8(gp + t0 * p.D, row, p.D);
     if (GATED) zr = load8(zp + t0 * p.z.st, row, p.z.st);
   };
-  auto stage_rows = [&](int buf) {
+  auto stage_rows = [&](int64_t chunk, int buf) {
 #pragma unroll
-    for (int i = 0; i < 2 * NB; ++i) (&s_row[buf][0][0][0])[threadIdx.x + 256 * i] = to_f32(bc[i]);
+    for (int i = 0; i < 2 * NB; ++i) (&s_row[buf][0][0][0])[threadIdx.x + threads * i] = to_f32(bc[i]);
+    for (int e = threadIdx.x + 2 * NB * threads; e < 2 * kChunk * NP; e += threads)
+      (&s_row[buf][0][0][0])[e] = to_f32(row_value(chunk, e));
   };
 
   int buf = 0;
   const int64_t last_chunk = (t_end - 1) / kChunk, first_chunk = t_begin / kChunk;
   fetch(last_chunk);
-  stage_rows(0);
+  stage_rows(last_chunk, 0);
   __syncthreads();
   for (int64_t chunk = last_chunk; chunk >= first_chunk; --chunk) {
     const int64_t t0 = chunk * kChunk;
@@ -438,12 +417,12 @@ __global__ __launch_bounds__(256, 2) void k_scan_bwd(BwdDev p) {
         s_bc[buf][wave][tile][lane] = sum_lanes16(db);
         s_bc[buf][wave][TILES + tile][lane] = sum_lanes16(dc);
       }
-      if (nb == NB - 1 && chunk > first_chunk) stage_rows(rb ^ 1);
+      if (nb == NB - 1 && chunk > first_chunk) stage_rows(chunk - 1, rb ^ 1);
       __syncthreads();  // the other buffers are free: all waves have passed this barrier after they were read
-#pragma unroll
-      for (int i = 0; i < 2 * TILES / kWaves; ++i) {
-        const int e = wave * (2 * TILES / kWaves) + i, which = e / TILES, tile = e % TILES;
-        const float v = (s_bc[buf][0][e][lane] + s_bc[buf][1][e][lane]) + (s_bc[buf][2][e][lane] + s_bc[buf][3][e][lane]);
+      for (int e = wave; e < 2 * TILES; e += p.waves) {
+        const int which = e / TILES, tile = e % TILES;
+        float v = s_bc[buf][0][e][lane];
+        for (int w = 1; w < p.waves; ++w) v += s_bc[buf][w][e][lane];
         (p.part_bc + ((((int64_t(which) * p.B + b) * p.cblocks + cb) * p.T4 + t0 / 4 + tile) * NB + nb) * 64)[lane] = v;
       }
       buf ^= 1;
@@ -530,9 +509,11 @@ struct BwdLayout {
 };
 BwdLayout layout(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) {
   BwdLayout l;
-  const int64_t NP = 16 * scan_state_blocks(N), wgs = B * G * ceil_div(D / G, kBlock), most = ceil_div(T, kChunk);
+  const int64_t NP = 16 * scan_state_blocks(N), wgs = B * G * ceil_div(D / G, kWaveCh * kWaves), most = ceil_div(T, kChunk);
   const int64_t rev = B * G * ceil_div(D / G, 64);
-  int64_t want = ceil_div(512, wgs), fine = ceil_div(4096, rev);
+  // workgroups of fewer waves: more of them
+  const int64_t w = ceil_div(D / G, kWaveCh), per = ceil_div(w, ceil_div(w, kWaves));
+  int64_t want = ceil_div(512 * kWaves / per, wgs), fine = ceil_div(4096, rev);
   want = want > most ? most : want;
   fine = fine > most ? most : fine;
   fine = fine < want ? want : fine;
@@ -551,19 +532,20 @@ BwdLayout layout(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) {
 }
 
 template <typename T, int NB, bool GATED>
-void go_main(const BwdDev& p, hipStream_t st) {
+hipError_t go_main(const BwdDev& p, hipStream_t st) {
   if (p.F > 1) {
-    const int64_t join = int64_t(p.B) * p.D * 16 * NB;
-    k_scan_rev<T, NB, GATED><<<dim3(unsigned(int64_t(p.rev_cblocks) * p.B * (p.F - 1))), 256, 0, st>>>(p);
-    k_scan_join_rev<<<dim3(unsigned(ceil_div(join, 256))), 256, 0, st>>>(p, 16 * NB, join);
+    k_scan_rev<T, NB, GATED><<<dim3(unsigned(int64_t(p.rev_cblocks) * p.B * (p.F - 1))), 64 * p.rev_waves, 0, st>>>(p);
+    const hipError_t e = launch_scan_join({p.A, p.dh_final, p.seg_g, p.seg_d, p.B, p.F, p.D, p.N, 16 * NB, true}, st);
+    if (e != hipSuccess) return e;
   }
-  k_scan_bwd<T, NB, GATED><<<dim3(unsigned(int64_t(p.cblocks) * p.B * p.S)), 256, 0, st>>>(p);
+  k_scan_bwd<T, NB, GATED><<<dim3(unsigned(int64_t(p.cblocks) * p.B * p.S)), 64 * p.waves, 0, st>>>(p);
+  return hipGetLastError();
 }
 
 template <typename T, int NB>
 hipError_t go(const BwdDev& p, hipStream_t st) {
-  if (p.z.p) go_main<T, NB, true>(p, st);
-  else go_main<T, NB, false>(p, st);
+  const hipError_t e = p.z.p ? go_main<T, NB, true>(p, st) : go_main<T, NB, false>(p, st);
+  if (e != hipSuccess) return e;
   const int64_t total = 2 * int64_t(p.B) * p.G * p.T4 * NB * 64;
   k_scan_bc<T, NB><<<dim3(unsigned(ceil_div(total, 256))), 256, 0, st>>>(p, total);
   return hipGetLastError();
@@ -589,8 +571,11 @@ hipError_t launch_scan_bwd(const ScanArgs& a, const ScanGrads& g, hipStream_t st
   p.part_bc = reinterpret_cast<float*>(ws + l.bc), p.part = reinterpret_cast<float*>(ws + l.part);
   p.T = a.T, p.D = a.D, p.chunks = ceil_div(a.T, kScanChunk), p.T4 = l.T4, p.len = l.len, p.flen = l.flen;
   p.N = int(a.N), p.G = int(a.G), p.Dg = int(a.D / a.G);
-  p.blocks = int(ceil_div(p.Dg, kBlock)), p.cblocks = int(p.blocks * a.G);
-  p.rev_blocks = int(ceil_div(p.Dg, kRevBlock)), p.rev_cblocks = int(p.rev_blocks * a.G);
+  const int64_t waves = ceil_div(p.Dg, kWaveCh);  // of a group: as few workgroups as hold them, of equal size
+  p.blocks = int(ceil_div(waves, kWaves)), p.waves = int(ceil_div(waves, p.blocks)), p.cblocks = int(p.blocks * a.G);
+  const int64_t rev = ceil_div(p.Dg, 64);
+  p.rev_blocks = int(ceil_div(rev, kWaves)), p.rev_waves = int(ceil_div(rev, p.rev_blocks));
+  p.rev_cblocks = int(p.rev_blocks * a.G);
   p.S = int(l.S), p.F = int(l.F), p.R = int(l.R), p.B = int(a.B), p.softplus = a.softplus;
   const Rows flat[4] = {{g.dy, 0, a.D}, {g.dx, 0, a.D}, {g.ddt, 0, a.D}, {g.dz, 0, a.D}};
   p.vec = p.Dg % 8 == 0 && rows_aligned(a.x, e, 16 / e) && rows_aligned(a.dt, e, 16 / e) && (!a.z.p || rows_aligned(a.z, e, 16 / e));

@@ -160,10 +160,10 @@ __global__ __launch_bounds__(256) void k_conv_step(ConvDev p) {
 // A lane walks its run and the W - 1 tokens after it (whose dv reach back into the run) and keeps the run's
 // sums; the workgroup's four runs are added in LDS, and k_colsum adds the workgroups.
 template <typename T, int W>
-__global__ __launch_bounds__(256) void k_conv_bwd(ConvDev p) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 5) void k_conv_bwd(ConvDev p) {
   constexpr int V = kVecBytes / sizeof(T);
   __shared__ float s_sum[4][64][V + 1];
-  const int lane = threadIdx.x & 63, strip = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, strip = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int64_t id = blockIdx.x;
   const int64_t cblocks = (p.ncv + 63) / 64, groups = (p.runs + 3) / 4;
   const int64_t cv = id % cblocks * 64 + lane;
@@ -192,64 +192,103 @@ __global__ __launch_bounds__(256) void k_conv_bwd(ConvDev p) {
     const T* dyp = static_cast<const T*>(p.dy) + b * p.T * p.D + d0;
     const T* xp = static_cast<const T*>(p.x.p) + b * p.x.sb + d0;
     const T* dfp = p.dfinal ? static_cast<const T*>(p.dfinal) + b * (W - 1) * p.D + d0 : nullptr;
+    T* dxp = static_cast<T*>(p.dx) + b * p.T * p.D + d0;
     typedef typename VecN<T, V>::type Vec;
-    constexpr int U = 2;
+    constexpr int U = 4;
     Vec xr[U], gr[U];
     const int64_t last = t1 + W - 1;  // one past the last dv that the run needs
-    auto fetch = [&](int64_t t) {
+    // Token t's dv (zero where !in), its share of the run's sums (where own), and o = dx of token t - (W - 1).
+    auto step = [&](const Vec& xv, const Vec& gv, bool in, bool own, float* o) {
 #pragma unroll
-      for (int k = 0; k < U; ++k) {
-        const int m = t + k < live && t + k < last ? n : 0;
-        xr[k] = load_n<T, V>(xp + (t + k) * p.x.st, m, p.vec);
-        gr[k] = load_n<T, V>(dyp + (t + k) * p.D, m, p.vec);
+      for (int i = 0; i < V; ++i) {
+#pragma unroll
+        for (int j = 0; j + 1 < W; ++j) e[j][i] = e[j + 1][i], dv[j][i] = dv[j + 1][i];
+        e[W - 1][i] = to_f32(T(xv[i]));
+        float g = to_f32(T(gv[i]));
+        if (p.act) {
+          float v = bias[i];
+#pragma unroll
+          for (int j = 0; j < W; ++j) v = fmaf(w[j][i], e[j][i], v);
+          g *= silu_grad(v, sigmoidf(v));
+        }
+        g = in ? g : 0.0f;
+        dv[W - 1][i] = g;  // dv[j] = dv of token t - (W - 1) + j
+        const float own_g = own ? g : 0.0f;
+        db[i] += own_g;
+        float a = 0.0f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+          dw[j][i] = fmaf(own_g, e[j][i], dw[j][i]);
+          a = fmaf(w[j][i], dv[W - 1 - j][i], a);
+        }
+        o[i] = a;
       }
     };
-    fetch(t0);
-    for (int64_t t = t0; t < last; t += U) {
-      float xf[U][V], gf[U][V];
+    // A run of whole vectors and whole groups of U tokens, with as many live tokens after it as it needs: no load or
+    // store depends on a condition, so that waiting for a load does not wait for what was issued after it.
+    if (p.vec && t1 - t0 == p.run && last + (U - W + 1) <= live && !(run == 0 && p.dinit)) {
+      auto fetch = [&](int64_t t) {
 #pragma unroll
-      for (int k = 0; k < U; ++k)
+        for (int k = 0; k < U; ++k) {
+          xr[k] = *reinterpret_cast<const Vec*>(xp + (t + k) * p.x.st);
+          gr[k] = *reinterpret_cast<const Vec*>(dyp + (t + k) * p.D);
+        }
+      };
+      Vec xk[U], gk[U];
+      auto next = [&] {
 #pragma unroll
-        for (int i = 0; i < V; ++i) xf[k][i] = to_f32(T(xr[k][i])), gf[k][i] = to_f32(T(gr[k][i]));
-      if (t + U < last) fetch(t + U);
+        for (int k = 0; k < U; ++k) xk[k] = xr[k], gk[k] = gr[k];
+      };
+      auto put = [&](int64_t s, const float* o) { store_n<T, V>(dxp + s * p.D, o, V, true); };
+      float o[V];
+      fetch(t0);
+      next();
+      fetch(t0 + U);
 #pragma unroll
       for (int k = 0; k < U; ++k) {
-        const int64_t tk = t + k, s = tk - (W - 1);
-        const bool in = tk < live && tk < last, own = tk < t1;
-        float o[V];
+        step(xk[k], gk[k], true, true, o);
+        if (k >= W - 1) put(t0 + k - (W - 1), o);
+      }
+      for (int64_t t = t0 + U; t < t1; t += U) {
+        next();
+        fetch(t + U);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-#pragma unroll
-          for (int j = 0; j + 1 < W; ++j) e[j][i] = e[j + 1][i], dv[j][i] = dv[j + 1][i];
-          e[W - 1][i] = xf[k][i];
-          float g = gf[k][i];
-          if (p.act) {
-            float v = bias[i];
-#pragma unroll
-            for (int j = 0; j < W; ++j) v = fmaf(w[j][i], e[j][i], v);
-            g *= silu_grad(v, sigmoidf(v));
-          }
-          g = in ? g : 0.0f;
-          dv[W - 1][i] = g;  // dv[j] = dv of token s + j
-          const float own_g = own ? g : 0.0f;
-          db[i] += own_g;
-          float a = 0.0f;
-#pragma unroll
-          for (int j = 0; j < W; ++j) {
-            dw[j][i] = fmaf(own_g, e[j][i], dw[j][i]);
-            a = fmaf(w[j][i], dv[W - 1 - j][i], a);
-          }
-          o[i] = a;
+        for (int k = 0; k < U; ++k) {
+          step(xk[k], gk[k], true, true, o);
+          put(t + k - (W - 1), o);
         }
-        if (dfp && s < live && s >= live - (W - 1)) {
-          const Vec f = load_n<T, V>(dfp + (s - live + W - 1) * p.D, n, p.vec);
+      }
 #pragma unroll
-          for (int i = 0; i < V; ++i) o[i] += to_f32(T(f[i]));
+      for (int k = 0; k < W - 1; ++k) {
+        step(xr[k], gr[k], true, false, o);
+        put(t1 + k - (W - 1), o);
+      }
+    } else {
+      auto fetch = [&](int64_t t) {
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+          const int m = t + k < live && t + k < last ? n : 0;
+          xr[k] = load_n<T, V>(xp + (t + k) * p.x.st, m, p.vec);
+          gr[k] = load_n<T, V>(dyp + (t + k) * p.D, m, p.vec);
         }
-        if (s >= t0 && s < t1) {
-          store_n<T, V>(static_cast<T*>(p.dx) + (b * p.T + s) * p.D + d0, o, n, p.vec);
-        } else if (s < 0 && run == 0 && p.dinit) {
-          store_n<T, V>(static_cast<T*>(p.dinit) + (b * (W - 1) + s + W - 1) * p.D + d0, o, n, p.vec);
+      };
+      for (int64_t t = t0; t < last; t += U) {
+        fetch(t);
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+          const int64_t tk = t + k, s = tk - (W - 1);
+          float o[V];
+          step(xr[k], gr[k], tk < live && tk < last, tk < t1, o);
+          if (dfp && s < live && s >= live - (W - 1)) {
+            const Vec f = load_n<T, V>(dfp + (s - live + W - 1) * p.D, n, p.vec);
+#pragma unroll
+            for (int i = 0; i < V; ++i) o[i] += to_f32(T(f[i]));
+          }
+          if (s >= t0 && s < t1) {
+            store_n<T, V>(dxp + s * p.D, o, n, p.vec);
+          } else if (s < 0 && run == 0 && p.dinit) {
+            store_n<T, V>(static_cast<T*>(p.dinit) + (b * (W - 1) + s + W - 1) * p.D + d0, o, n, p.vec);
+          }
         }
       }
     }
@@ -302,7 +341,7 @@ int elem(int dtype) { return dtype == 1 ? 2 : 4; }
 int run_length(int64_t B, int64_t T, int64_t ncv, int most) {
   int64_t r = B * T * ncv / (int64_t(1) << 18);
   r = r < 4 ? 4 : (r > most ? most : r);
-  return int(r / 4 * 4);
+  return int((r + 3) / 4 * 4);
 }
 
 bool conv_vec(const ConvArgs& a) {

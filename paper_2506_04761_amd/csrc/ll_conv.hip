@@ -194,6 +194,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 5) void k_conv_bwd(ConvDe
     const T* dfp = p.dfinal ? static_cast<const T*>(p.dfinal) + b * (W - 1) * p.D + d0 : nullptr;
     T* dxp = static_cast<T*>(p.dx) + b * p.T * p.D + d0;
     typedef typename VecN<T, V>::type Vec;
+    typedef typename VecN<T, V>::loose Loose;
     constexpr int U = 4;
     Vec xr[U], gr[U];
     const int64_t last = t1 + W - 1;  // one past the last dv that the run needs
@@ -226,12 +227,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 5) void k_conv_bwd(ConvDe
     };
     // A run of whole vectors and whole groups of U tokens, with as many live tokens after it as it needs: no load or
     // store depends on a condition, so that waiting for a load does not wait for what was issued after it.
-    if (p.vec && t1 - t0 == p.run && last + (U - W + 1) <= live && !(run == 0 && p.dinit)) {
+    if (n == V && t1 - t0 == p.run && last + (U - W + 1) <= live && !(run == 0 && p.dinit)) {
       auto fetch = [&](int64_t t) {
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-          xr[k] = *reinterpret_cast<const Vec*>(xp + (t + k) * p.x.st);
-          gr[k] = *reinterpret_cast<const Vec*>(dyp + (t + k) * p.D);
+          xr[k] = *reinterpret_cast<const Loose*>(xp + (t + k) * p.x.st);
+          gr[k] = *reinterpret_cast<const Loose*>(dyp + (t + k) * p.D);
         }
       };
       Vec xk[U], gk[U];
@@ -239,7 +240,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 5) void k_conv_bwd(ConvDe
 #pragma unroll
         for (int k = 0; k < U; ++k) xk[k] = xr[k], gk[k] = gr[k];
       };
-      auto put = [&](int64_t s, const float* o) { store_n<T, V>(dxp + s * p.D, o, V, true); };
+      auto put = [&](int64_t s, const float* o) { store_n<T, V>(dxp + s * p.D, o, V, false); };
       float o[V];
       fetch(t0);
       next();

@@ -11,15 +11,18 @@ namespace ll {
 template <typename T, int N>
 struct VecN {
   typedef T type __attribute__((ext_vector_type(N)));
+  typedef type loose __attribute__((aligned(sizeof(T))));  // at any element
 };
 
 // N adjacent elements at p, of which the first n are inputs (the others read as zero, and are not
-// touched): one load where `vec` says that rows are aligned for it (then n is 0 or N).
+// touched): `vec` says that rows are aligned for whole vectors (then n is 0 or N).
 template <typename T, int N>
 __device__ inline typename VecN<T, N>::type load_n(const T* p, int n, bool vec) {
   typename VecN<T, N>::type v = {};
   if (vec) {
     if (n > 0) v = *reinterpret_cast<const typename VecN<T, N>::type*>(p);
+  } else if (n == N) {
+    v = *reinterpret_cast<const typename VecN<T, N>::loose*>(p);
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i)
@@ -30,17 +33,17 @@ __device__ inline typename VecN<T, N>::type load_n(const T* p, int n, bool vec) 
 
 template <typename T, int N>
 __device__ inline void store_n(T* p, const float* f, int n, bool vec) {
-  if (vec) {
-    if (n > 0) {
-      typename VecN<T, N>::type v;
+  typename VecN<T, N>::type v;
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = from_f32<T>(f[i]);
-      *reinterpret_cast<typename VecN<T, N>::type*>(p) = v;
-    }
+  for (int i = 0; i < N; ++i) v[i] = from_f32<T>(f[i]);
+  if (vec) {
+    if (n > 0) *reinterpret_cast<typename VecN<T, N>::type*>(p) = v;
+  } else if (n == N) {
+    *reinterpret_cast<typename VecN<T, N>::loose*>(p) = v;
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (i < n) p[i] = from_f32<T>(f[i]);
+      if (i < n) p[i] = v[i];
   }
 }
 

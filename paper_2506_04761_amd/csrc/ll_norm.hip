@@ -25,7 +25,8 @@ struct NormDev {
   float* part;         // backward: [rows, 2, C] partial sums of du xh and du; slab forward: [N, chunks, ncv, 2]
   float* coef;         // slab backward: [N, G, 2]
   int64_t N, S, C, per, chunks, ncv;  // per: rows form, workgroups over the rows; slab, tokens of a chunk
-  int G, cg, act, vec, pvec;  // pvec: weight and bias are 16-byte aligned
+  int G, cg, act, vec, pvec;  // pvec: a lane's weights and biases are 16-byte aligned
+  int nvg;              // slab: channel vectors of a group (the last may be short)
   int slots, bpr, rpw;  // rows form: lanes of a row, workgroups of a row, rows of a workgroup
   float eps;
 };
@@ -56,6 +57,28 @@ __device__ inline float group_sum(float v, float* s) {
     v = (s[0] + s[1]) + (s[2] + s[3]);
   }
   return v;
+}
+
+// A lane's V channels of a group: the group's last vector, where it would be short, is moved back over the one before
+// (both lanes then store the same outputs), so that all loads and stores are whole vectors; what it takes part with in
+// sums is channels lo .. n - 1 of the vector.  Groups of less than a vector: channels 0 .. n - 1.
+struct Place {
+  int c = 0, lo = 0, n = 0;  // c: the first channel, within the group; n = 0: none
+  __device__ Place() {}
+  __device__ Place(int at, int cg, int V) {
+    if (at >= cg) return;
+    c = at, n = cg - at < V ? cg - at : V;
+    if (n < V && cg >= V) c = cg - V, lo = V - n, n = V;
+  }
+  __device__ bool has(int i) const { return i >= lo && i < n; }
+};
+
+// out[i] = v[i] for the channels that count.
+template <int V>
+__device__ inline void store_sums(float* out, const Place& at, const float* v) {
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (at.has(i)) out[i] = v[i];
 }
 
 // What a thread of the rows form works on: vectors lane, lane + LG, .. of one group, in rows first, first + step, ..
@@ -91,11 +114,12 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormDev p) {
   if (LG <= 64 && !q.on) return;
   float w[PV][V], bi[PV][V];
   int off[PV], n[PV];
+  Place at[PV];
 #pragma unroll
   for (int k = 0; k < PV; ++k) {
-    const int c = (q.lane + k * LG) * V;  // within the group
-    n[k] = c < p.cg ? (p.cg - c < V ? p.cg - c : V) : 0;
-    off[k] = q.g * p.cg + (n[k] ? c : 0);
+    at[k] = Place((q.lane + k * LG) * V, p.cg, V);
+    n[k] = at[k].n;
+    off[k] = q.g * p.cg + at[k].c;
     load_params<V>(p.weight ? p.weight + off[k] : nullptr, n[k], 1.0f, p.pvec, w[k]);
     load_params<V>(p.bias ? p.bias + off[k] : nullptr, n[k], 0.0f, p.pvec, bi[k]);
   }
@@ -119,7 +143,7 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormDev p) {
       for (int i = 0; i < V; ++i) {
         x[k][i] = to_f32(T(xr[k][i]));
         if (gated) z[k][i] = to_f32(T(zr[k][i]));
-        sum += x[k][i];
+        sum += at[k].has(i) ? x[k][i] : 0.0f;
       }
     fetch(r + q.step);
     const float mean = group_sum<LG>(sum, s) * inv;
@@ -129,7 +153,7 @@ __global__ __launch_bounds__(256) void k_norm_rows(NormDev p) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         x[k][i] -= mean;
-        sq += i < n[k] ? x[k][i] * x[k][i] : 0.0f;
+        sq += at[k].has(i) ? x[k][i] * x[k][i] : 0.0f;
       }
     const float rstd = 1.0f / sqrtf(fmaf(group_sum<LG>(sq, s), inv, p.eps));
     if (p.stats && q.lane == 0) {
@@ -168,6 +192,13 @@ __device__ inline void norm_du(const NormDev& p, bool gated, float mean, float r
   }
 }
 
+// The product that both a group's mean and its elements' differences from that mean are formed of: rounded by itself
+// in both, so that a group of one element has no gradient.
+__device__ inline float rounded_mul(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
+
 // Strips of a backward workgroup: four of one vector a lane, fewer of more (registers).
 template <int PV>
 constexpr int kBwdStrips = 4 / PV;
@@ -181,11 +212,12 @@ __global__ __launch_bounds__(256 * kBwdStrips<PV>) void k_norm_rows_bwd(NormDev 
   const RowPlan q(p, LG, STRIPS);
   float w[PV][V], bi[PV][V], dw[PV][V], db[PV][V];
   int off[PV], n[PV];
+  Place at[PV];
 #pragma unroll
   for (int k = 0; k < PV; ++k) {
-    const int c = (q.lane + k * LG) * V;
-    n[k] = q.on && c < p.cg ? (p.cg - c < V ? p.cg - c : V) : 0;
-    off[k] = q.g * p.cg + (n[k] ? c : 0);
+    if (q.on) at[k] = Place((q.lane + k * LG) * V, p.cg, V);
+    n[k] = at[k].n;
+    off[k] = q.g * p.cg + at[k].c;
     load_params<V>(p.weight ? p.weight + off[k] : nullptr, n[k], 1.0f, p.pvec, w[k]);
     load_params<V>(p.bias ? p.bias + off[k] : nullptr, n[k], 0.0f, p.pvec, bi[k]);
 #pragma unroll
@@ -227,12 +259,15 @@ __global__ __launch_bounds__(256 * kBwdStrips<PV>) void k_norm_rows_bwd(NormDev 
       if (gated) store_n<T, V>(static_cast<T*>(p.dz) + r * p.C + off[k], dz, row ? n[k] : 0, p.vec);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        if (i >= n[k] || !row) du[k][i] = 0.0f, x[k][i] = 0.0f;
-        db[k][i] += du[k][i];
-        dw[k][i] = fmaf(du[k][i], x[k][i], dw[k][i]);
-        du[k][i] *= w[k][i];
-        s1 += du[k][i];
-        s2 = fmaf(du[k][i], x[k][i], s2);
+        const bool on = row && at[k].has(i);
+        const float d = on ? du[k][i] : 0.0f;
+        if (!row) x[k][i] = 0.0f;
+        db[k][i] += d;
+        dw[k][i] = fmaf(d, x[k][i], dw[k][i]);
+        du[k][i] = rounded_mul(du[k][i], w[k][i]);
+        const float dg = on ? du[k][i] : 0.0f;
+        s1 += dg;
+        s2 = fmaf(dg, x[k][i], s2);
       }
     }
     s1 = group_sum<LG>(s1, s) * inv;
@@ -248,22 +283,22 @@ __global__ __launch_bounds__(256 * kBwdStrips<PV>) void k_norm_rows_bwd(NormDev 
   if (!p.part) return;
   // one row of partial sums for the workgroup's strips
   float* out = p.part + q.part * 2 * p.C;
-  const int at = threadIdx.x & 255;
+  const int slot = threadIdx.x & 255;
 #pragma unroll
   for (int k = 0; k < 2 * PV; ++k) {
     float(&v)[V] = k < PV ? dw[k % PV] : db[k % PV];
     __syncthreads();
     if (q.strip > 0) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) s_sum[q.strip > 0 ? q.strip - 1 : 0][i][at] = v[i];
+      for (int i = 0; i < V; ++i) s_sum[q.strip > 0 ? q.strip - 1 : 0][i][slot] = v[i];
     }
     __syncthreads();
     if (q.strip == 0) {
 #pragma unroll
       for (int j = 0; j < STRIPS - 1; ++j)
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] += s_sum[j][i][at];
-      store_n<float, V>(out + (k < PV ? 0 : p.C) + off[k % PV], v, n[k % PV], false);
+        for (int i = 0; i < V; ++i) v[i] += s_sum[j][i][slot];
+      store_sums<V>(out + (k < PV ? 0 : p.C) + off[k % PV], at[k % PV], v);
     }
   }
 }
@@ -281,9 +316,13 @@ __device__ inline void merge(float& n1, float& m1, float& q1, float n2, float m2
 }
 
 // Threads of the slab kernels: `lanes` channel vectors x 256 / lanes strips of tokens.
+template <int V>
 struct SlabPlan {
   int lanes, strip, strips;
   int64_t cv, n, t0, t1, chunk;
+  int g, width;  // the vector's group; its channels
+  Place at;
+  int64_t d0;    // its first channel
   __device__ SlabPlan(const NormDev& p) {
     lanes = p.ncv < 256 ? int(p.ncv) : 256;
     strips = 256 / lanes;
@@ -296,6 +335,10 @@ struct SlabPlan {
     n = id / p.chunks;
     t0 = chunk * p.per;
     t1 = t0 + p.per < p.S ? t0 + p.per : p.S;
+    g = int(cv / p.nvg);
+    at = Place(int(cv - int64_t(g) * p.nvg) * V, p.cg, V);
+    width = at.n;
+    d0 = int64_t(g) * p.cg + at.c;
   }
   __device__ bool on(const NormDev& p) const { return strip < strips && cv < p.ncv; }
 };
@@ -304,28 +347,28 @@ template <typename T, int V>
 __global__ __launch_bounds__(256) void k_norm_slab_stats(NormDev p) {
   constexpr int U = 8;
   __shared__ float s[256][3];
-  const SlabPlan q(p);
+  const SlabPlan<V> q(p);
   float cnt = 0.0f, mean = 0.0f, sq = 0.0f;
   if (q.on(p)) {
-    const T* xp = static_cast<const T*>(p.x.p) + q.n * p.x.sb + q.cv * V;
+    const T* xp = static_cast<const T*>(p.x.p) + q.n * p.x.sb + q.d0;
     for (int64_t t = q.t0 + q.strip; t < q.t1; t += U * q.strips) {
       typename VecN<T, V>::type v[U];
 #pragma unroll
-      for (int k = 0; k < U; ++k) v[k] = load_n<T, V>(xp + (t + k * q.strips) * p.x.st, t + k * q.strips < q.t1 ? V : 0, p.vec);
+      for (int k = 0; k < U; ++k) v[k] = load_n<T, V>(xp + (t + k * q.strips) * p.x.st, t + k * q.strips < q.t1 ? q.width : 0, p.vec);
       float a = 0.0f, b = 0.0f, m = 0.0f;
 #pragma unroll
       for (int k = 0; k < U; ++k)
 #pragma unroll
-        for (int i = 0; i < V; ++i) a += to_f32(T(v[k][i]));
+        for (int i = 0; i < V; ++i) a += q.at.has(i) ? to_f32(T(v[k][i])) : 0.0f;
 #pragma unroll
-      for (int k = 0; k < U; ++k) m += t + k * q.strips < q.t1 ? float(V) : 0.0f;
+      for (int k = 0; k < U; ++k) m += t + k * q.strips < q.t1 ? float(q.width - q.at.lo) : 0.0f;
       a /= m;
 #pragma unroll
       for (int k = 0; k < U; ++k)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           const float d = to_f32(T(v[k][i])) - a;
-          b += t + k * q.strips < q.t1 ? d * d : 0.0f;
+          b += t + k * q.strips < q.t1 && q.at.has(i) ? d * d : 0.0f;
         }
       merge(cnt, mean, sq, m, a, b);
     }
@@ -346,13 +389,14 @@ __global__ __launch_bounds__(256) void k_norm_slab_stats(NormDev p) {
 __global__ __launch_bounds__(256) void k_norm_slab_join(NormDev p, int V) {
   __shared__ float s[256][3];
   const int64_t n = blockIdx.x / p.G;
-  const int g = int(blockIdx.x % p.G), nv = p.cg / V;
+  const int g = int(blockIdx.x % p.G), nv = p.nvg;
   float cnt = 0.0f, mean = 0.0f, sq = 0.0f;
   for (int64_t e = threadIdx.x; e < p.chunks * nv; e += 256) {
     const int64_t chunk = e / nv, cv = int64_t(g) * nv + e % nv;
     const float* o = p.part + ((n * p.chunks + chunk) * p.ncv + cv) * 2;
     const int64_t t = p.S - chunk * p.per < p.per ? p.S - chunk * p.per : p.per;
-    merge(cnt, mean, sq, float(t) * V, o[0], o[1]);
+    const int last = p.cg - (nv - 1) * V, width = e % nv == nv - 1 ? last : V;
+    merge(cnt, mean, sq, float(t) * float(width), o[0], o[1]);
   }
   for (int half = 128; half > 0; half >>= 1) {
     s[threadIdx.x][0] = cnt, s[threadIdx.x][1] = mean, s[threadIdx.x][2] = sq;
@@ -370,31 +414,31 @@ __global__ __launch_bounds__(256) void k_norm_slab_join(NormDev p, int V) {
 }
 
 template <int V>
-__device__ inline void slab_params(const NormDev& p, const SlabPlan& q, float* w, float* b) {
-  load_params<V>(p.weight ? p.weight + q.cv * V : nullptr, V, 1.0f, p.pvec, w);
-  load_params<V>(p.bias ? p.bias + q.cv * V : nullptr, V, 0.0f, p.pvec, b);
+__device__ inline void slab_params(const NormDev& p, const SlabPlan<V>& q, float* w, float* b) {
+  load_params<V>(p.weight ? p.weight + q.d0 : nullptr, q.width, 1.0f, p.pvec, w);
+  load_params<V>(p.bias ? p.bias + q.d0 : nullptr, q.width, 0.0f, p.pvec, b);
 }
 
 template <typename T, int V>
 __global__ __launch_bounds__(256) void k_norm_slab_out(NormDev p) {
   constexpr int U = 4;
-  const SlabPlan q(p);
+  const SlabPlan<V> q(p);
   if (!q.on(p)) return;
   float w[V], b[V];
   slab_params<V>(p, q, w, b);
-  const float* st = p.stats + (q.n * p.G + q.cv * V / p.cg) * 2;
+  const float* st = p.stats + (q.n * p.G + q.g) * 2;
   const float mean = st[0], rstd = st[1];
   const bool gated = p.z.p;
-  const T* xp = static_cast<const T*>(p.x.p) + q.n * p.x.sb + q.cv * V;
-  const T* zp = static_cast<const T*>(p.z.p) + q.n * p.z.sb + q.cv * V;
-  T* yp = static_cast<T*>(p.y) + q.n * p.S * p.C + q.cv * V;
+  const T* xp = static_cast<const T*>(p.x.p) + q.n * p.x.sb + q.d0;
+  const T* zp = static_cast<const T*>(p.z.p) + q.n * p.z.sb + q.d0;
+  T* yp = static_cast<T*>(p.y) + q.n * p.S * p.C + q.d0;
   for (int64_t t = q.t0 + q.strip; t < q.t1; t += U * q.strips) {
     typename VecN<T, V>::type x[U], z[U];
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const int64_t tk = t + k * q.strips;
-      x[k] = load_n<T, V>(xp + tk * p.x.st, tk < q.t1 ? V : 0, p.vec);
-      if (gated) z[k] = load_n<T, V>(zp + tk * p.z.st, tk < q.t1 ? V : 0, p.vec);
+      x[k] = load_n<T, V>(xp + tk * p.x.st, tk < q.t1 ? q.width : 0, p.vec);
+      if (gated) z[k] = load_n<T, V>(zp + tk * p.z.st, tk < q.t1 ? q.width : 0, p.vec);
     }
 #pragma unroll
     for (int k = 0; k < U; ++k) {
@@ -405,37 +449,37 @@ __global__ __launch_bounds__(256) void k_norm_slab_out(NormDev p) {
         o[i] = gated ? u * act_of(to_f32(T(z[k][i])), p.act) : act_of(u, p.act);
       }
       const int64_t tk = t + k * q.strips;
-      store_n<T, V>(yp + tk * p.C, o, tk < q.t1 ? V : 0, p.vec);
+      store_n<T, V>(yp + tk * p.C, o, tk < q.t1 ? q.width : 0, p.vec);
     }
   }
 }
 
 // Slab backward, first pass (OUT = false): a chunk's sums of du xh and du for every channel, from which come
 // dw, db and, weighted, the two group sums that dx needs; with a gate, dz.  Second pass (OUT = true): dx.
-template <typename T, int V, bool OUT>
+template <typename T, int V, bool OUT, bool gated>
 __global__ __launch_bounds__(256) void k_norm_slab_bwd(NormDev p) {
   constexpr int U = 2;
   __shared__ float s[OUT ? 1 : 256 * (2 * V + 1)];
-  const SlabPlan q(p);
-  const bool on = q.on(p), gated = p.z.p;
+  const SlabPlan<V> q(p);
+  const bool on = q.on(p);
   float dw[V], db[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) dw[i] = db[i] = 0.0f;
   if (on) {
     float w[V], b[V];
     slab_params<V>(p, q, w, b);
-    const int64_t grp = q.n * p.G + q.cv * V / p.cg;
+    const int64_t grp = q.n * p.G + q.g;
     const float mean = p.stats[grp * 2], rstd = p.stats[grp * 2 + 1];
     const float s1 = OUT ? p.coef[grp * 2] : 0.0f, s2 = OUT ? p.coef[grp * 2 + 1] : 0.0f;
-    const T* xp = static_cast<const T*>(p.x.p) + q.n * p.x.sb + q.cv * V;
-    const T* zp = static_cast<const T*>(p.z.p) + q.n * p.z.sb + q.cv * V;
-    const int64_t base = q.n * p.S * p.C + q.cv * V;
+    const T* xp = static_cast<const T*>(p.x.p) + q.n * p.x.sb + q.d0;
+    const T* zp = static_cast<const T*>(p.z.p) + q.n * p.z.sb + q.d0;
+    const int64_t base = q.n * p.S * p.C + q.d0;
     for (int64_t t = q.t0 + q.strip; t < q.t1; t += U * q.strips) {
       typename VecN<T, V>::type x[U], z[U], g[U];
 #pragma unroll
       for (int k = 0; k < U; ++k) {
         const int64_t tk = t + k * q.strips;
-        const int m = tk < q.t1 ? V : 0;
+        const int m = tk < q.t1 ? q.width : 0;
         x[k] = load_n<T, V>(xp + tk * p.x.st, m, p.vec);
         g[k] = load_n<T, V>(static_cast<const T*>(p.dy) + base + tk * p.C, m, p.vec);
         if (gated) z[k] = load_n<T, V>(zp + tk * p.z.st, m, p.vec);
@@ -454,9 +498,9 @@ __global__ __launch_bounds__(256) void k_norm_slab_bwd(NormDev p) {
         if (OUT) {
 #pragma unroll
           for (int i = 0; i < V; ++i) o[i] = rstd * (fmaf(du[i], w[i], -s1) - xf[i] * s2);
-          store_n<T, V>(static_cast<T*>(p.dx) + base + tk * p.C, o, tk < q.t1 ? V : 0, p.vec);
+          store_n<T, V>(static_cast<T*>(p.dx) + base + tk * p.C, o, tk < q.t1 ? q.width : 0, p.vec);
         } else if (tk < q.t1) {
-          if (gated) store_n<T, V>(static_cast<T*>(p.dz) + base + tk * p.C, dz, V, p.vec);
+          if (gated) store_n<T, V>(static_cast<T*>(p.dz) + base + tk * p.C, dz, q.width, p.vec);
 #pragma unroll
           for (int i = 0; i < V; ++i) {
             db[i] += du[i];
@@ -477,9 +521,9 @@ __global__ __launch_bounds__(256) void k_norm_slab_bwd(NormDev p) {
 #pragma unroll
         for (int i = 0; i < V; ++i) dw[i] += o[i], db[i] += o[V + i];
       }
-      float* out = p.part + (q.n * p.chunks + q.chunk) * 2 * p.C + q.cv * V;
-      store_n<float, V>(out, dw, V, false);
-      store_n<float, V>(out + p.C, db, V, false);
+      float* out = p.part + (q.n * p.chunks + q.chunk) * 2 * p.C + q.d0;
+      store_sums<V>(out, q.at, dw);
+      store_sums<V>(out + p.C, q.at, db);
     }
   }
 }
@@ -561,11 +605,10 @@ void go_rows_bwd(const NormDev& p, unsigned grid, hipStream_t st) {
   else k_norm_rows_bwd<T, V, LG, PV, false><<<grid, 256 * kBwdStrips<PV>, 0, st>>>(p);
 }
 
-// Which of the forms calls reach: the half vectors are the backward's, and it takes whole ones only for groups that
-// fit no other way.
+// The half vectors are the backward's, which takes whole ones only for groups that fit no other way.
 template <typename T, int V, int LG>
 void go_rows(const NormDev& p, int PV, unsigned grid, bool bwd, hipStream_t st) {
-  constexpr bool kHalf = V > 1 && V * sizeof(T) == 8, kWhole = V > 1 && !kHalf;
+  constexpr bool kHalf = V * sizeof(T) == 8;
   constexpr int P2 = LG >= 64 ? 2 : 1, P4 = LG >= 64 ? 4 : 1;
   if (!bwd) {
     if constexpr (!kHalf) {
@@ -573,7 +616,7 @@ void go_rows(const NormDev& p, int PV, unsigned grid, bool bwd, hipStream_t st) 
       else if (PV == 2) k_norm_rows<T, V, LG, P2><<<grid, 256, 0, st>>>(p);
       else k_norm_rows<T, V, LG, P4><<<grid, 256, 0, st>>>(p);
     }
-  } else if constexpr (kWhole) {
+  } else if constexpr (!kHalf) {
     if constexpr (LG == 256) go_rows_bwd<T, V, LG, kMaxPV>(p, grid, st);
   } else {
     if (PV == 1) go_rows_bwd<T, V, LG, 1>(p, grid, st);
@@ -596,33 +639,45 @@ void go_rows_lanes(const NormDev& p, const RowShape& r, unsigned grid, bool bwd,
   }
 }
 
-template <typename T, int V>
+template <typename T>
+void go_rows_form(const NormDev& p, const RowShape& r, unsigned grid, bool bwd, hipStream_t st) {
+  constexpr int V = 16 / sizeof(T);
+  if (r.V == V) go_rows_lanes<T, V>(p, r, grid, bwd, st);
+  else go_rows_lanes<T, V / 2>(p, r, grid, bwd, st);
+}
+
+template <typename T>
 void go_slab(const NormDev& p, unsigned grid, bool bwd, hipStream_t st) {
+  constexpr int V = 16 / sizeof(T);
+  const unsigned groups = unsigned(p.N * p.G);
   if (!bwd) {
     k_norm_slab_stats<T, V><<<grid, 256, 0, st>>>(p);
-    k_norm_slab_join<<<unsigned(p.N * p.G), 256, 0, st>>>(p, V);
+    k_norm_slab_join<<<groups, 256, 0, st>>>(p, V);
     k_norm_slab_out<T, V><<<grid, 256, 0, st>>>(p);
+  } else if (p.z.p) {
+    k_norm_slab_bwd<T, V, false, true><<<grid, 256, 0, st>>>(p);
+    k_norm_slab_coef<<<groups, 256, 0, st>>>(p);
+    k_norm_slab_bwd<T, V, true, true><<<grid, 256, 0, st>>>(p);
   } else {
-    k_norm_slab_bwd<T, V, false><<<grid, 256, 0, st>>>(p);
-    k_norm_slab_coef<<<unsigned(p.N * p.G), 256, 0, st>>>(p);
-    k_norm_slab_bwd<T, V, true><<<grid, 256, 0, st>>>(p);
+    k_norm_slab_bwd<T, V, false, false><<<grid, 256, 0, st>>>(p);
+    k_norm_slab_coef<<<groups, 256, 0, st>>>(p);
+    k_norm_slab_bwd<T, V, true, false><<<grid, 256, 0, st>>>(p);
   }
 }
 
 // How a call is laid out and what it needs of the workspace.
 struct NormPlan {
   RowShape rows;
-  int V;
   int bpr = 1, rpw = 1, slots = 0;
-  int64_t per = 0, chunks = 0, ncv = 0, part = 0, coef = 0, stats = 0, total = 0;
+  int64_t per = 0, chunks = 0, ncv = 0, nvg = 0, part = 0, coef = 0, stats = 0, total = 0;
 };
-NormPlan plan(int64_t N, int64_t S, int64_t C, int64_t G, int V, bool bwd) {
+NormPlan plan(int64_t N, int64_t S, int64_t C, int64_t G, int dtype, bool bwd) {
   NormPlan q;
-  q.V = V;
+  const int V = 16 / elem(dtype);
   const int64_t cg = C / G;
   // A backward lane keeps its channels' parameters and sums too: half the vector (33.6 us instead of 57 for 8064 rows
   // of 2048 bf16 channels with a gate), where the group fits that way.
-  if (S == 1) q.rows = row_shape(cg, bwd && V > 1 ? V / 2 : V);
+  if (S == 1) q.rows = row_shape(cg, bwd ? V / 2 : V);
   if (S == 1 && bwd && !q.rows.LG) q.rows = row_shape(cg, V);
   if (q.rows.LG) {
     const int64_t slots = G * q.rows.LG;
@@ -633,7 +688,8 @@ NormPlan plan(int64_t N, int64_t S, int64_t C, int64_t G, int V, bool bwd) {
     q.total = bwd ? q.per * q.rpw * 2 * C * 4 : 0;
     return q;
   }
-  q.ncv = C / V;
+  q.nvg = ceil_div(cg, V);
+  q.ncv = G * q.nvg;
   q.per = slab_chunk(N, S, q.ncv);
   q.chunks = ceil_div(S, q.per);
   q.part = align256(N * q.chunks * (bwd ? 2 * C : 2 * q.ncv) * 4);
@@ -644,13 +700,11 @@ NormPlan plan(int64_t N, int64_t S, int64_t C, int64_t G, int V, bool bwd) {
 hipError_t launch(const NormArgs& a, const NormGrads* g, hipStream_t st) {
   NormDev p = {};
   p.vec = norm_vec(a, g);
-  const int V = p.vec ? 16 / elem(a.dtype) : 1;
-  const NormPlan q = plan(a.N, a.S, a.C, a.G, V, g != nullptr);
-  if (V == 1) p.vec = 1;  // one element at a time: always aligned
-  p.pvec = reinterpret_cast<uintptr_t>(a.weight) % 16 == 0 && reinterpret_cast<uintptr_t>(a.bias) % 16 == 0;
+  const NormPlan q = plan(a.N, a.S, a.C, a.G, a.dtype, g != nullptr);
+  p.pvec = a.C / a.G % 4 == 0 && reinterpret_cast<uintptr_t>(a.weight) % 16 == 0 && reinterpret_cast<uintptr_t>(a.bias) % 16 == 0;
   p.x = a.x, p.z = a.z, p.weight = a.weight, p.bias = a.bias, p.y = a.y, p.stats = a.stats;
   p.N = a.N, p.S = a.S, p.C = a.C, p.G = int(a.G), p.cg = int(a.C / a.G), p.act = a.act, p.eps = a.eps;
-  p.per = q.per, p.chunks = q.chunks, p.ncv = q.ncv, p.slots = q.slots, p.bpr = q.bpr, p.rpw = q.rpw;
+  p.per = q.per, p.chunks = q.chunks, p.ncv = q.ncv, p.nvg = int(q.nvg), p.slots = q.slots, p.bpr = q.bpr, p.rpw = q.rpw;
   char* ws = static_cast<char*>(a.workspace);
   const bool bwd = g != nullptr, sums = bwd && (g->dw || g->db);
   if (bwd) p.dy = g->dy, p.dx = g->dx, p.dz = g->dz;
@@ -659,16 +713,8 @@ hipError_t launch(const NormArgs& a, const NormGrads* g, hipStream_t st) {
     p.part = sums ? reinterpret_cast<float*>(ws) : nullptr;
     rows = q.per * q.rpw;
     const unsigned grid = unsigned(q.per * q.bpr);
-    const int rv = q.rows.V;
-    if (a.dtype == 1) {
-      if (rv == 1) go_rows_lanes<__bf16, 1>(p, q.rows, grid, bwd, st);
-      else if (rv == 4) go_rows_lanes<__bf16, 4>(p, q.rows, grid, bwd, st);
-      else go_rows_lanes<__bf16, 8>(p, q.rows, grid, bwd, st);
-    } else {
-      if (rv == 1) go_rows_lanes<float, 1>(p, q.rows, grid, bwd, st);
-      else if (rv == 2) go_rows_lanes<float, 2>(p, q.rows, grid, bwd, st);
-      else go_rows_lanes<float, 4>(p, q.rows, grid, bwd, st);
-    }
+    if (a.dtype == 1) go_rows_form<__bf16>(p, q.rows, grid, bwd, st);
+    else go_rows_form<float>(p, q.rows, grid, bwd, st);
   } else {
     p.part = reinterpret_cast<float*>(ws);
     p.coef = reinterpret_cast<float*>(ws + q.part);
@@ -676,8 +722,8 @@ hipError_t launch(const NormArgs& a, const NormGrads* g, hipStream_t st) {
     rows = a.N * q.chunks;
     const int64_t lanes = q.ncv < 256 ? q.ncv : 256;
     const unsigned grid = unsigned(ceil_div(q.ncv, lanes) * rows);
-    if (a.dtype == 1) V == 1 ? go_slab<__bf16, 1>(p, grid, bwd, st) : go_slab<__bf16, 8>(p, grid, bwd, st);
-    else V == 1 ? go_slab<float, 1>(p, grid, bwd, st) : go_slab<float, 4>(p, grid, bwd, st);
+    if (a.dtype == 1) go_slab<__bf16>(p, grid, bwd, st);
+    else go_slab<float>(p, grid, bwd, st);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !sums) return e;
@@ -690,15 +736,8 @@ hipError_t launch(const NormArgs& a, const NormGrads* g, hipStream_t st) {
 
 }  // namespace
 
-// Whether rows can be read as vectors depends on addresses, so the workspace holds either way.
 int64_t norm_workspace(int64_t N, int64_t S, int64_t C, int64_t G, int dtype, bool backward) {
-  const int V = 16 / elem(dtype);
-  int64_t need = plan(N, S, C, G, 1, backward).total;
-  if (C / G % V == 0) {
-    const int64_t v = plan(N, S, C, G, V, backward).total;
-    need = v > need ? v : need;
-  }
-  return need;
+  return plan(N, S, C, G, dtype, backward).total;
 }
 
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t st) { return launch(a, nullptr, st); }

@@ -381,14 +381,15 @@ typedef struct ll_scan_inputs {
 } ll_scan_inputs;
 
 /* Bytes of workspace of the forward (backward = 0; may be 0: then the workspace may be NULL) or of the
- * backward; bytes of the states that a forward leaves for the backward.  0 for invalid arguments. */
+ * backward (which is at least the forward's: one workspace serves both in turn); bytes of the states that
+ * a forward leaves for the backward.  0 for invalid arguments. */
 size_t ll_selective_scan_workspace_size(int64_t B, int64_t T, int64_t D, int64_t N, int64_t groups,
                                         int32_t backward);
 size_t ll_selective_scan_states_bytes(int64_t B, int64_t T, int64_t D, int64_t N);
 
 /* Forward: y [batch, T, channels] and the final state [batch, channels, N].  states (16-byte aligned,
- * NULL for inference) receives the state before every 64th token (N <= 16; 32nd up to 32 states, 16th
- * beyond), in the library's own layout, for ll_selective_scan_bwd on the same inputs. */
+ * NULL for inference) receives the state before every 16th token, in the library's own layout, for
+ * ll_selective_scan_bwd on the same inputs. */
 ll_status ll_selective_scan_fwd(const ll_scan_inputs* in, const float* initial_state, void* y,
                                 float* final_state, float* states, void* workspace,
                                 size_t workspace_bytes, void* stream);

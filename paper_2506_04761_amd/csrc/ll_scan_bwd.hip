@@ -15,8 +15,13 @@
 // as a row-broadcast (DPP) operand.  Step sizes, inputs and dy pass through LDS, 16 tokens x 32 channels to a wave,
 // eight channels of a token to a lane, and the sums over states come back the same way.  A chunk of 16 tokens starts
 // from the state that the forward saved before it: it is run once for the states before its tiles of 4 tokens, then
-// the tiles are taken last to first, forming rates and states again in registers.  The four waves of a workgroup are added in
-// LDS, workgroups by k_scan_bc.
+// the tiles are taken last to first, forming rates and states again in registers.  The waves of a workgroup are added
+// in LDS, workgroups by k_scan_bc.
+//
+// Bound by the vector ALU: two waves a SIMD (256 registers: rates, states and gradients of 4 tokens x 2 blocks, the
+// sums over channels), about 3200 instructions per 16 tokens x 32 channels x 16 states, the ALU busy 81 % of the time.
+// bf16, 2 x 4032 tokens of 2048 channels, 16 states: k_scan_bwd 250 us, k_scan_rev 69, the join 13, k_scan_bc 6.5, the
+// parameters' sums 5.  One block of 16 channels instead of two, at three and four waves a SIMD: 291 and 383 us.
 #include "ll_layer.hpp"
 #include "ll_layer_device.hpp"
 

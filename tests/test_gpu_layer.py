@@ -136,6 +136,25 @@ def test_conv_tokens_continue_a_prompt(D, W, dtype):
     assert torch.equal(state, x[:, T - W + 1:])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_conv_long_runs(dtype):
+    """Enough tokens for lanes that walk several groups of four, and an end inside a run.  The parameters' sums are
+    of 6322 terms, formed with at most 50 roundings of 2^-24 of sums of magnitudes, which are some 80 times the sum of
+    terms of either sign: 2.4e-4."""
+    import paper_2506_04761_amd as ll
+    B, T, D, W, ns = 2, 4100, 1030, 4, [4100, 2222]
+    d = _Draw(9, dtype)
+    x, w, b, dy = d.rows(B, T, D, off=1), d.f32(D, W), d.f32(D), d.rows(B, T, D)
+    xr, dyr = _blank(ns, x, dy)
+    y = ll.ll_causal_conv_fwd(x, w, b, lengths=_lengths(ns))
+    g = ll.ll_causal_conv_bwd(x, w, b, dy, lengths=_lengths(ns))
+    _ok(y, layer.conv(xr, _np(w), _np(b), True, None, ns)[0], TOL[dtype], "y")
+    want = layer.conv_grad(xr, _np(w), dyr, _np(b), True, None, ns, None)
+    _ok(g[0], want[0], TOL[dtype], "dx")
+    _ok(g[1], want[1], 2.4e-4, "dweight")
+    _ok(g[2], want[2], 2.4e-4, "dbias")
+
+
 # ------------------------------------------------------------------------------------ selective scan
 
 SCAN = [  # B, T, D, N, groups, lengths, start of the columns
@@ -191,6 +210,29 @@ def test_scan(case, gate, dtype):
     # the final state in place of the initial one; without the states for a backward
     y2 = ll.ll_selective_scan_fwd(x, dt, A, Bm, Cm, skip, z, bias, True, init, init, _lengths(ns))
     assert torch.equal(y2, y) and torch.equal(init, final)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,T,D,N", [(1, 4300, 20, 16), (2, 300, 1100, 16), (1, 4200, 9, 24)])
+def test_scan_in_many_segments(B, T, D, N, dtype):
+    """Few channels (hundreds of segments a channel, joined in runs) and many (joined in one).  Three roundings of 2^-24
+    a token, carried over at most T tokens."""
+    import paper_2506_04761_amd as ll
+    d = _Draw(T + D, dtype)
+    x, dt, z, Bm, Cm, A, skip, bias, init = _scan_inputs(d, B, T, D, N, 1, None)
+    dy, df = d.rows(B, T, D), d.f32(B, D, N)
+    carried = max(1e-4, 3 * T * 2.0 ** -24)
+    tol = {"f32": carried, "bf16": 2.0 ** -8 + carried}
+    final, states = init.clone(), ll.ll_selective_scan_states(x, Bm)
+    y = ll.ll_selective_scan_fwd(x, dt, A, Bm, Cm, skip, z, bias, True, init, final, None, states)
+    g = ll.ll_selective_scan_bwd(x, dt, A, Bm, Cm, states, dy, skip, z, bias, True, None, df, True)
+    args = (_np(x), _np(dt), _np(A), _np(Bm)[:, :, None], _np(Cm)[:, :, None])
+    wy, wf = layer.scan(*args, _np(skip), _np(z), _np(bias), True, _np(init), None)
+    want = layer.scan_grad(*args, _np(dy), _np(skip), _np(z), _np(bias), True, _np(init), None, _np(df))
+    _ok(y, wy, tol[dtype], "y")
+    _ok(final, wf, tol["f32"], "final state")
+    for name, got in zip(("x", "dt", "A", "B", "C", "D", "z", "dt_bias", "initial"), g):
+        _ok(got, want[name].reshape(got.shape), tol[dtype] if got.dtype == x.dtype else tol["f32"], "d" + name)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

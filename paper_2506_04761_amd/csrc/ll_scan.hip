@@ -12,7 +12,7 @@
 // input's product, the state's and the output's FMA (3 to 4 cycles each beside the exp, with four waves on a SIMD; a
 // lone wave issues one in 8), and about 30 instructions per token and channel.  bf16, 16 states, 4 x 8192 tokens of
 // 2048 channels: the two passes below take 190 and 245 us, in which counters see the ALU busy for 96 and 95 % of the
-// cycles, and the joining of segments between them 20; the bytes alone would take 104.
+// cycles, and the joining of segments between them 17; the bytes alone would take 104.
 //
 // The states of a channel are a chain over tokens, and channels x sequences alone rarely make four waves a SIMD, so the
 // length is split into S segments, run twice: k_scan_fwd<OUT = false> runs every segment but the last by itself (the
@@ -245,54 +245,67 @@ __global__ __launch_bounds__(64 * kWaves, NP <= 16 ? 4 : (NP <= 24 ? 3 : (NP <= 
 // A workgroup takes 64 adjacent (channel, state) chains; its RUNS rows of 64 threads take a run of segments each: first
 // a run's decay and own end, then, from the runs before it, its segments' starts.  Bound by reading and writing the
 // records.  RUNS = 1 reads them once and is for few segments or more workgroups than are resident at a time (131072
-// chains of 63 segments 20 us, RUNS = 16 30; 65536 chains of 63 segments 13.4 and 15.7).  RUNS = 16 has 16 times the
-// loads in flight (2048 chains of 39 segments 5 us, RUNS = 1 9.4; 32768 chains of 255 segments 22).
+// chains of 63 segments 17 us, RUNS = 16 28; 65536 chains of 63 segments 10.4 and 14.4).  RUNS = 16 has 16 times the
+// loads in flight (1152 chains of 1308 segments 23 us, RUNS = 1 83; 32768 chains of 255 segments 22 and 24.5; 8192
+// chains of 39 segments 5.2 and 6.1).
 template <int RUNS>
 __global__ __launch_bounds__(64 * RUNS) void k_scan_join(ScanJoin p) {
   constexpr int AHEAD = RUNS == 1 ? 32 : 8;  // segments whose loads are in flight together
   __shared__ float s_f[RUNS][64], s_v[RUNS][64];
-  const int run = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int run = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int64_t per = p.D * p.NP, chains = (per + 63) / 64, b = blockIdx.x / chains, e = blockIdx.x % chains * 64 + lane;
   const bool on = e < per;
   const int64_t ch = on ? e / p.NP : 0;
   const int n = on ? int(e - ch * p.NP) : 0;
   const float A2 = on && n < p.N ? p.A[ch * p.N + n] * kLog2e : 0.0f;
   const float init = on && p.init && n < p.N ? p.init[(b * p.D + ch) * p.N + n] : 0.0f;
-  float* q = p.h + b * p.S * per + (on ? e : 0);
-  const float* d = p.d + b * p.S * p.D + ch;
   const int len = (p.S + RUNS - 1) / RUNS, s0 = run * len, s1 = s0 + len < p.S ? s0 + len : p.S;
-  auto at = [&](int s) { return int64_t(p.reverse ? p.S - 1 - s : s); };
-  float f = 1.0f, v = 0.0f;
-  for (int s = s0; RUNS > 1 && s < s1; s += AHEAD) {
-    float own[AHEAD], step[AHEAD];
+  // Addresses step through the records: a product of 64 bits for each would be most of the work.
+  const int64_t h_step = p.reverse ? -per : per, d_step = p.reverse ? -p.D : p.D, first = p.reverse ? p.S - 1 - s0 : s0;
+  float* const q0 = p.h + (b * p.S + first) * per + (on ? e : 0);
+  const float* const d0 = p.d + (b * p.S + first) * p.D + ch;
+  // Nothing follows the last segment: it has no record of its own.  Loads do not depend on conditions (a branch between
+  // them would wait), so what is behind the last repeats it and is masked when used.
+  const int known = s1 < p.S ? s1 : p.S - 1;
+  float own[AHEAD], step[AHEAD];
+  const float *q = q0, *d = d0;
+  auto fetch = [&](int s) {
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-      const bool in = s + k < s1 && s + k < p.S - 1;  // nothing follows the last segment: it has no record of its own
-      own[k] = in ? q[at(s + k) * per] : 0.0f;
-      step[k] = in ? d[at(s + k) * p.D] : 0.0f;
+      own[k] = *q;
+      step[k] = *d;
+      const bool more = s + k + 1 < known;
+      q += more ? h_step : 0;
+      d += more ? d_step : 0;
     }
+    __builtin_amdgcn_sched_barrier(0);  // all on their way before the first is used
+  };
+  float f = 1.0f, v = 0.0f;
+  for (int s = s0; RUNS > 1 && s < known; s += AHEAD) {
+    fetch(s);
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
+      const bool in = s + k < known;
       const float a = s + k == 0 ? 0.0f : fast_exp2(A2 * step[k]);
-      v = s + k == 0 ? own[k] : fmaf(a, v, own[k]);
-      f *= a;
+      const float next = s + k == 0 ? own[k] : fmaf(a, v, own[k]);
+      v = in ? next : v;
+      f *= in ? a : 1.0f;
     }
   }
   s_f[run][lane] = f, s_v[run][lane] = v;
   __syncthreads();
   float h = init;
   for (int i = 0; i < run; ++i) h = i == 0 && s_f[0][lane] == 0.0f ? s_v[0][lane] : fmaf(s_f[i][lane], h, s_v[i][lane]);
+  float* out = q0;
+  q = q0, d = d0;
   for (int s = s0; s < s1; s += AHEAD) {
-    float own[AHEAD], step[AHEAD];
+    if (s < known) fetch(s);
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-      const bool in = s + k < s1 && s + k < p.S - 1;
-      own[k] = in ? q[at(s + k) * per] : 0.0f;
-      step[k] = in ? d[at(s + k) * p.D] : 0.0f;
-    }
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      if (on && s + k < s1) q[at(s + k) * per] = h;
+      if (s + k < s1) {
+        if (on) *out = h;
+        out += h_step;
+      }
       h = s + k == 0 ? own[k] : fmaf(fast_exp2(A2 * step[k]), h, own[k]);
     }
   }

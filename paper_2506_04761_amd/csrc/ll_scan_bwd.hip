@@ -20,7 +20,7 @@
 //
 // Bound by the vector ALU: two waves a SIMD (256 registers: rates, states and gradients of 4 tokens x 2 blocks, the
 // sums over channels), about 3200 instructions per 16 tokens x 32 channels x 16 states, the ALU busy 81 % of the time.
-// bf16, 2 x 4032 tokens of 2048 channels, 16 states: k_scan_bwd 250 us, k_scan_rev 69, the join 13, k_scan_bc 6.5, the
+// bf16, 2 x 4032 tokens of 2048 channels, 16 states: k_scan_bwd 250 us, k_scan_rev 69, the join 10, k_scan_bc 6.5, the
 // parameters' sums 5.  One block of 16 channels instead of two, at three and four waves a SIMD: 291 and 383 us.
 #include "ll_layer.hpp"
 #include "ll_layer_device.hpp"

@@ -29,7 +29,7 @@ struct NormDev {
   float* coef;         // slab backward: [N, G, 2]
   int64_t N, S, C, per, chunks, ncv;  // per: rows form, workgroups over the rows; slab, tokens of a chunk
   int G, cg, act, vec, pvec;  // pvec: a lane's weights and biases are 16-byte aligned
-  int nvg;              // slab: channel vectors of a group (the last may be short)
+  int nvg, lanes;       // slab: channel vectors of a group (the last may be short), of a workgroup
   int slots, bpr, rpw;  // rows form: lanes of a row, workgroups of a row, rows of a workgroup
   float eps;
 };
@@ -330,7 +330,7 @@ struct SlabPlan {
   Place at;
   int64_t d0;    // its first channel
   __device__ SlabPlan(const NormDev& p) {
-    lanes = p.ncv < 256 ? int(p.ncv) : 256;
+    lanes = p.lanes;
     strips = 256 / lanes;
     strip = threadIdx.x / lanes;
     const int64_t cblocks = (p.ncv + lanes - 1) / lanes;
@@ -589,9 +589,20 @@ int64_t row_blocks(int64_t rows, int rpw, int bpr, int most, int least) {
   return all < want ? all : want;
 }
 
+// Channel vectors of a slab workgroup, the other threads taking other tokens: all of them up to 256 (130 vectors: 49 us
+// together, 55 in blocks of 64), beyond that the block of 256, 128 or 64 that leaves the fewest threads without work
+// (training step of 64 x 512 fp32 tokens of 280 vectors: 374 us in blocks of 64, 467 in blocks of 256).
+int64_t slab_lanes(int64_t ncv) {
+  if (ncv <= 256) return ncv;
+  int64_t best = 256;
+  for (int64_t lanes = 128; lanes >= 64; lanes /= 2)
+    if (ceil_div(ncv, lanes) * lanes < ceil_div(ncv, best) * best) best = lanes;
+  return best;
+}
+
 // Tokens of a chunk of the slab form, for about 1024 workgroups.
 int64_t slab_chunk(int64_t N, int64_t S, int64_t ncv) {
-  const int64_t lanes = ncv < 256 ? ncv : 256, strips = 256 / lanes, cblocks = ceil_div(ncv, lanes);
+  const int64_t lanes = slab_lanes(ncv), strips = 256 / lanes, cblocks = ceil_div(ncv, lanes);
   int64_t chunks = ceil_div(1024, N * cblocks);
   const int64_t least = 8 * strips;
   int64_t per = ceil_div(S, chunks);
@@ -726,8 +737,8 @@ hipError_t launch(const NormArgs& a, const NormGrads* g, hipStream_t st) {
     p.coef = reinterpret_cast<float*>(ws + q.part);
     if (!bwd && !p.stats) p.stats = p.coef;
     rows = a.N * q.chunks;
-    const int64_t lanes = q.ncv < 256 ? q.ncv : 256;
-    const unsigned grid = unsigned(ceil_div(q.ncv, lanes) * rows);
+    p.lanes = int(slab_lanes(q.ncv));
+    const unsigned grid = unsigned(ceil_div(q.ncv, p.lanes) * rows);
     if (a.dtype == 1) go_slab<__bf16>(p, grid, bwd, st);
     else go_slab<float>(p, grid, bwd, st);
   }

@@ -10,7 +10,7 @@
 //
 // Bound by the vector ALU: per token, channel and state one exp (8 cycles of a wave), and the rate's product, the
 // input's product, the state's and the output's FMA (3 to 4 cycles each beside the exp, with four waves on a SIMD; a
-// lone wave issues one in 8), and about 30 instructions per token and channel.  bf16, 16 states, 4 x 8192 tokens of
+// lone wave issues one in 8), and about 27 instructions per token and channel.  bf16, 16 states, 4 x 8192 tokens of
 // 2048 channels: the two passes below take 190 and 245 us, in which counters see the ALU busy for 96 and 95 % of the
 // cycles, and the joining of segments between them 17; the bytes alone would take 104.
 //

@@ -5,7 +5,7 @@ for one token; and the three as differentiable functions.
 As in the rest of the binding, the wrappers check and pass arguments and every step of the computation runs
 in the library's HIP kernels.  x, dt, z, gate, B and C may be columns of wider rows (channels adjacent);
 everything else is contiguous.  Work is enqueued on `stream` (default: torch's current stream) and is not
-synchronised.
+synchronised; outputs, gradients and workspaces that a call allocates are memory of that stream.
 """
 
 import ctypes
@@ -13,7 +13,8 @@ from collections import namedtuple
 
 import torch
 
-from ._lib import LL_OK, LLError, _check, _dtype_code, _i32, _i64, _ptr, _stream, _sz, _vp, lib
+from ._lib import (LL_OK, LLError, _check, _dtype_code, _i32, _i64, _ptr, _results, _scratch, _stream, _sz, _vp,
+                   lib)
 
 LL_ACT_NONE, LL_ACT_SILU = 0, 1
 
@@ -93,10 +94,10 @@ def _buffer(nbytes, device):
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
-def _sized(workspace, need, device):
-    """A workspace's address and bytes: the caller's, or a new one where a call needs any."""
+def _sized(workspace, need, device, stream):
+    """A call's workspace: the caller's, or a new one."""
     if workspace is None:
-        workspace = _buffer(need(), device)
+        workspace = _scratch(lambda: _buffer(need(), device), stream)
     _check(workspace, "workspace", torch.uint8)
     return workspace
 
@@ -118,7 +119,7 @@ def ll_causal_conv_fwd(x, weight, bias=None, act=LL_ACT_SILU, initial_state=None
     _lengths(lengths, B)
     code = _dtype_code(x)
     if out is None:
-        out = x.new_empty((B, T, D))
+        out = _results(lambda: x.new_empty((B, T, D)), stream)
     else:
         _check(out, "out", x.dtype, (B, T, D))
     _ok(lib.ll_causal_conv_fwd(x.data_ptr(), x.stride(0), x.stride(1), weight.data_ptr(), _ptr(bias),
@@ -139,7 +140,7 @@ def ll_causal_conv_step(x, weight, bias, state, act=LL_ACT_SILU, new_state=None,
     _opt(new_state, "new_state", x.dtype, (B, W - 1, D))
     code = _dtype_code(x)
     if out is None:
-        out = x.new_empty((B, D))
+        out = _results(lambda: x.new_empty((B, D)), stream)
     else:
         _check(out, "out", x.dtype, (B, D))
     _ok(lib.ll_causal_conv_step(x.data_ptr(), x.stride(0), weight.data_ptr(), _ptr(bias), state.data_ptr(),
@@ -169,14 +170,15 @@ def ll_causal_conv_bwd(x, weight, bias, d_y, act=LL_ACT_SILU, initial_state=None
     _lengths(lengths, B)
     code = _dtype_code(x)
     if grads is None:
-        grads = ConvGrads(x.new_empty((B, T, D)), torch.empty_like(weight), None if bias is None else torch.empty_like(bias),
-                          None if initial_state is None else torch.empty_like(initial_state))
+        grads = _results(lambda: ConvGrads(x.new_empty((B, T, D)), torch.empty_like(weight),
+                                           None if bias is None else torch.empty_like(bias),
+                                           None if initial_state is None else torch.empty_like(initial_state)), stream)
     dx, dw, db, di = grads
     _check(dx, "grads.x", x.dtype, (B, T, D))
     _check(dw, "grads.weight", torch.float32, (D, W))
     _opt(db, "grads.bias", torch.float32, (D,))
     _opt(di, "grads.initial_state", x.dtype, (B, W - 1, D))
-    ws = _sized(workspace, lambda: lib.ll_causal_conv_bwd_workspace_size(code, B, T, D, W), x.device)
+    ws = _sized(workspace, lambda: lib.ll_causal_conv_bwd_workspace_size(code, B, T, D, W), x.device, stream)
     _ok(lib.ll_causal_conv_bwd(x.data_ptr(), x.stride(0), x.stride(1), weight.data_ptr(), _ptr(bias),
                                _ptr(initial_state), _ptr(lengths), d_y.data_ptr(), _ptr(d_final_state),
                                dx.data_ptr(), dw.data_ptr(), _ptr(db), _ptr(di), B, T, D, W, act, code,
@@ -246,10 +248,10 @@ def ll_selective_scan_fwd(x, dt, A, B, C, D=None, z=None, dt_bias=None, delta_so
     if states is not None:
         _check_states(states, s)
     if out is None:
-        out = x.new_empty(x.shape)
+        out = _results(lambda: x.new_empty(x.shape), stream)
     else:
         _check(out, "out", x.dtype, x.shape)
-    ws = _sized(workspace, lambda: lib.ll_selective_scan_workspace_size(s.batch, s.T, s.channels, s.N, s.groups, 0), x.device)
+    ws = _sized(workspace, lambda: lib.ll_selective_scan_workspace_size(s.batch, s.T, s.channels, s.N, s.groups, 0), x.device, stream)
     _ok(lib.ll_selective_scan_fwd(s, _ptr(initial_state), out.data_ptr(), _ptr(final_state), _ptr(states),
                                   _ptr(ws), ws.numel(), _stream(stream)))
     return out
@@ -264,7 +266,7 @@ def ll_selective_scan_step(x, dt, A, B, C, state, D=None, z=None, dt_bias=None, 
     _check(state, "state", torch.float32, shape)
     _opt(new_state, "new_state", torch.float32, shape)
     if out is None:
-        out = x.new_empty(x.shape)
+        out = _results(lambda: x.new_empty(x.shape), stream)
     else:
         _check(out, "out", x.dtype, x.shape)
     _ok(lib.ll_selective_scan_step(s, state.data_ptr(), (state if new_state is None else new_state).data_ptr(),
@@ -284,10 +286,11 @@ def ll_selective_scan_bwd(x, dt, A, B, C, states, d_y, D=None, z=None, dt_bias=N
     _opt(d_final_state, "d_final_state", torch.float32, shape)
     if grads is None:
         new = x.new_empty
-        grads = ScanGrads(new(x.shape), new(x.shape), torch.empty_like(A), new(B.shape), new(C.shape),
-                          None if D is None else torch.empty_like(D), None if z is None else new(x.shape),
-                          None if dt_bias is None else torch.empty_like(dt_bias),
-                          A.new_empty(shape) if initial_state_grad else None)
+        grads = _results(lambda: ScanGrads(new(x.shape), new(x.shape), torch.empty_like(A), new(B.shape), new(C.shape),
+                                           None if D is None else torch.empty_like(D),
+                                           None if z is None else new(x.shape),
+                                           None if dt_bias is None else torch.empty_like(dt_bias),
+                                           A.new_empty(shape) if initial_state_grad else None), stream)
     g = ScanGrads(*grads)
     _check(g.x, "grads.x", x.dtype, x.shape)
     _check(g.dt, "grads.dt", x.dtype, x.shape)
@@ -298,7 +301,7 @@ def ll_selective_scan_bwd(x, dt, A, B, C, states, d_y, D=None, z=None, dt_bias=N
     _opt(g.z, "grads.z", x.dtype, x.shape)
     _opt(g.dt_bias, "grads.dt_bias", torch.float32, (s.channels,))
     _opt(g.initial_state, "grads.initial_state", torch.float32, shape)
-    ws = _sized(workspace, lambda: lib.ll_selective_scan_workspace_size(s.batch, s.T, s.channels, s.N, s.groups, 1), x.device)
+    ws = _sized(workspace, lambda: lib.ll_selective_scan_workspace_size(s.batch, s.T, s.channels, s.N, s.groups, 1), x.device, stream)
     _ok(lib.ll_selective_scan_bwd(s, states.data_ptr(), d_y.data_ptr(), _ptr(d_final_state), g.x.data_ptr(),
                                   g.dt.data_ptr(), _ptr(g.z), g.A.data_ptr(), g.B.data_ptr(), g.C.data_ptr(),
                                   _ptr(g.D), _ptr(g.dt_bias), _ptr(g.initial_state), _ptr(ws), ws.numel(),
@@ -344,10 +347,10 @@ def ll_group_norm_fwd(x, groups, weight=None, bias=None, gate=None, eps=1e-5, ac
     _opt(stats, "stats", torch.float32, (N, groups, 2))
     code = _dtype_code(x)
     if out is None:
-        out = x.new_empty(x.shape)
+        out = _results(lambda: x.new_empty(x.shape), stream)
     else:
         _check(out, "out", x.dtype, x.shape)
-    ws = _sized(workspace, lambda: _norm_need(x, groups, False), x.device)
+    ws = _sized(workspace, lambda: _norm_need(x, groups, False), x.device, stream)
     _ok(lib.ll_group_norm_fwd(*rows, _ptr(weight), _ptr(bias), out.data_ptr(), _ptr(stats), N, S, C, groups, eps, act,
                               code, _ptr(ws), ws.numel(), _stream(stream)))
     return out
@@ -363,14 +366,15 @@ def ll_group_norm_bwd(x, groups, weight, bias, stats, d_y, gate=None, act=LL_ACT
     _check(d_y, "d_y", x.dtype, x.shape)
     code = _dtype_code(x)
     if grads is None:
-        grads = NormGrads(x.new_empty(x.shape), None if weight is None else torch.empty_like(weight),
-                          None if bias is None else torch.empty_like(bias), None if gate is None else x.new_empty(x.shape))
+        grads = _results(lambda: NormGrads(x.new_empty(x.shape), None if weight is None else torch.empty_like(weight),
+                                           None if bias is None else torch.empty_like(bias),
+                                           None if gate is None else x.new_empty(x.shape)), stream)
     g = NormGrads(*grads)
     _check(g.x, "grads.x", x.dtype, x.shape)
     _opt(g.weight, "grads.weight", torch.float32, (C,))
     _opt(g.bias, "grads.bias", torch.float32, (C,))
     _opt(g.gate, "grads.gate", x.dtype, x.shape)
-    ws = _sized(workspace, lambda: _norm_need(x, groups, True), x.device)
+    ws = _sized(workspace, lambda: _norm_need(x, groups, True), x.device, stream)
     _ok(lib.ll_group_norm_bwd(*rows, _ptr(weight), _ptr(bias), stats.data_ptr(), d_y.data_ptr(), g.x.data_ptr(),
                               _ptr(g.gate), _ptr(g.weight), _ptr(g.bias), N, S, C, groups, act, code, _ptr(ws),
                               ws.numel(), _stream(stream)))

@@ -152,7 +152,32 @@ def _stream(stream):
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
-def _prepare(variant, q, k, v, log_alpha, beta, lam, C, out, workspace, grouped=False):
+# What a call allocates by itself is memory of the stream that its work runs on, as if the call stood under
+# torch.cuda.stream(stream): a block of the current stream could be handed to the next allocation there (a
+# workspace as soon as the wrapper returns) or still be in use there, while the kernels run on the other stream.
+
+def _scratch(make, stream):
+    """make(), a tensor that dies with the call."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        return make()
+
+
+def _results(make, stream):
+    """make(), a tensor or a tuple of them that the caller gets and uses on the current stream too."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        made = make()
+    current = torch.cuda.current_stream(stream.device)
+    for t in (made,) if isinstance(made, torch.Tensor) else made:
+        if t is not None:
+            t.record_stream(current)
+    return made
+
+
+def _prepare(variant, q, k, v, log_alpha, beta, lam, C, out, workspace, stream, grouped=False):
     B, T, Hqk, dk = q.shape
     H = v.shape[2] if grouped else Hqk
     dv = v.shape[-1]
@@ -167,12 +192,12 @@ def _prepare(variant, q, k, v, log_alpha, beta, lam, C, out, workspace, grouped=
         _check(lam, "lambda", torch.float32, (B, T, H, L))
     code = _dtype_code(q)
     if out is None:
-        out = q.new_empty((B, T, H, dv))
+        out = _results(lambda: q.new_empty((B, T, H, dv)), stream)
     else:
         _check(out, "out", q.dtype, (B, T, H, dv))
     if workspace is None:
         need = ll_workspace_size(variant, code, B, T, H, dk, dv, C, lam is not None)
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+        workspace = _scratch(lambda: torch.empty(max(need, 1), dtype=torch.uint8, device=q.device), stream)
     _check(workspace, "workspace", torch.uint8)
     return (B, T, H, dk, dv, code), out, workspace
 
@@ -181,7 +206,7 @@ def ll_mamba2_fwd(q, k, v, log_alpha, lam, C, out=None, workspace=None, stream=N
     """Log-linear Mamba-2 forward on device tensors laid out [B, T, H, d]; `lam` may be None
     (all level weights 1, i.e. Mamba-2).  Returns `out`.  Work is enqueued on `stream`
     (default: torch's current stream) and is not synchronised."""
-    (B, T, H, dk, dv, code), out, ws = _prepare(LL_MAMBA2, q, k, v, log_alpha, None, lam, C, out, workspace)
+    (B, T, H, dk, dv, code), out, ws = _prepare(LL_MAMBA2, q, k, v, log_alpha, None, lam, C, out, workspace, stream)
     st = lib.ll_mamba2_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(lam), _ptr(out),
                            B, T, H, dk, dv, C, code, _ptr(ws), ws.numel(), _stream(stream))
     if st != LL_OK:
@@ -225,11 +250,11 @@ def _ml_call(q, k, v, log_alpha, Lam, C, out, workspace, stream, handles):
         _check(Lam, "Lambda", torch.float32, (B, T, H, L, dk, dk))
     code = _dtype_code(q)
     if out is None:
-        out = q.new_empty((B, T, H, dv))
+        out = _results(lambda: q.new_empty((B, T, H, dv)), stream)
     else:
         _check(out, "out", q.dtype, (B, T, H, dv))
     if workspace is None:
-        workspace = ll_mamba2_matrix_lambda_workspace(q, v, C, full=form == LL_LAMBDA_FULL)
+        workspace = _scratch(lambda: ll_mamba2_matrix_lambda_workspace(q, v, C, full=form == LL_LAMBDA_FULL), stream)
     _check(workspace, "workspace", torch.uint8)
     args = [_ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(Lam), form, _ptr(out), B, T, H, dk, dv, C, code,
             _ptr(workspace), workspace.numel(), _stream(stream)]
@@ -269,7 +294,7 @@ def ll_mamba2_fwd_grouped(q, k, v, log_alpha, lam, C, out=None, workspace=None, 
     and v, log_alpha, lam, out have H heads (H a multiple of H_qk; head h uses query/key head
     h // (H // H_qk)).  Returns `out`."""
     (B, T, H, dk, dv, code), out, ws = _prepare(LL_MAMBA2, q, k, v, log_alpha, None, lam, C, out, workspace,
-                                                grouped=True)
+                                                stream, grouped=True)
     st = lib.ll_mamba2_fwd_grouped(_ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(lam), _ptr(out),
                                    B, T, H, q.shape[2], dk, dv, C, code, _ptr(ws), ws.numel(), _stream(stream))
     if st != LL_OK:
@@ -303,7 +328,7 @@ def ll_mamba2_decode_step(q, k, v, log_alpha, lam, state, t, L, out=None, stream
         _check(lam, "lambda", torch.float32, (B, H, L))
     _check(state, "state", torch.uint8)
     if out is None:
-        out = q.new_empty((B, H, dv))
+        out = _results(lambda: q.new_empty((B, H, dv)), stream)
     else:
         _check(out, "out", q.dtype, (B, H, dv))
     st = lib.ll_mamba2_decode_step(_ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(lam), _ptr(out), _ptr(state),
@@ -335,7 +360,7 @@ def ll_gdn_decode_step(q, k, v, log_alpha, beta, lam, state, t, L, out=None, str
         _check(lam, "lambda", torch.float32, (B, H, L))
     _check(state, "state", torch.uint8)
     if out is None:
-        out = q.new_empty((B, H, dv))
+        out = _results(lambda: q.new_empty((B, H, dv)), stream)
     else:
         _check(out, "out", q.dtype, (B, H, dv))
     st = lib.ll_gdn_decode_step(_ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(beta), _ptr(lam), _ptr(out),
@@ -367,7 +392,7 @@ def ll_mamba2_fwd_staged(q, k, v, log_alpha, lam, C, events, out=None, workspace
     synchronising."""
     handles, s = _event_handles(events, 4, stream)
     (B, T, H, dk, dv, code), out, ws = _prepare(LL_MAMBA2, q, k, v, log_alpha, None, lam, C, out, workspace,
-                                                grouped=True)
+                                                s, grouped=True)
     st = lib.ll_mamba2_fwd_staged(_ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(lam), _ptr(out),
                                   B, T, H, q.shape[2], dk, dv, C, code, _ptr(ws), ws.numel(), _stream(s), handles)
     if st != LL_OK:
@@ -388,9 +413,9 @@ def _bwd_call(q, k, v, log_alpha, lam, d_o, C, grads, workspace, stream, handles
     code = _dtype_code(q)
     if grads is None:
         dev = q.device
-        grads = (torch.empty_like(q), torch.empty_like(k), torch.empty_like(v),
-                 torch.empty((B, T, H), dtype=torch.float32, device=dev),
-                 torch.empty((B, T, H, L), dtype=torch.float32, device=dev))
+        grads = _results(lambda: (torch.empty_like(q), torch.empty_like(k), torch.empty_like(v),
+                                  torch.empty((B, T, H), dtype=torch.float32, device=dev),
+                                  torch.empty((B, T, H, L), dtype=torch.float32, device=dev)), stream)
     dq, dk_, dv_, dla, dlam = grads
     _check(dq, "dq", q.dtype, q.shape)
     _check(dk_, "dk", q.dtype, k.shape)
@@ -401,7 +426,7 @@ def _bwd_call(q, k, v, log_alpha, lam, d_o, C, grads, workspace, stream, handles
         if after_fwd:
             raise ValueError("ll_mamba2_bwd_after_fwd needs the workspace its forward ran in")
         need = lib.ll_mamba2_bwd_workspace_size(code, B, T, H, Hqk, dk, dv, C)
-        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+        workspace = _scratch(lambda: torch.empty(max(need, 1), dtype=torch.uint8, device=q.device), stream)
     _check(workspace, "workspace", torch.uint8)
     args = [_ptr(x) for x in (q, k, v, log_alpha, lam, d_o, dq, dk_, dv_, dla, dlam)]
     tail = [dk, dv, C, code, _ptr(workspace), workspace.numel(), _stream(stream)]
@@ -450,7 +475,7 @@ def ll_mamba2_bwd_staged(q, k, v, log_alpha, lam, d_o, C, events, grads=None, wo
 
 def ll_gdn_fwd(q, k, v, log_alpha, beta, lam, C, out=None, workspace=None, stream=None):
     """Log-linear Gated DeltaNet forward; as ll_mamba2_fwd plus `beta` [B, T, H] float32."""
-    (B, T, H, dk, dv, code), out, ws = _prepare(LL_GDN, q, k, v, log_alpha, beta, lam, C, out, workspace)
+    (B, T, H, dk, dv, code), out, ws = _prepare(LL_GDN, q, k, v, log_alpha, beta, lam, C, out, workspace, stream)
     st = lib.ll_gdn_fwd(_ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(beta), _ptr(lam), _ptr(out),
                         B, T, H, dk, dv, C, code, _ptr(ws), ws.numel(), _stream(stream))
     if st != LL_OK:
@@ -462,7 +487,7 @@ def ll_gdn_fwd_staged(q, k, v, log_alpha, beta, lam, C, events, out=None, worksp
     """As ll_gdn_fwd, recording three torch.cuda.Event objects around its two kernel stages
     (the WY kernel of pairs of chunks; block tree and read-out); see ll_mamba2_fwd_staged."""
     handles, s = _event_handles(events, 3, stream)
-    (B, T, H, dk, dv, code), out, ws = _prepare(LL_GDN, q, k, v, log_alpha, beta, lam, C, out, workspace)
+    (B, T, H, dk, dv, code), out, ws = _prepare(LL_GDN, q, k, v, log_alpha, beta, lam, C, out, workspace, s)
     st = lib.ll_gdn_fwd_staged(_ptr(q), _ptr(k), _ptr(v), _ptr(log_alpha), _ptr(beta), _ptr(lam), _ptr(out),
                                B, T, H, dk, dv, C, code, _ptr(ws), ws.numel(), _stream(s), handles)
     if st != LL_OK:
@@ -472,7 +497,7 @@ def ll_gdn_fwd_staged(q, k, v, log_alpha, beta, lam, C, events, out=None, worksp
 
 def ll_debug_level_map(T, C, stream=None):
     """The level map the kernels use, as a [T, T] int8 device tensor (-1 above the diagonal)."""
-    out = torch.empty((T, T), dtype=torch.int8, device="cuda")
+    out = _results(lambda: torch.empty((T, T), dtype=torch.int8, device="cuda"), stream)
     st = lib.ll_debug_level_map(T, C, _ptr(out), _stream(stream))
     if st != LL_OK:
         raise LLError(st)

@@ -13,8 +13,8 @@ from collections import namedtuple
 
 import torch
 
-from ._lib import (LL_OK, LLError, _check, _dtype_code, _i32, _i64, _ptr, _results, _scratch, _stream, _sz, _vp,
-                   lib)
+from ._lib import (LL_OK, LLError, _check, _dtype_code, _i32, _i64, _once, _ptr, _results, _scratch, _stream, _sz,
+                   _vp, lib)
 
 LL_ACT_NONE, LL_ACT_SILU = 0, 1
 
@@ -409,7 +409,7 @@ class _CausalConv(torch.autograd.Function):
         x, weight, bias, initial_state, lengths = ctx.saved_tensors
         d_y = x.new_zeros(x.shape) if d_y is None else d_y.contiguous()
         g = ll_causal_conv_bwd(x, weight, bias, d_y, ctx.act, initial_state, lengths, _dense(d_final))
-        return g.x, g.weight, g.bias, g.initial_state, None, None, None
+        return (*_once(g), None, None, None)
 
 
 class _SelectiveScan(torch.autograd.Function):
@@ -433,7 +433,7 @@ class _SelectiveScan(torch.autograd.Function):
         d_y = x.new_zeros(x.shape) if d_y is None else d_y.contiguous()
         g = ll_selective_scan_bwd(x, dt, A, B, C, states, d_y, D, z, dt_bias, ctx.delta_softplus, lengths,
                                   _dense(d_final), ctx.from_state)
-        return g.x, g.dt, g.A, g.B, g.C, g.D, g.z, g.dt_bias, g.initial_state, None, None, None
+        return (*_once(g), None, None, None)
 
 
 class _GroupNorm(torch.autograd.Function):
@@ -450,7 +450,7 @@ class _GroupNorm(torch.autograd.Function):
     def backward(ctx, d_y):
         x, weight, bias, gate, stats = ctx.saved_tensors
         g = ll_group_norm_bwd(x, ctx.groups, weight, bias, stats, d_y.contiguous(), gate, ctx.act)
-        return g.x, g.weight, g.bias, g.gate, None, None, None
+        return (*_once(g), None, None, None)
 
 
 def causal_conv(x, weight, bias=None, act=LL_ACT_SILU, initial_state=None, lengths=None, return_final_state=False):

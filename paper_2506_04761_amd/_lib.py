@@ -506,6 +506,27 @@ def ll_debug_level_map(T, C, stream=None):
 
 # ----------------------------------------------------------------------- autograd
 
+class _OnlyOnce(torch.autograd.Function):
+    """Identity on gradients, behind a leaf, so that differentiating them is an error."""
+
+    @staticmethod
+    def forward(ctx, leaf, *grads):
+        return grads
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("this operator has no second derivatives: its gradients cannot be differentiated")
+
+
+def _once(grads):
+    """The gradients that a backward returns.  Where it runs for a graph of itself (create_graph=True), what
+    differentiates them fails: the kernels leave no graph, and terms through them would be missing without a word."""
+    if not torch.is_grad_enabled():
+        return grads
+    tied = iter(_OnlyOnce.apply(torch.empty(0, requires_grad=True), *(g for g in grads if g is not None)))
+    return tuple(None if g is None else next(tied) for g in grads)
+
+
 def _autograd_function():
 
     class LogLinearMamba2(torch.autograd.Function):
@@ -532,7 +553,7 @@ def _autograd_function():
             # the workspace stays with ctx (freed with the graph): a second backward through the
             # same graph (retain_graph=True) reuses it as well
             grads = ll_mamba2_bwd_after_fwd(q, k, v, log_alpha, lam, d_o.contiguous(), ctx.C, ctx.ws)
-            return (*grads, None)
+            return (*_once(grads), None)
 
     return LogLinearMamba2
 

@@ -1,0 +1,32 @@
+"""The operators around a mixer at the edges of their inputs, against the float64 oracle: sequences without a token whose
+states hold NaN, axes of one token with any stride, values near the top of float32's range, arguments that are not
+tensors; and second derivatives, which none of the differentiable functions has."""
+
+import numpy as np
+import pytest
+
+from oracle import layer
+from tests.test_gpu_layer import SCAN_TOL, TOL, _device, _Draw, _lengths, _np, _ok, _scan_inputs  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def test_second_derivatives_are_refused():
+    """The gradients are no functions that can be differentiated: an expression that would need it says so, where the
+    terms through the operators would be missing from it otherwise."""
+    import torch
+    import paper_2506_04761_amd as ll
+    d = _Draw(4, "f32")
+    x, w, A, BC, n = d.f32(2, 9, 32), d.f32(32, 4), -torch.exp(d.f32(32, 8)), d.f32(2, 9, 8), d.f32(32)
+    q, la, lam = d.f32(1, 32, 1, 16), -torch.rand((1, 32, 1), device="cuda"), torch.rand((1, 32, 1, ll.ll_num_levels(32)), device="cuda")
+    for f, v in ((lambda t: ll.causal_conv(t, w), x), (lambda t: ll.selective_scan(t, x, A, BC, BC), x),
+                 (lambda t: ll.group_norm(t, 4, n), x), (lambda t: ll.log_linear_mamba2(t, q, q, la, lam, 16), q)):
+        t = v.clone().requires_grad_()
+        g, = torch.autograd.grad(f(t).sum(), t, create_graph=True)
+        plain, = torch.autograd.grad(f(t).sum(), t)
+        assert torch.equal(g, plain)
+        with pytest.raises(RuntimeError, match="second derivatives"):
+            (g * t).sum().backward()
+        g, = torch.autograd.grad(f(t).square().sum(), t, create_graph=True)
+        with pytest.raises(RuntimeError, match="second derivatives"):
+            (g * t).sum().backward()

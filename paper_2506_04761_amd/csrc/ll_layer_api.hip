@@ -7,7 +7,8 @@ namespace {
 
 constexpr int64_t kMaxTokenStride = int64_t(1) << 24;  // elements; the kernels keep offsets within a tile in 32 bits
 constexpr int64_t kMaxChannels = int64_t(1) << 24;
-constexpr int64_t kMaxSize = int64_t(1) << 40;         // tokens of a tensor
+constexpr int64_t kMaxSize = int64_t(1) << 40;         // sequences, tokens of a sequence
+constexpr int64_t kMaxElements = int64_t(1) << 44;     // of a tensor: sizes in bytes (up to 2^13 an element) fit 64 bits
 constexpr int64_t kMaxGrid = (int64_t(1) << 31) - 1;
 
 bool known_dtype(int32_t d) { return d == LL_F32 || d == LL_BF16; }
@@ -17,8 +18,8 @@ bool aligned(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p)
 // B sequences of T tokens of D channels, sizes within what the kernels index.
 ll_status check_sizes(int64_t B, int64_t T, int64_t D) {
   if (B < 1 || T < 1 || D < 1) return LL_ERR_BAD_SHAPE;
-  if (D >= kMaxChannels || B >= kMaxSize || T >= kMaxSize || B * (T >> 8 ? T >> 8 : 1) >= kMaxSize) return LL_ERR_UNSUPPORTED;
-  return LL_OK;
+  if (D >= kMaxChannels || B >= kMaxSize || T >= kMaxSize) return LL_ERR_UNSUPPORTED;
+  return T <= kMaxElements / D / B ? LL_OK : LL_ERR_UNSUPPORTED;
 }
 ll_status check_strides(int64_t batch, int64_t token) {
   if (batch < 0 || token < 0) return LL_ERR_BAD_SHAPE;

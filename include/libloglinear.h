@@ -336,6 +336,8 @@ ll_status ll_gdn_fwd_staged(const void* q, const void* k, const void* v, const f
  * States.   A call may continue a sequence from an initial state and leave the final one; both may be
  *           the same buffer (overlap otherwise is not allowed).  NULL: zeros, or not wanted.
  * Sums.     Sums over tokens are formed in an order that the sizes alone fix: no atomics.
+ * Limits.   Fewer than 2^24 channels, 2^44 elements at most, and no launch of 2^32 threads (one for each sequence
+ *           and group takes 256 of them where a norm has statistics over tokens): LL_ERR_UNSUPPORTED otherwise.
  * Arithmetic is float32 with one rounding at the end, whatever the storage dtype. */
 typedef enum { LL_ACT_NONE = 0, LL_ACT_SILU = 1 } ll_act;  /* SiLU: v / (1 + e^-v) */
 

@@ -408,6 +408,12 @@ hipError_t launch_colsum(const ColSum& p, hipStream_t st) {
   return hipGetLastError();
 }
 
+// The sums of columns hold at most 5 x 2^24 / 64 workgroups.
+bool conv_launchable(const ConvArgs& a, bool backward) {
+  const ConvDev p = conv_dev(a, backward ? kBwdRun : kFwdRun);
+  return launchable(backward ? ceil_div(p.ncv, 64) * a.B * ceil_div(p.runs, 4) : ceil_div(p.total, 256), 256);
+}
+
 hipError_t launch_conv_fwd(const ConvArgs& a, hipStream_t st) {
   const ConvDev p = conv_dev(a, kFwdRun);
   if (a.dtype == 1) go_fwd<__bf16>(p, int(a.W), st);

@@ -10,6 +10,9 @@ namespace ll {
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// A launch holds fewer than 2^32 threads.
+inline bool launchable(int64_t workgroups, int threads) { return workgroups <= int64_t(0xffffffff) / threads; }
+
 // A [B, T, D] tensor whose channels are adjacent: strides of a sequence and of a token in elements.
 struct Rows {
   const void* p = nullptr;
@@ -68,12 +71,17 @@ struct ScanJoin {
   int N, NP;
   bool reverse;
 };
+int64_t scan_join_workgroups(int64_t B, int64_t D, int64_t NP);  // of 64 threads, or at most 512 of 1024
 hipError_t launch_scan_join(const ScanJoin& p, hipStream_t st);
 int scan_state_blocks(int64_t N);            // blocks of 16 states a lane group holds: 1, 2 or 4
 constexpr int kScanChunk = 16;               // tokens between two saved states
 int64_t scan_states_bytes(int64_t B, int64_t T, int64_t D, int64_t N);
 int64_t scan_fwd_workspace(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G);
 int64_t scan_bwd_workspace(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G);
+// The *_launchable: whether each launch of a call on these sizes holds few enough threads.
+bool scan_fwd_launchable(const ScanArgs& a);
+bool scan_bwd_launchable(const ScanArgs& a);
+bool scan_step_launchable(const ScanArgs& a);
 hipError_t launch_scan_fwd(const ScanArgs& a, hipStream_t st);
 hipError_t launch_scan_bwd(const ScanArgs& a, const ScanGrads& g, hipStream_t st);
 hipError_t launch_scan_step(const ScanArgs& a, hipStream_t st);  // h0 -> h_final, one token
@@ -100,6 +108,7 @@ struct ConvGrads {
   void* workspace;
 };
 int64_t conv_bwd_workspace(int64_t B, int64_t T, int64_t D, int64_t W, int dtype);
+bool conv_launchable(const ConvArgs& a, bool backward);
 hipError_t launch_conv_fwd(const ConvArgs& a, hipStream_t st);
 hipError_t launch_conv_bwd(const ConvArgs& a, const ConvGrads& g, hipStream_t st);
 hipError_t launch_conv_step(const ConvArgs& a, hipStream_t st);
@@ -124,6 +133,7 @@ struct NormGrads {
   float* db;               // may be null
 };
 int64_t norm_workspace(int64_t N, int64_t S, int64_t C, int64_t G, int dtype, bool backward);
+bool norm_launchable(const NormArgs& a, bool backward);
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t st);
 hipError_t launch_norm_bwd(const NormArgs& a, const NormGrads& g, hipStream_t st);
 

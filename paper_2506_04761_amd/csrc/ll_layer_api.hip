@@ -9,7 +9,6 @@ constexpr int64_t kMaxTokenStride = int64_t(1) << 24;  // elements; the kernels 
 constexpr int64_t kMaxChannels = int64_t(1) << 24;
 constexpr int64_t kMaxSize = int64_t(1) << 40;         // sequences, tokens of a sequence
 constexpr int64_t kMaxElements = int64_t(1) << 44;     // of a tensor: sizes in bytes (up to 2^13 an element) fit 64 bits
-constexpr int64_t kMaxGrid = (int64_t(1) << 31) - 1;
 
 bool known_dtype(int32_t d) { return d == LL_F32 || d == LL_BF16; }
 bool known_act(int32_t a) { return a == LL_ACT_NONE || a == LL_ACT_SILU; }
@@ -45,7 +44,6 @@ ll_status conv_args(const void* x, int64_t xbs, int64_t xts, const float* weight
   LL_TRY(check_strides(xbs, xts));
   if (W < 1) return LL_ERR_BAD_SHAPE;
   if (W < 2 || W > 4 || !known_act(act) || !known_dtype(dtype)) return LL_ERR_UNSUPPORTED;
-  if (ll::ceil_div(D, 4) * ll::ceil_div(T, 4) > (kMaxGrid - 1) * 256 / B) return LL_ERR_UNSUPPORTED;
   a->x = {x, xbs, xts};
   a->weight = weight;
   a->B = B, a->T = T, a->D = D, a->W = W, a->act = act, a->dtype = dtype;
@@ -62,9 +60,6 @@ ll_status scan_args(const ll_scan_inputs* in, ll::ScanArgs* a) {
   LL_TRY(check_strides(in->C_strides[0], in->C_strides[1]));
   if (in->z) LL_TRY(check_strides(in->z_strides[0], in->z_strides[1]));
   if (in->N > ll::kScanMaxN || !known_dtype(in->dtype)) return LL_ERR_UNSUPPORTED;
-  // workgroups: one for 64 channels (of a group) and at least 64 tokens
-  const int64_t cblocks = in->groups * ll::ceil_div(in->channels / in->groups, 64);
-  if (in->batch > kMaxGrid / cblocks || ll::ceil_div(in->T, 64) > kMaxGrid / (cblocks * in->batch)) return LL_ERR_UNSUPPORTED;
   a->x = {in->x, in->x_strides[0], in->x_strides[1]};
   a->dt = {in->dt, in->dt_strides[0], in->dt_strides[1]};
   a->Bm = {in->B, in->B_strides[0], in->B_strides[1]};
@@ -90,9 +85,6 @@ ll_status norm_args(const void* x, int64_t xbs, int64_t xts, const void* gate, i
   LL_TRY(check_strides(xbs, xts));
   if (gate) LL_TRY(check_strides(gbs, gts));
   if (!known_act(act) || !known_dtype(dtype)) return LL_ERR_UNSUPPORTED;
-  // workgroups: at most one for a sequence's group, or for 8 tokens of 256 channels
-  const int64_t cblocks = ll::ceil_div(C, 256);
-  if (N > kMaxGrid / (G > cblocks ? G : cblocks) || ll::ceil_div(S, 8) > kMaxGrid / (N * cblocks)) return LL_ERR_UNSUPPORTED;
   a->x = {x, xbs, xts};
   if (gate) a->z = {gate, gbs, gts};
   a->N = N, a->S = S, a->C = C, a->G = G, a->act = act, a->dtype = dtype;
@@ -110,6 +102,7 @@ ll_status ll_causal_conv_fwd(const void* x, int64_t x_batch_stride, int64_t x_to
   ll::ConvArgs a = {};
   LL_TRY(conv_args(x, x_batch_stride, x_token_stride, weight, B, T, D, W, act, dtype, &a));
   if (!y) return LL_ERR_NULL_ARG;
+  if (!ll::conv_launchable(a, false)) return LL_ERR_UNSUPPORTED;
   a.bias = bias, a.state = initial_state, a.new_state = final_state, a.lengths = lengths, a.y = y;
   return launched(ll::launch_conv_fwd(a, static_cast<hipStream_t>(stream)));
 }
@@ -120,6 +113,7 @@ ll_status ll_causal_conv_step(const void* x, int64_t x_batch_stride, const float
   ll::ConvArgs a = {};
   LL_TRY(conv_args(x, x_batch_stride, 0, weight, B, 1, D, W, act, dtype, &a));
   if (!state || !new_state || !y) return LL_ERR_NULL_ARG;
+  if (!ll::conv_launchable(a, false)) return LL_ERR_UNSUPPORTED;
   a.bias = bias, a.state = state, a.new_state = new_state, a.y = y;
   return launched(ll::launch_conv_step(a, static_cast<hipStream_t>(stream)));
 }
@@ -137,6 +131,7 @@ ll_status ll_causal_conv_bwd(const void* x, int64_t x_batch_stride, int64_t x_to
   ll::ConvArgs a = {};
   LL_TRY(conv_args(x, x_batch_stride, x_token_stride, weight, B, T, D, W, act, dtype, &a));
   if (!d_y || !dx || !dweight) return LL_ERR_NULL_ARG;
+  if (!ll::conv_launchable(a, true)) return LL_ERR_UNSUPPORTED;
   LL_TRY(check_workspace(workspace, workspace_bytes, ll::conv_bwd_workspace(B, T, D, W, dtype)));
   a.bias = bias, a.state = initial_state, a.lengths = lengths;
   const ll::ConvGrads g = {d_y, d_final_state, dx, dweight, dbias, d_initial_state, workspace};
@@ -158,6 +153,7 @@ ll_status ll_selective_scan_fwd(const ll_scan_inputs* in, const float* initial_s
   ll::ScanArgs a = {};
   LL_TRY(scan_args(in, &a));
   if (!y) return LL_ERR_NULL_ARG;
+  if (!ll::scan_fwd_launchable(a)) return LL_ERR_UNSUPPORTED;
   LL_TRY(check_workspace(workspace, workspace_bytes, ll::scan_fwd_workspace(a.B, a.T, a.D, a.N, a.G)));
   if (!aligned(states, 16)) return LL_ERR_WORKSPACE;
   a.h0 = initial_state, a.h_final = final_state, a.states = states, a.y = y, a.workspace = workspace;
@@ -170,6 +166,7 @@ ll_status ll_selective_scan_step(const ll_scan_inputs* in, const float* state, f
   LL_TRY(scan_args(in, &a));
   if (!state || !new_state || !y) return LL_ERR_NULL_ARG;
   if (a.T != 1 || a.lengths) return LL_ERR_BAD_SHAPE;
+  if (!ll::scan_step_launchable(a)) return LL_ERR_UNSUPPORTED;
   a.h0 = state, a.h_final = new_state, a.y = y;
   return launched(ll::launch_scan_step(a, static_cast<hipStream_t>(stream)));
 }
@@ -181,6 +178,7 @@ ll_status ll_selective_scan_bwd(const ll_scan_inputs* in, const float* states, c
   ll::ScanArgs a = {};
   LL_TRY(scan_args(in, &a));
   if (!states || !d_y || !dx || !ddt || !dA || !dB || !dC || (a.z.p && !dz)) return LL_ERR_NULL_ARG;
+  if (!ll::scan_bwd_launchable(a)) return LL_ERR_UNSUPPORTED;
   LL_TRY(check_workspace(workspace, workspace_bytes, ll::scan_bwd_workspace(a.B, a.T, a.D, a.N, a.G)));
   if (!aligned(states, 16)) return LL_ERR_WORKSPACE;
   a.states = const_cast<float*>(states), a.workspace = workspace;
@@ -203,6 +201,7 @@ ll_status ll_group_norm_fwd(const void* x, int64_t x_batch_stride, int64_t x_tok
   LL_TRY(norm_args(x, x_batch_stride, x_token_stride, gate, gate_batch_stride, gate_token_stride, N, S, C, groups, act,
                    dtype, &a));
   if (!y) return LL_ERR_NULL_ARG;
+  if (!ll::norm_launchable(a, false)) return LL_ERR_UNSUPPORTED;
   LL_TRY(check_workspace(workspace, workspace_bytes, ll::norm_workspace(N, S, C, groups, dtype, false)));
   if (!aligned(stats, 8)) return LL_ERR_WORKSPACE;
   a.weight = weight, a.bias = bias, a.y = y, a.stats = stats, a.eps = eps, a.workspace = workspace;
@@ -218,6 +217,7 @@ ll_status ll_group_norm_bwd(const void* x, int64_t x_batch_stride, int64_t x_tok
   LL_TRY(norm_args(x, x_batch_stride, x_token_stride, gate, gate_batch_stride, gate_token_stride, N, S, C, groups, act,
                    dtype, &a));
   if (!stats || !d_y || !dx || (gate && !dgate)) return LL_ERR_NULL_ARG;
+  if (!ll::norm_launchable(a, true)) return LL_ERR_UNSUPPORTED;
   LL_TRY(check_workspace(workspace, workspace_bytes, ll::norm_workspace(N, S, C, groups, dtype, true)));
   if (!aligned(stats, 8)) return LL_ERR_WORKSPACE;
   a.weight = weight, a.bias = bias, a.stats = const_cast<float*>(stats), a.workspace = workspace;

@@ -757,6 +757,13 @@ int64_t norm_workspace(int64_t N, int64_t S, int64_t C, int64_t G, int dtype, bo
   return plan(N, S, C, G, dtype, backward).total;
 }
 
+// The sums of columns hold at most 2^25 / 64 workgroups.
+bool norm_launchable(const NormArgs& a, bool backward) {
+  const NormPlan q = plan(a.N, a.S, a.C, a.G, a.dtype, backward);
+  if (q.rows.LG) return launchable(q.per * q.bpr, 256 * (backward ? 4 / q.rows.PV : 1));
+  return launchable(ceil_div(q.ncv, slab_lanes(q.ncv)) * a.N * q.chunks, 256) && launchable(a.N * a.G, 256);
+}
+
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t st) { return launch(a, nullptr, st); }
 hipError_t launch_norm_bwd(const NormArgs& a, const NormGrads& g, hipStream_t st) { return launch(a, &g, st); }
 

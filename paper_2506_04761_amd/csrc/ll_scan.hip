@@ -383,8 +383,10 @@ int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
 
 }  // namespace
 
+int64_t scan_join_workgroups(int64_t B, int64_t D, int64_t NP) { return B * ceil_div(D * NP, 64); }
+
 hipError_t launch_scan_join(const ScanJoin& p, hipStream_t st) {
-  const int64_t wgs = p.B * ceil_div(p.D * p.NP, 64);
+  const int64_t wgs = scan_join_workgroups(p.B, p.D, p.NP);
   if (p.S > 16 && wgs <= 512) k_scan_join<16><<<dim3(unsigned(wgs)), 1024, 0, st>>>(p);
   else k_scan_join<1><<<dim3(unsigned(wgs)), 64, 0, st>>>(p);
   return hipGetLastError();
@@ -437,6 +439,15 @@ hipError_t run_fwd(const ScanDev& p, hipStream_t st) {
 }  // namespace
 
 int64_t scan_fwd_workspace(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) { return layout(B, T, D, N, G).total; }
+
+bool scan_fwd_launchable(const ScanArgs& a) {
+  const FwdLayout l = layout(a.B, a.T, a.D, a.N, a.G);
+  const int64_t waves = ceil_div(a.D / a.G, 64), blocks = ceil_div(waves, kWaves);
+  return launchable(a.B * a.G * blocks * l.split.S, int(64 * ceil_div(waves, blocks))) &&
+         (l.split.S == 1 || launchable(scan_join_workgroups(a.B, a.D, lane_states(a.N)), 64));
+}
+
+bool scan_step_launchable(const ScanArgs& a) { return launchable(ceil_div(a.B * a.D, 64), 256); }
 
 hipError_t launch_scan_fwd(const ScanArgs& a, hipStream_t st) {
   const FwdLayout l = layout(a.B, a.T, a.D, a.N, a.G);

@@ -536,6 +536,8 @@ BwdLayout layout(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) {
   return l;
 }
 
+int64_t bc_threads(int64_t B, int64_t G, int64_t T4, int64_t NP) { return 2 * B * G * T4 * NP * 4; }
+
 template <typename T, int NB, bool GATED>
 hipError_t go_main(const BwdDev& p, hipStream_t st) {
   if (p.F > 1) {
@@ -551,7 +553,7 @@ template <typename T, int NB>
 hipError_t go(const BwdDev& p, hipStream_t st) {
   const hipError_t e = p.z.p ? go_main<T, NB, true>(p, st) : go_main<T, NB, false>(p, st);
   if (e != hipSuccess) return e;
-  const int64_t total = 2 * int64_t(p.B) * p.G * p.T4 * NB * 64;
+  const int64_t total = bc_threads(p.B, p.G, p.T4, 16 * NB);
   k_scan_bc<T, NB><<<dim3(unsigned(ceil_div(total, 256))), 256, 0, st>>>(p, total);
   return hipGetLastError();
 }
@@ -561,6 +563,18 @@ hipError_t go(const BwdDev& p, hipStream_t st) {
 int64_t scan_bwd_workspace(int64_t B, int64_t T, int64_t D, int64_t N, int64_t G) {
   const int64_t own = layout(B, T, D, N, G).total, fwd = scan_fwd_workspace(B, T, D, N, G);
   return own > fwd ? own : fwd;  // one workspace serves both
+}
+
+bool scan_bwd_launchable(const ScanArgs& a) {
+  const BwdLayout l = layout(a.B, a.T, a.D, a.N, a.G);
+  const int64_t NP = 16 * scan_state_blocks(a.N), BG = a.B * a.G;
+  const int64_t waves = ceil_div(a.D / a.G, kWaveCh), blocks = ceil_div(waves, kWaves);
+  const int64_t rev = ceil_div(a.D / a.G, 64), rev_blocks = ceil_div(rev, kWaves);
+  return launchable(BG * blocks * l.S, int(64 * ceil_div(waves, blocks))) &&
+         launchable(BG * rev_blocks * (l.F - 1), int(64 * ceil_div(rev, rev_blocks))) &&
+         (l.F == 1 || launchable(scan_join_workgroups(a.B, a.D, NP), 64)) &&
+         launchable(ceil_div(bc_threads(a.B, a.G, l.T4, NP), 256), 256) &&
+         launchable(ceil_div(a.D * NP, 64) + 2 * ceil_div(a.D, 64), 1024);
 }
 
 hipError_t launch_scan_bwd(const ScanArgs& a, const ScanGrads& g, hipStream_t st) {

@@ -218,12 +218,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 5) void k_conv_bwd(ConvDe
         }
         g = in ? g : 0.0f;
         dv[W - 1][i] = g;  // dv[j] = dv of token t - (W - 1) + j
-        const float own_g = own ? g : 0.0f;
-        db[i] += own_g;
+        db[i] += own ? g : 0.0f;
         float a = 0.0f;
 #pragma unroll
         for (int j = 0; j < W; ++j) {
-          dw[j][i] = fmaf(own_g, e[j][i], dw[j][i]);
+          // a sequence without tokens has a part in no sum, whatever its state holds
+          dw[j][i] = own && in ? fmaf(g, e[j][i], dw[j][i]) : dw[j][i];
           a = fmaf(w[j][i], dv[W - 1 - j][i], a);
         }
         o[i] = a;

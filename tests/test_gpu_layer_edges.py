@@ -11,6 +11,22 @@ from tests.test_gpu_layer import SCAN_TOL, TOL, _device, _Draw, _lengths, _np, _
 pytestmark = pytest.mark.gpu
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,bad", [(5, float("nan")), (5, float("inf")), (70, float("nan"))])
+def test_conv_gradients_without_a_token(T, bad, dtype):
+    """A sequence of no token has a part in no sum, whatever its state holds (a slot of a cache that nothing has
+    written); its state's gradient is the final state's."""
+    import paper_2506_04761_amd as ll
+    B, D, W, ns = 3, 66, 4, [T, 0, 2]
+    d = _Draw(T, dtype)
+    x, w, b, init, dy, df = d.rows(B, T, D), d.f32(D, W), d.f32(D), d.rows(B, W - 1, D), d.rows(B, T, D), d.rows(B, W - 1, D)
+    init[1] = bad
+    g = ll.ll_causal_conv_bwd(x, w, b, dy, ll.LL_ACT_SILU, init, _lengths(ns), df)
+    want = layer.conv_grad(_np(x), _np(w), _np(dy), _np(b), True, _np(init), ns, _np(df))
+    for got, v, name in zip(g, want, ("dx", "dweight", "dbias", "dinitial")):
+        _ok(got, v, TOL[dtype] if got.dtype == x.dtype else TOL["f32"], name)
+
+
 def test_second_derivatives_are_refused():
     """The gradients are no functions that can be differentiated: an expression that would need it says so, where the
     terms through the operators would be missing from it otherwise."""

@@ -471,7 +471,8 @@ __global__ __launch_bounds__(256, 2) void k_scan_bwd(BwdDev p) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int n = nb * 16 + 4 * r + i;
-          row[ch * NP + n] = dA[k][nb][i];
+          // where no token was, a state or gradient that is not finite has left its product with zero
+          row[ch * NP + n] = end > t_begin ? dA[k][nb][i] : 0.0f;
           if (seg == 0 && p.dh0 && n < p.N) p.dh0[(int64_t(b) * p.D + ch) * p.N + n] = g[k][nb][i];
         }
     }

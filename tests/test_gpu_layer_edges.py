@@ -27,6 +27,28 @@ def test_conv_gradients_without_a_token(T, bad, dtype):
         _ok(got, v, TOL[dtype] if got.dtype == x.dtype else TOL["f32"], name)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N", [(5, 16), (70, 7), (70, 40)])
+def test_scan_gradients_without_a_token(T, N, dtype):
+    """As above, with NaN in the state, in the final state's gradient, or in both."""
+    import paper_2506_04761_amd as ll
+    B, D, ns = 4, 36, [T, 0, 0, 0]
+    d = _Draw(T + N, dtype)
+    x, dt, z, Bm, Cm, A, skip, bias, init = _scan_inputs(d, B, T, D, N, 1, None)
+    dy, df = d.rows(B, T, D), d.f32(B, D, N)
+    init[1] = init[3] = float("nan")
+    df[2] = df[3] = float("nan")
+    states = ll.ll_selective_scan_states(x, Bm)
+    ll.ll_selective_scan_fwd(x, dt, A, Bm, Cm, skip, z, bias, True, init, None, _lengths(ns), states)
+    g = ll.ll_selective_scan_bwd(x, dt, A, Bm, Cm, states, dy, skip, z, bias, True, _lengths(ns), df, True)
+    want = layer.scan_grad(_np(x), _np(dt), _np(A), _np(Bm)[:, :, None], _np(Cm)[:, :, None], _np(dy), _np(skip), _np(z),
+                           _np(bias), True, _np(init), ns, _np(df))
+    for name, got in zip(("x", "dt", "A", "B", "C", "D", "z", "dt_bias"), g):
+        _ok(got, want[name].reshape(got.shape), SCAN_TOL[dtype] if got.dtype == x.dtype else SCAN_TOL["f32"], "d" + name)
+    assert np.array_equal(_np(g.initial_state)[1:], _np(df)[1:], equal_nan=True)
+    _ok(g.initial_state[0], want["initial"][0], SCAN_TOL["f32"], "dinitial")
+
+
 def test_second_derivatives_are_refused():
     """The gradients are no functions that can be differentiated: an expression that would need it says so, where the
     terms through the operators would be missing from it otherwise."""

@@ -69,6 +69,11 @@ def _rows(t, name, dtype, shape):
     return strides
 
 
+def _token_stride(t):
+    """The stride of a token of [B, T, channels]; that of an only token is whatever the tensor came by, and not used."""
+    return t.stride(1) if t.shape[1] != 1 else 0
+
+
 def _opt(t, name, dtype, shape):
     if t is not None:
         _check(t, name, dtype, shape)
@@ -122,7 +127,7 @@ def ll_causal_conv_fwd(x, weight, bias=None, act=LL_ACT_SILU, initial_state=None
         out = _results(lambda: x.new_empty((B, T, D)), stream)
     else:
         _check(out, "out", x.dtype, (B, T, D))
-    _ok(lib.ll_causal_conv_fwd(x.data_ptr(), x.stride(0), x.stride(1), weight.data_ptr(), _ptr(bias),
+    _ok(lib.ll_causal_conv_fwd(x.data_ptr(), x.stride(0), _token_stride(x), weight.data_ptr(), _ptr(bias),
                                _ptr(initial_state), _ptr(final_state), _ptr(lengths), out.data_ptr(), B, T, D, W,
                                act, code, _stream(stream)))
     return out
@@ -179,7 +184,7 @@ def ll_causal_conv_bwd(x, weight, bias, d_y, act=LL_ACT_SILU, initial_state=None
     _opt(db, "grads.bias", torch.float32, (D,))
     _opt(di, "grads.initial_state", x.dtype, (B, W - 1, D))
     ws = _sized(workspace, lambda: lib.ll_causal_conv_bwd_workspace_size(code, B, T, D, W), x.device, stream)
-    _ok(lib.ll_causal_conv_bwd(x.data_ptr(), x.stride(0), x.stride(1), weight.data_ptr(), _ptr(bias),
+    _ok(lib.ll_causal_conv_bwd(x.data_ptr(), x.stride(0), _token_stride(x), weight.data_ptr(), _ptr(bias),
                                _ptr(initial_state), _ptr(lengths), d_y.data_ptr(), _ptr(d_final_state),
                                dx.data_ptr(), dw.data_ptr(), _ptr(db), _ptr(di), B, T, D, W, act, code,
                                _ptr(ws), ws.numel(), _stream(stream)))
@@ -210,6 +215,8 @@ def _scan_inputs(x, dt, A, Bm, Cm, D, z, dt_bias, delta_softplus, lengths, step)
     if lengths is not None:
         _lengths(lengths, nb)
     T = 1 if step else lead[1]
+    if T == 1 and not step:  # see _token_stride
+        xs, ds, zs, bs, cs = ((v[0], 0) for v in (xs, ds, zs, bs, cs))
     return _ScanInputs(x.data_ptr(), dt.data_ptr(), _ptr(z), Bm.data_ptr(), Cm.data_ptr(), xs[0], xs[1], ds[0], ds[1],
                        zs[0], zs[1], bs[0], bs[1], cs[0], cs[1], A.data_ptr(), _ptr(D), _ptr(dt_bias), _ptr(lengths), nb,
                        T, ch, N, groups, 1 if delta_softplus else 0, _dtype_code(x))
@@ -318,8 +325,8 @@ def _norm_args(x, groups, weight, bias, gate):
         _rows(gate, "gate", x.dtype, x.shape)
     _opt(weight, "weight", torch.float32, (C,))
     _opt(bias, "bias", torch.float32, (C,))
-    rows = (x.data_ptr(), x.stride(0), x.stride(1))
-    return rows + ((None, 0, 0) if gate is None else (gate.data_ptr(), gate.stride(0), gate.stride(1)))
+    rows = (x.data_ptr(), x.stride(0), _token_stride(x))
+    return rows + ((None, 0, 0) if gate is None else (gate.data_ptr(), gate.stride(0), _token_stride(gate)))
 
 
 def _norm_need(x, groups, backward):

@@ -49,6 +49,34 @@ def test_scan_gradients_without_a_token(T, N, dtype):
     _ok(g.initial_state[0], want["initial"][0], SCAN_TOL["f32"], "dinitial")
 
 
+def test_axes_of_one_token_have_any_stride():
+    """[T, 1, D] of the rows of one long sequence, turned: the stride of its single token is the sequence's size, which
+    is beyond what a token stride may be."""
+    import torch
+    import paper_2506_04761_amd as ll
+    R, D, N = 8200, 2048, 4
+    d = _Draw(2, "bf16")
+    x = torch.randn((1, R, D), device="cuda", generator=torch.Generator("cuda").manual_seed(1)).bfloat16().transpose(0, 1)
+    assert x.shape == (R, 1, D) and x.stride(1) >= 1 << 24
+    dense = x.clone(memory_format=torch.contiguous_format)
+    assert dense.stride(1) == D
+    w, A, bias = d.f32(D, 4), -torch.exp(d.f32(D, N)), d.f32(D)
+    BC = torch.randn((1, R, (1 << 24) // R + N + 1), device="cuda").bfloat16().transpose(0, 1)[..., :N]
+    assert BC.stride(1) >= 1 << 24
+    stats = ll.ll_group_norm_stats(x, 16)
+    results = []
+    for t, bc in ((x, BC), (dense, BC.clone(memory_format=torch.contiguous_format))):
+        states = ll.ll_selective_scan_states(t, bc)
+        out = [ll.ll_group_norm_fwd(t, 16, gate=t, stats=stats), ll.ll_causal_conv_fwd(t, w),
+               ll.ll_selective_scan_fwd(t, t, A, bc, bc, bias, t, states=states)]
+        out += ll.ll_group_norm_bwd(t, 16, bias, None, stats, dense, gate=t)
+        out += ll.ll_causal_conv_bwd(t, w, None, dense)
+        out += ll.ll_selective_scan_bwd(t, t, A, bc, bc, states, dense, bias, t)
+        results.append([o for o in out if o is not None])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
 def test_second_derivatives_are_refused():
     """The gradients are no functions that can be differentiated: an expression that would need it says so, where the
     terms through the operators would be missing from it otherwise."""

@@ -311,13 +311,14 @@ __global__ __launch_bounds__(256 * kBwdStrips<PV>) void k_norm_rows_bwd(NormDev 
 
 // ---- statistics over tokens
 
-// Merges (n2, mean2, M2_2) into (n1, mean1, M2_1): counts, means and centred sums of squares.
+// Merges (n2, mean2, M2_2) into (n1, mean1, M2_1): counts, means and centred sums of squares.  The square of the means'
+// difference is not formed by itself: beside nothing (n1 = 0) it is that of a mean, which may be beyond float32.
 __device__ inline void merge(float& n1, float& m1, float& q1, float n2, float m2, float q2) {
   const float n = n1 + n2, d = m2 - m1;
   if (n2 == 0.0f) return;
   const float f = n2 / n;
   m1 = fmaf(d, f, m1);
-  q1 += q2 + d * d * n1 * f;
+  q1 += q2 + (d * n1) * (d * f);
   n1 = n;
 }
 

@@ -77,6 +77,17 @@ def test_axes_of_one_token_have_any_stride():
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("S", [1, 40])
+def test_norm_of_large_values(S):
+    """Means whose square is beyond float32, with a spread whose square is not.  A mean is off by a few roundings of
+    2^-24 of 300 spreads, 2e-5 each."""
+    import paper_2506_04761_amd as ll
+    d = _Draw(S, "f32")
+    x = d.rows(3, S, 64, scale=1e17) + 3e19
+    y = ll.ll_group_norm_fwd(x, 8, act=ll.LL_ACT_NONE)
+    _ok(y, layer.norm(_np(x), 8, silu=False), 1e-4, "y")
+
+
 def test_second_derivatives_are_refused():
     """The gradients are no functions that can be differentiated: an expression that would need it says so, where the
     terms through the operators would be missing from it otherwise."""

@@ -157,7 +157,8 @@ def ll_causal_conv_step(x, weight, bias, state, act=LL_ACT_SILU, new_state=None,
 def ll_causal_conv_bwd_workspace(x, weight):
     """A workspace for ll_causal_conv_bwd of x [B, T, D] with weight [D, W]."""
     B, T, D = _dims(x, "x", 3)
-    return _buffer(lib.ll_causal_conv_bwd_workspace_size(_dtype_code(x), B, T, D, weight.shape[1]), x.device)
+    W = _dims(weight, "weight", 2)[1]
+    return _buffer(lib.ll_causal_conv_bwd_workspace_size(_dtype_code(x), B, T, D, W), x.device)
 
 
 def ll_causal_conv_bwd(x, weight, bias, d_y, act=LL_ACT_SILU, initial_state=None, lengths=None, d_final_state=None,
@@ -193,6 +194,13 @@ def ll_causal_conv_bwd(x, weight, bias, d_y, act=LL_ACT_SILU, initial_state=None
 
 # ------------------------------------------------------------------------------------ selective scan
 
+def _groups(t, name, n):
+    """The groups of B or C: [.., N], of `n` axes, for one, [.., groups, N] for several."""
+    if not isinstance(t, torch.Tensor) or not n <= t.dim() <= n + 1:
+        raise ValueError(f"{name} must be a tensor of {n} axes, or of {n + 1} with groups")
+    return 1 if t.dim() == n else t.shape[-2]
+
+
 def _scan_inputs(x, dt, A, Bm, Cm, D, z, dt_bias, delta_softplus, lengths, step):
     """The checked inputs of a scan call.  With `step`, tensors of one token ([B, ...])."""
     lead = _dims(x, "x", 2 if step else 3)
@@ -202,8 +210,7 @@ def _scan_inputs(x, dt, A, Bm, Cm, D, z, dt_bias, delta_softplus, lengths, step)
     xs, ds = _rows(x, "x", dtype, lead), _rows(dt, "dt", dtype, lead)
     zs = (0, 0, 1) if z is None else _rows(z, "z", dtype, lead)
     _check(A, "A", torch.float32, (ch, N))
-    # [.., N] for one group, [.., groups, N] for several
-    groups = 1 if Bm.dim() == len(lead) else Bm.shape[-2]
+    groups = _groups(Bm, "B", len(lead))
     shape = (*lead[:-1], N) if Bm.dim() == len(lead) else (*lead[:-1], groups, N)
     bs, cs = _rows(Bm, "B", dtype, shape), _rows(Cm, "C", dtype, shape)
     if groups > 1 and (bs[-2] != N or cs[-2] != N):
@@ -225,14 +232,14 @@ def _scan_inputs(x, dt, A, Bm, Cm, D, z, dt_bias, delta_softplus, lengths, step)
 def ll_selective_scan_workspace(x, B, backward=False):
     """A workspace for the forward (or backward) scan of x [B, T, D] with B [B, T, N] or [B, T, groups, N]."""
     nb, T, ch = _dims(x, "x", 3)
-    groups = B.shape[2] if B.dim() == 4 else 1
-    need = lib.ll_selective_scan_workspace_size(nb, T, ch, B.shape[-1], groups, int(backward))
+    need = lib.ll_selective_scan_workspace_size(nb, T, ch, B.shape[-1], _groups(B, "B", 3), int(backward))
     return _buffer(need, x.device)
 
 
 def ll_selective_scan_states(x, B):
     """The buffer in which a forward scan of x [B, T, D] leaves its states for the backward."""
     nb, T, ch = _dims(x, "x", 3)
+    _groups(B, "B", 3)
     return _buffer(lib.ll_selective_scan_states_bytes(nb, T, ch, B.shape[-1]), x.device)
 
 
@@ -422,8 +429,9 @@ class _CausalConv(torch.autograd.Function):
 class _SelectiveScan(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, dt, A, B, C, D, z, dt_bias, initial_state, lengths, delta_softplus, want_state):
+        _groups(B, "B", 3), _groups(C, "C", 3)
         x, dt, z, B, C = (_channels_last(t) for t in (x, dt, z, B, C))
-        if B.dim() == 4:  # groups of a token adjacent
+        if B.dim() == C.dim() == 4:  # groups of a token adjacent
             B, C = (t if t.stride(2) == t.shape[3] else t.contiguous() for t in (B, C))
         A, D, dt_bias, initial_state = (_dense(t) for t in (A, D, dt_bias, initial_state))
         final = A.new_empty((x.shape[0], *A.shape)) if want_state else None

@@ -88,6 +88,28 @@ def test_norm_of_large_values(S):
     _ok(y, layer.norm(_np(x), 8, silu=False), 1e-4, "y")
 
 
+def test_scan_refuses_what_are_no_tensors_of_its_axes():
+    import torch
+    import paper_2506_04761_amd as ll
+    x, A, BC = torch.zeros((2, 8, 64), device="cuda"), torch.zeros((64, 16), device="cuda"), torch.zeros((2, 8, 16), device="cuda")
+    states = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
+    for b, c in ((None, BC), (BC, None), (BC[0, 0], BC), (BC, BC[0, 0]), (3.0, BC), (BC[0], BC[0]), (BC[:, :, None], BC)):
+        with pytest.raises((TypeError, ValueError)):
+            ll.ll_selective_scan_fwd(x, x, A, b, c)
+        with pytest.raises((TypeError, ValueError)):
+            ll.ll_selective_scan_bwd(x, x, A, b, c, states, x)
+        with pytest.raises((TypeError, ValueError)):
+            ll.selective_scan(x, x, A, b, c)
+    for b in (None, BC[0, 0], 3.0, BC[0]):
+        with pytest.raises((TypeError, ValueError)):
+            ll.ll_selective_scan_workspace(x, b)
+        with pytest.raises((TypeError, ValueError)):
+            ll.ll_selective_scan_states(x, b)
+    for w in (None, A[0], 3.0):
+        with pytest.raises((TypeError, ValueError)):
+            ll.ll_causal_conv_bwd_workspace(x, w)
+
+
 def test_second_derivatives_are_refused():
     """The gradients are no functions that can be differentiated: an expression that would need it says so, where the
     terms through the operators would be missing from it otherwise."""

@@ -232,7 +232,8 @@ def _scan_inputs(x, dt, A, Bm, Cm, D, z, dt_bias, delta_softplus, lengths, step)
 def ll_selective_scan_workspace(x, B, backward=False):
     """A workspace for the forward (or backward) scan of x [B, T, D] with B [B, T, N] or [B, T, groups, N]."""
     nb, T, ch = _dims(x, "x", 3)
-    need = lib.ll_selective_scan_workspace_size(nb, T, ch, B.shape[-1], _groups(B, "B", 3), int(backward))
+    groups = _groups(B, "B", 3)
+    need = lib.ll_selective_scan_workspace_size(nb, T, ch, B.shape[-1], groups, int(backward))
     return _buffer(need, x.device)
 
 

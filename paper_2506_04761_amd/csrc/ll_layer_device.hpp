@@ -117,7 +117,8 @@ __device__ inline float row_bcast(float v) {
 // One token of a backward scan for four states: g_i += c_i dy, then sum_i b_i g_i and, with H, sum_i c_i h_i, where
 // b_i and c_i are lane M + i of each row of `b` and `c`: DPP operands, in multiply-adds that the compiler does not form
 // by itself.  A register needs two wait states between its write and its use as a DPP operand; the compiler does not
-// see into the block, so it waits itself.
+// see into the block, so it waits itself.  Every g_i is written before the last input is read (early clobber): an input of
+the same value needs a register of its own.
 template <int M, bool H>
 __device__ inline void grad_token(float* g, float b, float c, float dy, const float* h, float& bg, float& ch) {
 #define LL_DPP(op, d, s, v, m) op " " d ", " s ", " v " row_newbcast:" m " row_mask:0xf bank_mask:0xf\n\t"
@@ -129,7 +130,7 @@ __device__ inline void grad_token(float* g, float b, float c, float dy, const fl
         LL_DPP("v_fmac_f32_dpp", "%5", "%7", "%10", "%14") LL_DPP("v_fmac_f32_dpp", "%4", "%6", "%1", "%14")
         LL_DPP("v_fmac_f32_dpp", "%5", "%7", "%11", "%15") LL_DPP("v_fmac_f32_dpp", "%4", "%6", "%2", "%15")
         LL_DPP("v_fmac_f32_dpp", "%5", "%7", "%12", "%16") LL_DPP("v_fmac_f32_dpp", "%4", "%6", "%3", "%16")
-        : "+v"(g[0]), "+v"(g[1]), "+v"(g[2]), "+v"(g[3]), "=&v"(bg), "=&v"(ch)
+        : "+&v"(g[0]), "+&v"(g[1]), "+&v"(g[2]), "+&v"(g[3]), "=&v"(bg), "=&v"(ch)
         : "v"(b), "v"(c), "v"(dy), "v"(h[0]), "v"(h[1]), "v"(h[2]), "v"(h[3]), "n"(M), "n"(M + 1), "n"(M + 2), "n"(M + 3));
   } else {
     asm("s_nop 1\n\t"
@@ -137,7 +138,7 @@ __device__ inline void grad_token(float* g, float b, float c, float dy, const fl
         LL_DPP("v_fmac_f32_dpp", "%2", "%6", "%7", "%10") LL_DPP("v_fmac_f32_dpp", "%3", "%6", "%7", "%11")
         LL_DPP("v_mul_f32_dpp", "%4", "%5", "%0", "%8") LL_DPP("v_fmac_f32_dpp", "%4", "%5", "%1", "%9")
         LL_DPP("v_fmac_f32_dpp", "%4", "%5", "%2", "%10") LL_DPP("v_fmac_f32_dpp", "%4", "%5", "%3", "%11")
-        : "+v"(g[0]), "+v"(g[1]), "+v"(g[2]), "+v"(g[3]), "=&v"(bg)
+        : "+&v"(g[0]), "+&v"(g[1]), "+&v"(g[2]), "+&v"(g[3]), "=&v"(bg)
         : "v"(b), "v"(c), "v"(dy), "n"(M), "n"(M + 1), "n"(M + 2), "n"(M + 3));
     ch = 0.0f;
   }

@@ -118,7 +118,7 @@ __device__ inline float row_bcast(float v) {
 // b_i and c_i are lane M + i of each row of `b` and `c`: DPP operands, in multiply-adds that the compiler does not form
 // by itself.  A register needs two wait states between its write and its use as a DPP operand; the compiler does not
 // see into the block, so it waits itself.  Every g_i is written before the last input is read (early clobber): an input of
-the same value needs a register of its own.
+// the same value needs a register of its own.
 template <int M, bool H>
 __device__ inline void grad_token(float* g, float b, float c, float dy, const float* h, float& bg, float& ch) {
 #define LL_DPP(op, d, s, v, m) op " " d ", " s ", " v " row_newbcast:" m " row_mask:0xf bank_mask:0xf\n\t"

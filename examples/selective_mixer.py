@@ -53,10 +53,15 @@ class SelectiveMixer(nn.Module):
 
     def forward(self, h, lengths=None, cache=None):
         """h [B, T, d_model]; `lengths` int32 [B] for sequences that end early.  With a cache (see new_cache) the
-        sequences continue it, and it is brought up to their ends."""
+        sequences continue it, and it is brought up to their ends; gradients end at it."""
         x, z = self.into(h).chunk(2, -1)
         if cache is None:
             u = ll.causal_conv(x, self.conv_weight, self.conv_bias, lengths=lengths)
+        elif torch.is_grad_enabled():
+            # the backward reads the states that it started from, which the cache does not keep
+            u, end = ll.causal_conv(x, self.conv_weight, self.conv_bias, initial_state=cache["conv"].clone(),
+                                    lengths=lengths, return_final_state=True)
+            cache["conv"].copy_(end.detach())
         else:
             u = ll.ll_causal_conv_fwd(x, self.conv_weight, self.conv_bias, initial_state=cache["conv"],
                                       final_state=cache["conv"], lengths=lengths)
@@ -64,6 +69,9 @@ class SelectiveMixer(nn.Module):
         a = (u, dt, -torch.exp(self.log_rate), B, C, self.skip, z, self.dt_bias)
         if cache is None:
             y = ll.selective_scan(*a, lengths=lengths)
+        elif torch.is_grad_enabled():
+            y, end = ll.selective_scan(*a, initial_state=cache["scan"].clone(), lengths=lengths, return_final_state=True)
+            cache["scan"].copy_(end.detach())
         else:
             y = ll.ll_selective_scan_fwd(*a, initial_state=cache["scan"], final_state=cache["scan"], lengths=lengths)
         return self._normed(y)

@@ -623,21 +623,22 @@ void go_rows_bwd(const NormDev& p, unsigned grid, hipStream_t st) {
   else k_norm_rows_bwd<T, V, LG, PV, false><<<grid, 256 * kBwdStrips<PV>, 0, st>>>(p);
 }
 
-// The half vectors are the backward's, which takes whole ones only for groups that fit no other way.
+// The half vectors are the backward's, which takes whole ones only for groups that fit no other way.  A lane has one
+// vector below 64 lanes, one, two or four at 64, two or four at 256.
 template <typename T, int V, int LG>
 void go_rows(const NormDev& p, int PV, unsigned grid, bool bwd, hipStream_t st) {
   constexpr bool kHalf = V * sizeof(T) == 8;
-  constexpr int P2 = LG >= 64 ? 2 : 1, P4 = LG >= 64 ? 4 : 1;
+  constexpr int P1 = LG == 256 ? 2 : 1, P2 = LG >= 64 ? 2 : 1, P4 = LG >= 64 ? 4 : 1;
   if (!bwd) {
     if constexpr (!kHalf) {
-      if (PV == 1) k_norm_rows<T, V, LG, 1><<<grid, 256, 0, st>>>(p);
+      if (PV == 1) k_norm_rows<T, V, LG, P1><<<grid, 256, 0, st>>>(p);
       else if (PV == 2) k_norm_rows<T, V, LG, P2><<<grid, 256, 0, st>>>(p);
       else k_norm_rows<T, V, LG, P4><<<grid, 256, 0, st>>>(p);
     }
   } else if constexpr (!kHalf) {
     if constexpr (LG == 256) go_rows_bwd<T, V, LG, kMaxPV>(p, grid, st);
   } else {
-    if (PV == 1) go_rows_bwd<T, V, LG, 1>(p, grid, st);
+    if (PV == 1) go_rows_bwd<T, V, LG, P1>(p, grid, st);
     else if (PV == 2) go_rows_bwd<T, V, LG, P2>(p, grid, st);
     else go_rows_bwd<T, V, LG, P4>(p, grid, st);
   }

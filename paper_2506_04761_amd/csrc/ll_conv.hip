@@ -189,7 +189,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 5) void k_conv_bwd(ConvDe
     load_taps<W, V>(p, d0, n, w, bias);
 #pragma unroll
     for (int j = 0; j < W; ++j) {
-      if (j > 0) token<T, W, V>(p, b, t0 - W + j, live, d0, n, e[j]);
+      // a sequence without tokens has a part in no sum, whatever its state holds
+      if (j > 0) token<T, W, V>(p, b, t0 - W + j, live, d0, live > 0 ? n : 0, e[j]);
 #pragma unroll
       for (int i = 0; i < V; ++i) dv[j][i] = 0.0f;
     }
@@ -218,12 +219,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 5) void k_conv_bwd(ConvDe
         }
         g = in ? g : 0.0f;
         dv[W - 1][i] = g;  // dv[j] = dv of token t - (W - 1) + j
-        db[i] += own ? g : 0.0f;
+        const float own_g = own ? g : 0.0f;
+        db[i] += own_g;
         float a = 0.0f;
 #pragma unroll
         for (int j = 0; j < W; ++j) {
-          // a sequence without tokens has a part in no sum, whatever its state holds
-          dw[j][i] = own && in ? fmaf(g, e[j][i], dw[j][i]) : dw[j][i];
+          dw[j][i] = fmaf(own_g, e[j][i], dw[j][i]);
           a = fmaf(w[j][i], dv[W - 1 - j][i], a);
         }
         o[i] = a;

@@ -1,6 +1,6 @@
 """ctypes binding of the operators around a token mixer (include/libloglinear.h): the short causal
 convolution, the selective state space scan and the group norm, with their backward passes and their forms
-for one token; and the three as differentiable functions.
+for one token; and the three as functions that can be differentiated once.
 
 As in the rest of the binding, the wrappers check and pass arguments and every step of the computation runs
 in the library's HIP kernels.  x, dt, z, gate, B and C may be columns of wider rows (channels adjacent);

@@ -6,7 +6,9 @@
 // registers, so that a token is read again only by the run after it.  16 bytes to a lane took 76 us where 8 take 60
 // (the taps alone are then 32 registers).  bf16, W = 4: 32768 tokens of 2048 channels 51 us, 5.2 TB/s, the rate of a
 // copy; forward of 8064 tokens 18 us (3.7 TB/s: a single round of waves), backward 29 us (3.4 TB/s).  One token for 64
-// sequences 3.5 us, a launch's latency.
+// sequences 3.5 us, a launch's latency.  float32, 32768 tokens of 2048 channels 110 us, 4.9 TB/s.  Channels that are not
+// whole vectors: 118 us for 2047 in bf16, 142 in float32, where each of the forward's loads and stores goes through the
+// test for a short vector as well.
 #include "ll_layer.hpp"
 #include "ll_layer_device.hpp"
 
@@ -162,7 +164,8 @@ __global__ __launch_bounds__(256) void k_conv_step(ConvDev p) {
 // Backward: dv_t = dy_t act'(v_t), dx_s = sum_j w_j dv_(s+W-1-j), dw_j = sum_t dv_t e_(t+j), db = sum_t dv_t.
 // A lane walks its run and the W - 1 tokens after it (whose dv reach back into the run) and keeps the run's
 // sums; the workgroup's four runs are added in LDS, and k_colsum adds the workgroups (4.7 us of 8064 tokens' 33).
-// Registers (126 of the 128 that four waves a SIMD leave): taps, their sums, W tokens of x and of dv, loads ahead.
+// Registers (126 of the 128 that four waves a SIMD leave, and for bf16 with W = 4 four in scratch): taps, their sums, W
+// tokens of x and of dv, loads ahead.
 template <typename T, int W>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 5) void k_conv_bwd(ConvDev p) {
   constexpr int V = kVecBytes / sizeof(T);

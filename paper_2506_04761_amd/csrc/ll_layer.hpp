@@ -56,7 +56,8 @@ struct ScanGrads {
 
 constexpr int kScanMaxN = 64;
 
-// How a scan is split over its length: S segments of `len` tokens (a multiple of the states' chunk).
+// How a scan is split over its length: S segments of `len` tokens (a multiple of 4: one of fewer than 16 may hold no
+// saved state).
 struct ScanSplit {
   int64_t S = 1, len = 0;
 };

@@ -9,8 +9,10 @@
 //   rows  (S = 1, the norm of every token by itself): a group's values stay in the registers of up to 64
 //         lanes, or of a workgroup, between the statistics and the output; one pass over the data.
 //   slab  (statistics over tokens too): partial statistics of runs of tokens, their combination, and a
-//         second pass (a sequence's rows do not fit on a compute unit).  Partial statistics are means and
-//         centred sums of squares, merged pairwise, so that a large mean costs no precision.
+//         second pass (a sequence's rows do not fit on a compute unit; short ones, which would, go the same way).
+//         Partial statistics are means and centred sums of squares, merged pairwise, so that a large mean costs no
+//         precision.  One workgroup to a sequence and group combines them, so that few groups in all take long: one
+//         sequence of 65536 tokens of 1024 bf16 channels in one group 313 us, its training step 2112 us.
 #include "ll_layer.hpp"
 #include "ll_layer_device.hpp"
 

@@ -18,10 +18,13 @@
 // the tiles are taken last to first, forming rates and states again in registers.  The waves of a workgroup are added
 // in LDS, workgroups by k_scan_bc.
 //
-// Bound by the vector ALU: two waves a SIMD (256 registers: rates, states and gradients of 4 tokens x 2 blocks, the
-// sums over channels), about 3200 instructions per 16 tokens x 32 channels x 16 states, the ALU busy 81 % of the time.
+// Bound by the vector ALU: two waves a SIMD up to 16 states (256 registers: rates, states and gradients of 4 tokens x 2
+// blocks, the sums over channels; the gated float32 instance has 17 more in scratch), one beyond (registers, and 101 and
+// 109 KiB of LDS), about 3200 instructions per 16 tokens x 32 channels x 16 states, the ALU busy 81 % of the time.
 // bf16, 2 x 4032 tokens of 2048 channels, 16 states: k_scan_bwd 250 us, k_scan_rev 69, the join 10, k_scan_bc 6.5, the
 // parameters' sums 5.  One block of 16 channels instead of two, at three and four waves a SIMD: 291 and 383 us.
+// A training step of those tokens, forward and backward: 8 states 433 us, 16 466, 24 875, 32 932, 64 1963 (8 and 24 work
+// as 16 and 32 here).
 #include "ll_layer.hpp"
 #include "ll_layer_device.hpp"
 
@@ -508,7 +511,8 @@ __global__ __launch_bounds__(256) void k_scan_bc(BwdDev p, int64_t total) {
 int elem(int dtype) { return dtype == 1 ? 2 : 4; }
 int64_t align256(int64_t v) { return (v + 255) / 256 * 256; }
 
-// Segments: two workgroups of k_scan_bwd on every compute unit; split further for k_scan_rev, to four waves on
+// Segments: two workgroups of k_scan_bwd on every compute unit (beyond 16 states one is resident: they take two
+// rounds); split further for k_scan_rev, to four waves on
 // every SIMD.
 struct BwdLayout {
   int64_t S, len, F, flen, R, T4, seg_g, seg_d, bc, part, total;

@@ -51,9 +51,12 @@ def _norm(N, S, C, G, dtype=1):
 
 
 def _conv(B, T, D, dtype=1):
-    a = (B, T, D, 4, 1, dtype)
-    return (lib.ll_causal_conv_fwd(FAKE, 64, 8, FAKE, None, None, None, None, FAKE, *a, None),
-            lib.ll_causal_conv_bwd(FAKE, 64, 8, FAKE, None, None, None, FAKE, None, FAKE, FAKE, None, None, *a, FAKE, BIG, None))
+    return lib.ll_causal_conv_fwd(FAKE, 64, 8, FAKE, None, None, None, None, FAKE, B, T, D, 4, 1, dtype, None)
+
+
+def _conv_bwd(B, T, D, dtype=1):
+    return lib.ll_causal_conv_bwd(FAKE, 64, 8, FAKE, None, None, None, FAKE, None, FAKE, FAKE, None, None, B, T, D, 4, 1,
+                                  dtype, FAKE, BIG, None)
 
 
 def test_launches_of_too_many_threads_are_refused():
@@ -62,9 +65,10 @@ def test_launches_of_too_many_threads_are_refused():
     # a workgroup of 256 to a sequence and group
     assert _norm(1 << 20, 2, 64, 16) == (UNSUPPORTED,) * 2 and _norm(1 << 24, 3, 8, 1, dtype=0) == (UNSUPPORTED,) * 2
     # a thread to a run and channel vector
-    assert _conv(1 << 32, 1, 1) == (UNSUPPORTED,) * 2 and _conv(1 << 20, 1, (1 << 24) - 1, dtype=0)[0] == UNSUPPORTED
-    # workgroups of the backward to a sequence, of which each has only a channel
-    assert _conv(1 << 24, 4, 1)[1] == UNSUPPORTED
+    assert _conv(1 << 32, 1, 1) == UNSUPPORTED and _conv(1 << 20, 1, (1 << 24) - 1, dtype=0) == UNSUPPORTED
+    assert _conv_bwd(1 << 32, 1, 1) == UNSUPPORTED
+    # a workgroup of the backward to a sequence, of which each has only a channel (the forward would take these)
+    assert _conv_bwd(1 << 24, 4, 1) == UNSUPPORTED
     # sequences of one token
     assert lib.ll_causal_conv_step(FAKE, 8, FAKE, None, FAKE, FAKE, FAKE, 1 << 30, 64, 4, 1, 1, None) == UNSUPPORTED
     assert lib.ll_selective_scan_step(_scan_inputs(1 << 24, 1, 64, 16, 1), FAKE, FAKE, FAKE, None) == UNSUPPORTED

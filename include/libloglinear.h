@@ -431,6 +431,34 @@ ll_status ll_group_norm_bwd(const void* x, int64_t x_batch_stride, int64_t x_tok
                             int64_t C, int64_t groups, int32_t act, int32_t dtype, void* workspace,
                             size_t workspace_bytes, void* stream);
 
+/* ---- Projections ------------------------------------------------------------------------------
+ *
+ * Matrix products in front of and behind a mixer, with what follows them:
+ *   u = x W^T + bias,   y = act(u) + residual.
+ * x [M, K] and residual [M, N] (NULL: none) may be columns of wider rows: each comes with the stride of a
+ * row in elements, >= 0 and below 2^24.  W [N, K], y [M, N] and the gradients are dense.  x, W, residual, y
+ * and the gradients dx, dW have the storage dtype; bias [N] (NULL: none) and dbias are float32.  Sums are
+ * float32 in an order that the sizes alone fix; y may not overlap an input.  Fewer than 2^24 for K and N,
+ * 2^44 elements at most.  Rows that start at a multiple of 16 bytes and hold a multiple of 16 are fastest, a
+ * few rows (up to 64) have kernels of their own.
+ *
+ * pre [M, N] (float32; NULL: not wanted) receives u, which the backward of an activation reads.  Gradients
+ * from d_y [M, N]:
+ *   du = d_y act'(u),   dx = du W,   dW = du^T x,   dbias = sum over the rows of du   (residual: d_y itself),
+ * dx, dW and dbias each NULL where not wanted, pre not used without an activation.  du enters the products
+ * rounded to the storage dtype, dbias as it is.  The workspace is ll_projection_workspace_size(...) bytes
+ * (0: NULL is accepted; 0 for invalid arguments too); the backward's is at least the forward's. */
+size_t ll_projection_workspace_size(int32_t dtype, int64_t M, int64_t K, int64_t N, int32_t act,
+                                    int32_t backward);
+ll_status ll_projection_fwd(const void* x, int64_t x_stride, const void* weight, const float* bias,
+                            const void* residual, int64_t residual_stride, void* y, float* pre, int64_t M,
+                            int64_t K, int64_t N, int32_t act, int32_t dtype, void* workspace,
+                            size_t workspace_bytes, void* stream);
+ll_status ll_projection_bwd(const void* x, int64_t x_stride, const void* weight, const float* pre,
+                            const void* d_y, void* dx, void* dweight, float* dbias, int64_t M, int64_t K,
+                            int64_t N, int32_t act, int32_t dtype, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
 /* Debug: writes out[t*T + s] = the Fenwick level l(t,s) that the forward kernels assign to the
  * pair (t, s) for chunk size C (Sec. 3.1; the intra/inter split of Eq. 5), and -1 for s > t.
  * `out` is device memory of T*T bytes.  Computed on the GPU by the same device functions the

@@ -1,5 +1,5 @@
 """Float64 oracle of the operators around a token mixer: the short causal convolution, the selective state
-space scan and the group norm, each with its gradients.  Token by token and group by group, from the formulas;
+space scan, the group norm and the projections, each with its gradients.  Token by token and group by group, from the formulas;
 `lengths` ends the sequences of a batch early."""
 
 import numpy as np
@@ -169,3 +169,19 @@ def norm_grad(x, G, d_y, w=None, b=None, z=None, eps=1e-5, silu=True):
     xg = xh.reshape(v.shape)
     dx = r * (g - g.mean((1, 3), keepdims=True) - xg * (g * xg).mean((1, 3), keepdims=True))
     return dx.reshape(N, S, C), (du * xh).sum((0, 1)), du.sum((0, 1)), dz
+
+
+# ------------------------------------------------------------------------------------ projection
+
+def projection(x, w, bias=None, residual=None, silu=False):
+    """(y, u): u = x w^T + bias, y = act(u) + residual."""
+    x, w, bias, residual = _f64(x, w, bias, residual)
+    u = x @ w.T + (0.0 if bias is None else bias)
+    return act(u, silu) + (0.0 if residual is None else residual), u
+
+
+def projection_grad(x, w, d_y, bias=None, silu=False):
+    """Gradients of sum(y d_y): (dx, dw, dbias)."""
+    x, w, d_y = _f64(x, w, d_y)
+    du = d_y * act_grad(projection(x, w, bias)[1], silu)
+    return du @ w, du.T @ x, du.sum(0)

@@ -21,6 +21,7 @@ LL_ACT_NONE, LL_ACT_SILU = 0, 1
 ConvGrads = namedtuple("ConvGrads", "x weight bias initial_state")
 ScanGrads = namedtuple("ScanGrads", "x dt A B C D z dt_bias initial_state")
 NormGrads = namedtuple("NormGrads", "x weight bias gate")
+ProjectionGrads = namedtuple("ProjectionGrads", "x weight bias")
 
 
 class _ScanInputs(ctypes.Structure):
@@ -51,6 +52,9 @@ _declare("ll_selective_scan_bwd", [_inputs] + [_vp] * 13 + [_sz, _vp])
 _declare("ll_group_norm_workspace_size", [_i32] + [_i64] * 4 + [_i32], _sz)
 _declare("ll_group_norm_fwd", [_vp, _i64, _i64] * 2 + [_vp] * 4 + [_i64] * 4 + [_f32, _i32, _i32, _vp, _sz, _vp])
 _declare("ll_group_norm_bwd", [_vp, _i64, _i64] * 2 + [_vp] * 8 + [_i64] * 4 + [_i32, _i32, _vp, _sz, _vp])
+_declare("ll_projection_workspace_size", [_i32] + [_i64] * 3 + [_i32, _i32], _sz)
+_declare("ll_projection_fwd", [_vp, _i64] + [_vp] * 3 + [_i64] + [_vp] * 2 + [_i64] * 3 + [_i32, _i32, _vp, _sz, _vp])
+_declare("ll_projection_bwd", [_vp, _i64] + [_vp] * 6 + [_i64] * 3 + [_i32, _i32, _vp, _sz, _vp])
 
 
 # ------------------------------------------------------------------------------------ checks
@@ -396,6 +400,69 @@ def ll_group_norm_bwd(x, groups, weight, bias, stats, d_y, gate=None, act=LL_ACT
     return grads
 
 
+# ------------------------------------------------------------------------------------ projection
+
+def _projection_args(x, weight, bias):
+    """M, K, N and the stride of x's rows (that of an only row is not used) of checked arguments."""
+    M, K = _dims(x, "x", 2)
+    N = _dims(weight, "weight", 2)[0]
+    stride = _rows(x, "x", x.dtype, x.shape)[0]
+    _check(weight, "weight", x.dtype, (N, K))
+    _opt(bias, "bias", torch.float32, (N,))
+    return M, K, N, stride if M != 1 else 0
+
+
+def _projection_need(x, weight, act, backward):
+    return lib.ll_projection_workspace_size(_dtype_code(x), *x.shape, weight.shape[0], act, int(backward))
+
+
+def ll_projection_workspace(x, weight, act=LL_ACT_NONE, backward=False):
+    """A workspace for the forward (or backward, which serves both) projection of x [M, K] with weight [N, K]."""
+    _dims(x, "x", 2), _dims(weight, "weight", 2)
+    return _buffer(_projection_need(x, weight, act, backward), x.device)
+
+
+def ll_projection_fwd(x, weight, bias=None, residual=None, act=LL_ACT_NONE, pre=None, out=None, workspace=None,
+                      stream=None):
+    """y = act(u) + residual, u = x [M, K] @ weight [N, K].T + bias; returns y [M, N].  x and residual may be columns of
+    wider rows.  `pre` (float32 [M, N]) receives u, for ll_projection_bwd of an activation."""
+    M, K, N, stride = _projection_args(x, weight, bias)
+    dtype = x.dtype
+    code = _dtype_code(x)
+    res_stride = 0 if residual is None else _rows(residual, "residual", dtype, (M, N))[0]
+    _opt(pre, "pre", torch.float32, (M, N))
+    if out is None:
+        out = _results(lambda: x.new_empty((M, N)), stream)
+    else:
+        _check(out, "out", dtype, (M, N))
+    ws = _sized(workspace, lambda: lib.ll_projection_workspace_size(code, M, K, N, act, 0), x.device, stream)
+    _ok(lib.ll_projection_fwd(x.data_ptr(), stride, weight.data_ptr(), _ptr(bias), _ptr(residual),
+                              res_stride if M != 1 else 0, out.data_ptr(), _ptr(pre), M, K, N, act, code, _ptr(ws), ws.numel(), _stream(stream)))
+    return out
+
+
+def ll_projection_bwd(x, weight, bias, d_y, act=LL_ACT_NONE, pre=None, grads=None, workspace=None, stream=None):
+    """Gradients of ll_projection_fwd on the same inputs (that of a residual is d_y): a ProjectionGrads (x, weight,
+    bias) of new tensors, or `grads` filled in, of which each may be None: not wanted.  That of a bias that is None is
+    None.  With an activation `pre` is what the forward left."""
+    M, K, N, stride = _projection_args(x, weight, bias)
+    _check(d_y, "d_y", x.dtype, (M, N))
+    _opt(pre, "pre", torch.float32, (M, N))
+    code = _dtype_code(x)
+    if grads is None:
+        grads = _results(lambda: ProjectionGrads(x.new_empty((M, K)), torch.empty_like(weight),
+                                                 None if bias is None else torch.empty_like(bias)), stream)
+    g = ProjectionGrads(*grads)
+    _opt(g.x, "grads.x", x.dtype, (M, K))
+    _opt(g.weight, "grads.weight", x.dtype, (N, K))
+    _opt(g.bias, "grads.bias", torch.float32, (N,))
+    ws = _sized(workspace, lambda: lib.ll_projection_workspace_size(code, M, K, N, act, 1), x.device, stream)
+    _ok(lib.ll_projection_bwd(x.data_ptr(), stride, weight.data_ptr(), _ptr(pre), d_y.data_ptr(), _ptr(g.x),
+                              _ptr(g.weight), _ptr(g.bias), M, K, N, act, code, _ptr(ws), ws.numel(),
+                              _stream(stream)))
+    return grads
+
+
 # ------------------------------------------------------------------------------------ autograd
 
 def _dense(t):
@@ -469,6 +536,38 @@ class _GroupNorm(torch.autograd.Function):
         return (*_once(g), None, None, None)
 
 
+class _Projection(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, residual, act):
+        lead = x.shape[:-1]
+        x, weight, bias = _channels_last(x.reshape(-1, x.shape[-1])), weight.contiguous(), _dense(bias)
+        if residual is not None:
+            if residual.shape != (*lead, weight.shape[0]):
+                raise ValueError(f"residual has shape {tuple(residual.shape)}, expected {(*lead, weight.shape[0])}")
+            residual = _channels_last(residual.reshape(-1, residual.shape[-1]))
+        keep = act != LL_ACT_NONE and any(ctx.needs_input_grad[:3])
+        pre = weight.new_empty((x.shape[0], weight.shape[0]), dtype=torch.float32) if keep else None
+        y = ll_projection_fwd(x, weight, bias, residual, act, pre)
+        ctx.save_for_backward(x, weight, bias, pre)
+        ctx.act, ctx.lead = act, lead
+        return y.view(*lead, -1)
+
+    @staticmethod
+    def backward(ctx, d_y):
+        x, weight, bias, pre = ctx.saved_tensors
+        wants = ctx.needs_input_grad
+        dx = dw = db = None
+        if any(wants[:3]):
+            dy = d_y.reshape(x.shape[0], -1).contiguous()
+            want = ProjectionGrads(x.new_empty(x.shape) if wants[0] else None,
+                                   torch.empty_like(weight) if wants[1] else None,
+                                   torch.empty_like(bias) if wants[2] else None)
+            # the residual's gradient is d_y, which may be differentiated again; what the kernels give may not
+            dx, dw, db = _once(ll_projection_bwd(x, weight, bias, dy, ctx.act, pre, want))
+            dx = None if dx is None else dx.view(*ctx.lead, -1)
+        return dx, dw, db, d_y if wants[3] else None, None
+
+
 def causal_conv(x, weight, bias=None, act=LL_ACT_SILU, initial_state=None, lengths=None, return_final_state=False):
     """Differentiable ll_causal_conv_fwd: y, or (y, final state); gradients flow to x, weight, bias and the states."""
     y, final = _CausalConv.apply(x, weight, bias, initial_state, lengths, act, return_final_state)
@@ -487,3 +586,9 @@ def selective_scan(x, dt, A, B, C, D=None, z=None, dt_bias=None, delta_softplus=
 def group_norm(x, groups, weight=None, bias=None, gate=None, eps=1e-5, act=LL_ACT_SILU):
     """Differentiable ll_group_norm_fwd; gradients flow to x, weight, bias and gate."""
     return _GroupNorm.apply(x, weight, bias, gate, groups, eps, act)
+
+
+def projection(x, weight, bias=None, residual=None, act=LL_ACT_NONE):
+    """Differentiable ll_projection_fwd of x [.., K] with weight [N, K], for any leading axes: act(x @ weight.T + bias) +
+    residual [.., N]; gradients flow to x, weight, bias and residual."""
+    return _Projection.apply(x, weight, bias, residual, act)

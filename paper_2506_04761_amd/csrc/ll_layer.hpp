@@ -1,5 +1,5 @@
 // Host-side argument bundles of the operators around a token mixer (short causal convolution,
-// selective state space scan, group norm), shared by their C ABI (ll_layer_api.hip) and kernels.
+// selective state space scan, group norm) and of the projections, shared by their C ABI (ll_layer_api.hip) and kernels.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -137,6 +137,31 @@ int64_t norm_workspace(int64_t N, int64_t S, int64_t C, int64_t G, int dtype, bo
 bool norm_launchable(const NormArgs& a, bool backward);
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t st);
 hipError_t launch_norm_bwd(const NormArgs& a, const NormGrads& g, hipStream_t st);
+
+// ---- projection
+struct ProjArgs {
+  const void* x;
+  int64_t x_stride;
+  const void* weight;      // [N, K]
+  const float* bias;       // may be null
+  const void* residual;    // may be null
+  int64_t residual_stride;
+  void* y;
+  float* pre;              // [M, N] sums before the activation; forward: may be null
+  int64_t M, K, N;
+  int act, dtype;
+  void* workspace;
+};
+struct ProjGrads {
+  const void* dy;
+  void* dx;                // each may be null
+  void* dweight;
+  float* dbias;
+};
+int64_t projection_workspace(int64_t M, int64_t K, int64_t N, int act, int dtype, bool backward);
+bool projection_launchable(int64_t M, int64_t K, int64_t N, int act, int dtype, bool backward);
+hipError_t launch_projection_fwd(const ProjArgs& a, hipStream_t st);
+hipError_t launch_projection_bwd(const ProjArgs& a, const ProjGrads& g, hipStream_t st);
 
 // Column sums of an fp32 matrix of partial sums, rows added in an order that the sizes alone fix.  Output k
 // takes columns col0 .. col0 + cols - 1; column c goes to out[(c / in_cols) * major + (c % in_cols) * minor],

@@ -91,6 +91,14 @@ ll_status norm_args(const void* x, int64_t xbs, int64_t xts, const void* gate, i
   return LL_OK;
 }
 
+// x [M, K] and W [N, K] to [M, N].
+ll_status projection_sizes(int64_t M, int64_t K, int64_t N, int32_t act, int32_t dtype) {
+  LL_TRY(check_sizes(M, 1, K));
+  LL_TRY(check_sizes(M, 1, N));
+  LL_TRY(check_sizes(N, 1, K));
+  return known_act(act) && known_dtype(dtype) ? LL_OK : LL_ERR_UNSUPPORTED;
+}
+
 }  // namespace
 
 extern "C" {
@@ -223,6 +231,41 @@ ll_status ll_group_norm_bwd(const void* x, int64_t x_batch_stride, int64_t x_tok
   a.weight = weight, a.bias = bias, a.stats = const_cast<float*>(stats), a.workspace = workspace;
   const ll::NormGrads g = {d_y, dx, gate ? dgate : nullptr, dweight, dbias};
   return launched(ll::launch_norm_bwd(a, g, static_cast<hipStream_t>(stream)));
+}
+
+size_t ll_projection_workspace_size(int32_t dtype, int64_t M, int64_t K, int64_t N, int32_t act, int32_t backward) {
+  if (projection_sizes(M, K, N, act, dtype) != LL_OK) return 0;
+  return (size_t)ll::projection_workspace(M, K, N, act, dtype, backward != 0);
+}
+
+ll_status ll_projection_fwd(const void* x, int64_t x_stride, const void* weight, const float* bias,
+                            const void* residual, int64_t residual_stride, void* y, float* pre, int64_t M, int64_t K,
+                            int64_t N, int32_t act, int32_t dtype, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+  if (!x || !weight || !y) return LL_ERR_NULL_ARG;
+  LL_TRY(projection_sizes(M, K, N, act, dtype));
+  LL_TRY(check_strides(0, x_stride));
+  if (residual) LL_TRY(check_strides(0, residual_stride));
+  if (!ll::projection_launchable(M, K, N, act, dtype, false)) return LL_ERR_UNSUPPORTED;
+  LL_TRY(check_workspace(workspace, workspace_bytes, ll::projection_workspace(M, K, N, act, dtype, false)));
+  const ll::ProjArgs a = {x, x_stride, weight, bias, residual, residual_stride, y, pre, M, K, N, act, dtype, workspace};
+  return launched(ll::launch_projection_fwd(a, static_cast<hipStream_t>(stream)));
+}
+
+ll_status ll_projection_bwd(const void* x, int64_t x_stride, const void* weight, const float* pre, const void* d_y,
+                            void* dx, void* dweight, float* dbias, int64_t M, int64_t K, int64_t N, int32_t act,
+                            int32_t dtype, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!x || !weight || !d_y) return LL_ERR_NULL_ARG;
+  LL_TRY(projection_sizes(M, K, N, act, dtype));
+  LL_TRY(check_strides(0, x_stride));
+  if (act != LL_ACT_NONE && !pre) return LL_ERR_NULL_ARG;
+  if (!ll::projection_launchable(M, K, N, act, dtype, true)) return LL_ERR_UNSUPPORTED;
+  LL_TRY(check_workspace(workspace, workspace_bytes, ll::projection_workspace(M, K, N, act, dtype, true)));
+  ll::ProjArgs a = {};
+  a.x = x, a.x_stride = x_stride, a.weight = weight, a.pre = const_cast<float*>(pre), a.M = M, a.K = K, a.N = N;
+  a.act = act, a.dtype = dtype, a.workspace = workspace;
+  const ll::ProjGrads g = {d_y, dx, dweight, dbias};
+  return launched(ll::launch_projection_bwd(a, g, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -1,0 +1,543 @@
+// Projections: u = x W^T + bias, y = act(u) + residual, x [M, K], W [N, K], and their gradients
+//   du = dy act'(u), dx = du W, dW = du^T x, dbias = sum over the rows of du.
+//
+// One kernel serves the three products.  Each is out[m, n] = sum_k a(n, k) b(m, k); an operand lies in memory
+// "along" the reduction (x and W in the forward: rows of k) or "down" it (W in dx, du and x in dW: every row is one
+// k).  A stage of 128 bytes of k of both operands is copied to LDS as it lies, and the fragments of the matrix
+// instructions are read from there along or down the rows, so that nothing is transposed in memory.
+#include "ll_layer.hpp"
+#include "ll_layer_device.hpp"
+
+namespace ll {
+
+namespace {
+
+// A fragment is 16 bytes of k of each of 16 outputs: lane (g = lane / 16, i = lane % 16) holds k = KF / 4 * g + {0 ..}
+// of output i.
+template <typename T>
+struct Op;
+template <>
+struct Op<__bf16> {
+  static constexpr int KF = 32;
+  typedef bf16x8 Frag;
+  __device__ static inline f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Op<float> {
+  static constexpr int KF = 16;
+  typedef f32x4 Frag;
+  __device__ static inline f32x4 mma(Frag a, Frag b, f32x4 c) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[r], b[r], c, 0, 0, 0);
+    return c;
+  }
+};
+
+// Outputs are taken in pairs of 16: output i of fragment t is 32 (t / 2) + 8 (i / 4) + 4 (t % 2) + i % 4, so that the four
+// results that a lane holds of each of a pair are eight adjacent ones.
+__device__ inline int output_of(int t, int i) { return 32 * (t >> 1) + 8 * (i >> 2) + 4 * (t & 1) + (i & 3); }
+
+constexpr int kStageBytes = 128;  // of k
+
+// The LDS tile of TD outputs' stage: 16-byte chunks, chunk c of a row at c ^ key(row), with keys for which the lanes that
+// an LDS read serves together (rows 0 - 3 and 8 - 11 along; four rows of four chunks, or four rows 4 apart, down) touch
+// different banks.
+template <typename T, int TD, bool DOWN>
+struct Tile {
+  static constexpr int E = 16 / sizeof(T);
+  static constexpr int BK = kStageBytes / sizeof(T);
+  static constexpr int CH = DOWN ? TD / E : 8;  // chunks of a row
+  __device__ static inline int key(int row) {
+    if (!DOWN) return (row & 3) | ((row >> 1) & 4);
+    if (sizeof(T) == 4) return ((row >> 2) & 1) | (row & 8);
+    return CH == 8 ? 4 * ((row >> 1) & 1) : 4 * (row & 3);
+  }
+  // Fragment t of k step ks of the outputs from d0 on.
+  __device__ static inline typename Op<T>::Frag frag(const T* s, int d0, int t, int ks, int lane) {
+    const int g = lane >> 4, i = lane & 15;
+    if constexpr (!DOWN) {
+      const int row = d0 + output_of(t, i);
+      return *reinterpret_cast<const typename Op<T>::Frag*>(s + (row * CH + ((4 * ks + g) ^ key(row))) * E);
+    } else if constexpr (sizeof(T) == 2) {
+      // lane 4 j + c of 16 supplies four outputs of row j, see lds_read_tr
+      const int row = 32 * ks + 8 * g + (i >> 2), d = d0 + output_of(t, 4 * (i & 3));
+      const int at = (d >> 3) ^ key(row);
+      const bf16x4 lo = lds_read_tr(s + (row * CH + at) * E + (d & 7));
+      const bf16x4 hi = lds_read_tr(s + ((row + 4) * CH + at) * E + (d & 7));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      const int row = 16 * ks + 4 * g, d = d0 + output_of(t, i);
+      const int at = (d >> 2) ^ key(row);
+      f32x4 f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) f[r] = s[((row + r) * CH + at) * E + (d & 3)];
+      return f;
+    }
+  }
+};
+
+// An operand: `n` outputs, rows of memory `stride` elements apart.
+struct Side {
+  const void* p;
+  int64_t stride, n;
+};
+
+__device__ const uint4 kZeros = {0, 0, 0, 0};  // the k beyond the last
+
+// Copies stages of an operand to LDS, 16 bytes a thread at a time: straight there (DIRECT: rows of whole, aligned
+// chunks), or through registers (any rows).
+template <typename T, int TD, bool DOWN, bool DIRECT, int NT>
+struct Copy {
+  typedef Tile<T, TD, DOWN> Tl;
+  typedef typename VecN<T, Tl::E>::type Vec;
+  static constexpr int E = Tl::E, ITS = TD * 8 / NT;
+  const T* src[ITS];
+  int ofs[ITS];    // first k of the chunk within a stage
+  int count[ITS];  // outputs (down) or rows (along, 0 or E) that are inputs
+  Vec held[DIRECT ? 1 : ITS];
+  int64_t step;
+
+  __device__ inline void start(const Side& s, int64_t d0, int64_t k0) {
+    step = DOWN ? Tl::BK * s.stride : Tl::BK;
+#pragma unroll
+    for (int it = 0; it < ITS; ++it) {
+      const int q = it * NT + threadIdx.x, row = q / Tl::CH, c = (q % Tl::CH) ^ Tl::key(row);
+      if (DOWN) {
+        int64_t d = d0 + c * E;
+        ofs[it] = row;
+        count[it] = d >= s.n ? 0 : (s.n - d < E ? int(s.n - d) : E);
+        if (DIRECT && d > s.n - E) d = s.n - E;  // some input, for outputs that are not stored
+        src[it] = static_cast<const T*>(s.p) + (k0 + row) * s.stride + d;
+      } else {
+        int64_t d = d0 + row;
+        ofs[it] = c * E;
+        count[it] = d < s.n ? E : 0;
+        if (DIRECT && d >= s.n) d = s.n - 1;
+        src[it] = static_cast<const T*>(s.p) + d * s.stride + k0 + c * E;
+      }
+    }
+  }
+  // Begins the copy of the next stage, of which `left` k are inputs.
+  __device__ inline void load(T* lds, int64_t left) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int it = 0; it < ITS; ++it) {
+      if constexpr (DIRECT) {
+        const void* from = src[it];
+        if (left < Tl::BK && ofs[it] >= left) from = &kZeros;
+        __builtin_amdgcn_global_load_lds(from, (__attribute__((address_space(3))) void*)(lds + (it * NT + wave * 64) * E), 16, 0, 0);
+      } else {
+        int n = count[it];
+        if (left < Tl::BK) {
+          const int k = int(left) - ofs[it];
+          if (DOWN) n = k > 0 ? n : 0;
+          else n = n == 0 || k <= 0 ? 0 : (k < E ? k : E);
+        }
+        held[it] = load_n<T, E>(src[it], n, false);
+      }
+      src[it] += step;
+    }
+  }
+  // Through registers: ends the copy.
+  __device__ inline void store(T* lds) {
+    if constexpr (!DIRECT) {
+#pragma unroll
+      for (int it = 0; it < ITS; ++it) *reinterpret_cast<Vec*>(lds + (it * NT + threadIdx.x) * E) = held[it];
+    }
+  }
+};
+
+// What becomes of a product's sums.
+struct Finish {
+  void* out;           // [M, N]
+  const float* bias;   // may be null
+  const void* res;     // may be null
+  int64_t res_stride;
+  float* pre;          // may be null
+  int64_t M, N;
+  int act;
+};
+
+// V adjacent sums of row m from column n on.
+template <typename T, int V>
+__device__ inline void finish(const Finish& f, float* v, int64_t m, int64_t n) {
+  if (m >= f.M || n >= f.N) return;
+  const int count = f.N - n < V ? int(f.N - n) : V;
+  if (f.bias) {
+    float b[V];
+    load_params<V>(f.bias + n, count, 0.0f, false, b);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] += b[i];
+  }
+  if (f.pre) store_n<float, V>(f.pre + m * f.N + n, v, count, false);
+  if (f.act) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = silu(v[i]);
+  }
+  if (f.res) {
+    const auto r = load_n<T, V>(static_cast<const T*>(f.res) + m * f.res_stride + n, count, false);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] += to_f32(T(r[i]));
+  }
+  store_n<T, V>(static_cast<T*>(f.out) + m * f.N + n, v, count, false);
+}
+
+struct GemmDev {
+  Side a, b;               // outputs n, outputs m
+  int64_t K, span;         // span: k of a split, whole stages
+  int64_t m_tiles, n_tiles, splits;
+  float* part;             // several splits: [splits, M, N] partial sums
+  Finish f;
+};
+
+template <typename T, int TM, int TN, int WM, int WN, bool DOWN_M, bool DOWN_N, bool DIRECT>
+__global__ __launch_bounds__(64 * WM * WN) void k_gemm(GemmDev p) {
+  constexpr int NT = 64 * WM * WN, FM = TM / WM / 16, FN = TN / WN / 16;
+  typedef Tile<T, TM, DOWN_M> TlM;
+  typedef Tile<T, TN, DOWN_N> TlN;
+  constexpr int BK = TlM::BK, KS = BK / Op<T>::KF;
+  constexpr int kStage = (TM + TN) * BK;
+  __shared__ __attribute__((aligned(1024))) T s[2 * kStage];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WN * (TM / WM), wn = wave % WN * (TN / WN);
+
+  // an XCD takes adjacent tiles, eight rows of tiles at a time, so that its L2 serves both operands
+  const int64_t tiles = p.m_tiles * p.n_tiles;
+  int64_t id = xcd_remap(blockIdx.x, tiles * p.splits);
+  const int64_t split = id / tiles;
+  id %= tiles;
+  const int64_t strip = id / (8 * p.n_tiles), rows = p.m_tiles - 8 * strip < 8 ? p.m_tiles - 8 * strip : 8;
+  id %= 8 * p.n_tiles;
+  const int64_t m0 = (8 * strip + id % rows) * TM, n0 = id / rows * TN;
+
+  const int64_t k0 = split * p.span;
+  int64_t left = p.K - k0 < p.span ? p.K - k0 : p.span;
+  Copy<T, TM, DOWN_M, DIRECT, NT> cm;
+  Copy<T, TN, DOWN_N, DIRECT, NT> cn;
+  cm.start(p.b, m0, k0);
+  cn.start(p.a, n0, k0);
+  f32x4 acc[FM][FN] = {};
+  cm.load(s, left);
+  cn.load(s + TM * BK, left);
+  cm.store(s);
+  cn.store(s + TM * BK);
+  const int stages = int((left + BK - 1) / BK);
+  for (int st = 0; st < stages; ++st) {
+    T* now = s + (st & 1) * kStage;
+    T* next = s + (~st & 1) * kStage;
+    if (DIRECT) wait_vmem();
+    __syncthreads();
+    left -= BK;
+    if (left > 0) {
+      cm.load(next, left);
+      cn.load(next + TM * BK, left);
+    }
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      typename Op<T>::Frag a[FN], b[FM];
+#pragma unroll
+      for (int j = 0; j < FN; ++j) a[j] = TlN::frag(now + TM * BK, wn, j, ks, lane);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) b[i] = TlM::frag(now, wm, i, ks, lane);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = Op<T>::mma(a[j], b[i], acc[i][j]);
+    }
+    if (left > 0) {
+      cm.store(next);
+      cn.store(next + TM * BK);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    const int64_t m = m0 + wm + output_of(i, lane & 15);
+#pragma unroll
+    for (int j = 0; j < FN; j += 2) {
+      const int64_t n = n0 + wn + 16 * j + 8 * (lane >> 4);
+      float v[8];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = acc[i][j][r], v[4 + r] = acc[i][j + 1][r];
+      if (p.part) {
+        if (m < p.f.M && n < p.f.N)
+          store_n<float, 8>(p.part + (split * p.f.M + m) * p.f.N + n, v, p.f.N - n < 8 ? int(p.f.N - n) : 8, false);
+      } else {
+        finish<T, 8>(p.f, v, m, n);
+      }
+    }
+  }
+}
+
+// The splits' partial sums, added in their order, and what becomes of them.
+template <typename T>
+__global__ __launch_bounds__(256) void k_gemm_join(GemmDev p) {
+  constexpr int V = 4;
+  const int64_t per_row = (p.f.N + V - 1) / V, id = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  const int64_t m = id / per_row, n = id % per_row * V;
+  if (m >= p.f.M) return;
+  const int count = p.f.N - n < V ? int(p.f.N - n) : V;
+  float v[V] = {};
+#pragma unroll 4
+  for (int64_t s = 0; s < p.splits; ++s) {
+    const auto w = load_n<float, V>(p.part + (s * p.f.M + m) * p.f.N + n, count, false);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] += w[i];
+  }
+  finish<T, V>(p.f, v, m, n);
+}
+
+// A few rows (up to 16 MT): 16 outputs n to a workgroup, whose waves take 128 bytes of k each in turn, straight from
+// memory, and are added at the end in their order.
+constexpr int kFewWaves = 8;
+template <typename T, int MT>
+__global__ __launch_bounds__(64 * kFewWaves) void k_few_rows(GemmDev p, bool vec) {
+  constexpr int E = 16 / sizeof(T), KF = Op<T>::KF;
+  __shared__ f32x4 s[kFewWaves][MT][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i = lane & 15;
+  const int64_t n0 = int64_t(blockIdx.x) * 16;
+  const int64_t arow = n0 + i < p.a.n ? n0 + i : p.a.n - 1;
+  const T* a = static_cast<const T*>(p.a.p) + arow * p.a.stride;
+  const T* b[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) b[t] = static_cast<const T*>(p.b.p) + (16 * t + i < p.b.n ? 16 * t + i : p.b.n - 1) * p.b.stride;
+  f32x4 acc[MT] = {};
+  for (int64_t k0 = wave * 2 * KF; k0 < p.K; k0 += kFewWaves * 2 * KF) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t k = k0 + h * KF + E * g;
+      const int n = k >= p.K ? 0 : (p.K - k < E ? int(p.K - k) : E);
+      const auto fa = load_n<T, E>(a + k, n, vec);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) acc[t] = Op<T>::mma(fa, load_n<T, E>(b[t] + k, n, vec), acc[t]);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < MT; ++t) s[wave][t][lane] = acc[t];
+  __syncthreads();
+  for (int t = wave; t < MT; t += kFewWaves) {
+    float v[4] = {};
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] += s[w][t][lane][r];
+    finish<T, 4>(p.f, v, 16 * t + i, n0 + 4 * g);
+  }
+}
+
+// du = dy act'(pre), rounded to the storage type for the two products that read it, and its sums over strips of rows,
+// which take it as it is.  64 lanes of E columns and four rows at a time to a workgroup.
+struct DuDev {
+  const void* dy;
+  const float* pre;  // null: du = dy, only the sums
+  void* du;
+  float* part;       // [strips, N]; may be null
+  int64_t M, N, rows, cols;  // rows of a strip, workgroups over the columns
+};
+template <typename T>
+__global__ __launch_bounds__(256) void k_du(DuDev p) {
+  constexpr int E = 16 / sizeof(T);
+  __shared__ float s[4][64][E + 1];
+  const int lane = threadIdx.x & 63, sub = threadIdx.x >> 6;
+  const int64_t strip = blockIdx.x / p.cols, n = (blockIdx.x % p.cols * 64 + lane) * E;
+  const int count = n >= p.N ? 0 : (p.N - n < E ? int(p.N - n) : E);
+  const int64_t end = (strip + 1) * p.rows < p.M ? (strip + 1) * p.rows : p.M;
+  float sum[E] = {};
+  if (count > 0) {
+#pragma unroll 4
+    for (int64_t m = strip * p.rows + sub; m < end; m += 4) {
+      const auto g = load_n<T, E>(static_cast<const T*>(p.dy) + m * p.N + n, count, false);
+      float d[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) d[i] = to_f32(T(g[i]));
+      if (p.pre) {
+        const auto u = load_n<float, E>(p.pre + m * p.N + n, count, false);
+#pragma unroll
+        for (int i = 0; i < E; ++i) d[i] *= silu_grad(u[i], sigmoidf(u[i]));
+        store_n<T, E>(static_cast<T*>(p.du) + m * p.N + n, d, count, false);
+      }
+#pragma unroll
+      for (int i = 0; i < E; ++i) sum[i] += d[i];
+    }
+  }
+  if (!p.part) return;
+#pragma unroll
+  for (int i = 0; i < E; ++i) s[sub][lane][i] = sum[i];
+  __syncthreads();
+  for (int c = threadIdx.x; c < 64 * E; c += 256) {
+    const int64_t col = blockIdx.x % p.cols * 64 * E + c;
+    if (col < p.N) p.part[strip * p.N + col] = s[0][c / E][c % E] + s[1][c / E][c % E] + s[2][c / E][c % E] + s[3][c / E][c % E];
+  }
+}
+
+// ------------------------------------------------------------------------------------ plans
+
+int elem(int dtype) { return dtype == 1 ? 2 : 4; }
+
+enum Product { kForward, kDx, kDw };
+
+struct GemmPlan {
+  int few = 0;             // fragments of 16 rows, or 0
+  int tile = 0;            // outputs of a tile's sides
+  int64_t m_tiles = 0, n_tiles = 0, splits = 1, span = 0;
+  int64_t workgroups = 0;
+  int64_t bytes = 0;       // of partial sums
+};
+
+// out [M, N] over K.
+GemmPlan plan(int64_t M, int64_t N, int64_t K, int dtype, Product what) {
+  GemmPlan q;
+  const int64_t BK = kStageBytes / elem(dtype), stages = ceil_div(K, BK);
+  if (what == kForward && M <= 64) {
+    q.few = M <= 16 ? 1 : M <= 32 ? 2 : 4;
+    q.workgroups = ceil_div(N, 16);
+    return q;
+  }
+  auto tiles = [&](int t) { return ceil_div(M, t) * ceil_div(N, t); };
+  q.tile = tiles(128) >= 256 ? 128 : 64;
+  q.m_tiles = ceil_div(M, q.tile), q.n_tiles = ceil_div(N, q.tile);
+  const int64_t n = q.m_tiles * q.n_tiles;
+  if (n < 256) {
+    q.splits = 512 / n < stages / 4 ? 512 / n : stages / 4;
+    q.splits = q.splits < 1 ? 1 : (q.splits > 32 ? 32 : q.splits);
+  }
+  const int64_t each = ceil_div(stages, q.splits);
+  q.span = each * BK;
+  q.splits = ceil_div(stages, each);
+  q.workgroups = n * q.splits;
+  q.bytes = q.splits > 1 ? q.splits * M * N * 4 : 0;
+  return q;
+}
+
+int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
+
+struct DuPlan {
+  int64_t cols, rows, strips;
+};
+DuPlan du_plan(int64_t M, int64_t N, int dtype) {
+  DuPlan q;
+  q.cols = ceil_div(N, 64 * (16 / elem(dtype)));
+  q.rows = ceil_div(M * q.cols, 1024);
+  q.rows = ceil_div(q.rows < 16 ? 16 : q.rows, 4) * 4;
+  q.strips = ceil_div(M, q.rows);
+  return q;
+}
+
+struct BwdPlan {
+  GemmPlan dx, dw;
+  DuPlan du;
+  int64_t o_du = 0, o_part = 0, total = 0;  // du; partial sums of whichever kernel runs
+};
+BwdPlan bwd_plan(int64_t M, int64_t K, int64_t N, int dtype, bool act) {
+  BwdPlan q;
+  q.dx = plan(M, K, N, dtype, kDx);
+  q.dw = plan(N, K, M, dtype, kDw);
+  q.du = du_plan(M, N, dtype);
+  q.o_part = act ? up256(M * N * elem(dtype)) : 0;
+  int64_t part = q.du.strips * N * 4;
+  part = part < q.dx.bytes ? q.dx.bytes : part;
+  part = part < q.dw.bytes ? q.dw.bytes : part;
+  q.total = q.o_part + up256(part);
+  return q;
+}
+
+bool direct(const Side& s, bool down, int64_t K, int esize) {
+  const int e = 16 / esize;
+  return reinterpret_cast<uintptr_t>(s.p) % 16 == 0 && s.stride % e == 0 && (down ? s.n : K) % e == 0;
+}
+
+template <typename T, int TILE, bool DM, bool DN, bool DIRECT>
+void launch_tiles(const GemmDev& p, int64_t workgroups, hipStream_t st) {
+  k_gemm<T, TILE, TILE, 2, 2, DM, DN, DIRECT><<<dim3(uint32_t(workgroups)), dim3(256), 0, st>>>(p);
+}
+
+template <typename T, bool DM, bool DN>
+hipError_t launch_product(GemmDev p, const GemmPlan& q, float* part, hipStream_t st) {
+  p.m_tiles = q.m_tiles, p.n_tiles = q.n_tiles, p.splits = q.splits, p.span = q.span;
+  p.part = q.splits > 1 ? part : nullptr;
+  const bool dir = direct(p.b, DM, p.K, sizeof(T)) && direct(p.a, DN, p.K, sizeof(T));
+  if (q.tile == 128) dir ? launch_tiles<T, 128, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 128, DM, DN, false>(p, q.workgroups, st);
+  else dir ? launch_tiles<T, 64, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 64, DM, DN, false>(p, q.workgroups, st);
+  if (q.splits > 1) {
+    p.part = part;
+    k_gemm_join<T><<<dim3(uint32_t(ceil_div(p.f.M * ceil_div(p.f.N, 4), 256))), dim3(256), 0, st>>>(p);
+  }
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_few(const GemmDev& p, const GemmPlan& q, hipStream_t st) {
+  const bool vec = direct(p.a, false, p.K, sizeof(T)) && direct(p.b, false, p.K, sizeof(T));
+  const dim3 grid(uint32_t(q.workgroups)), block(64 * kFewWaves);
+  if (q.few == 1) k_few_rows<T, 1><<<grid, block, 0, st>>>(p, vec);
+  else if (q.few == 2) k_few_rows<T, 2><<<grid, block, 0, st>>>(p, vec);
+  else k_few_rows<T, 4><<<grid, block, 0, st>>>(p, vec);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t fwd(const ProjArgs& a, hipStream_t st) {
+  const GemmPlan q = plan(a.M, a.N, a.K, a.dtype, kForward);
+  GemmDev p = {};
+  p.a = {a.weight, a.K, a.N}, p.b = {a.x, a.x_stride, a.M}, p.K = a.K;
+  p.f = {a.y, a.bias, a.residual, a.residual_stride, a.pre, a.M, a.N, a.act};
+  if (q.few) return launch_few<T>(p, q, st);
+  return launch_product<T, false, false>(p, q, static_cast<float*>(a.workspace), st);
+}
+
+template <typename T>
+hipError_t bwd(const ProjArgs& a, const ProjGrads& g, hipStream_t st) {
+  const BwdPlan q = bwd_plan(a.M, a.K, a.N, a.dtype, a.act != 0);
+  char* ws = static_cast<char*>(a.workspace);
+  float* part = reinterpret_cast<float*>(ws + q.o_part);
+  const void* du = a.act ? ws + q.o_du : g.dy;
+  hipError_t e = hipSuccess;
+  if (a.act || g.dbias) {
+    const DuDev d = {g.dy, a.act ? a.pre : nullptr, ws + q.o_du, g.dbias ? part : nullptr, a.M, a.N, q.du.rows, q.du.cols};
+    k_du<T><<<dim3(uint32_t(q.du.cols * q.du.strips)), dim3(256), 0, st>>>(d);
+    e = hipGetLastError();
+    if (e == hipSuccess && g.dbias) {
+      ColSum c;
+      c.part = part, c.rows = q.du.strips, c.stride = a.N, c.n = 1;
+      c.out[0] = {0, a.N, g.dbias, a.N, a.N, 0, 1};
+      e = launch_colsum(c, st);
+    }
+  }
+  if (e == hipSuccess && g.dx) {
+    GemmDev p = {};
+    p.a = {a.weight, a.K, a.K}, p.b = {du, a.N, a.M}, p.K = a.N;
+    p.f = {g.dx, nullptr, nullptr, 0, nullptr, a.M, a.K, 0};
+    e = launch_product<T, false, true>(p, q.dx, part, st);
+  }
+  if (e == hipSuccess && g.dweight) {
+    GemmDev p = {};
+    p.a = {a.x, a.x_stride, a.K}, p.b = {du, a.N, a.N}, p.K = a.M;
+    p.f = {g.dweight, nullptr, nullptr, 0, nullptr, a.N, a.K, 0};
+    e = launch_product<T, true, true>(p, q.dw, part, st);
+  }
+  return e;
+}
+
+}  // namespace
+
+int64_t projection_workspace(int64_t M, int64_t K, int64_t N, int act, int dtype, bool backward) {
+  const int64_t f = up256(plan(M, N, K, dtype, kForward).bytes);
+  if (!backward) return f;
+  const int64_t b = bwd_plan(M, K, N, dtype, act != 0).total;
+  return b > f ? b : f;
+}
+
+bool projection_launchable(int64_t M, int64_t K, int64_t N, int act, int dtype, bool backward) {
+  auto ok = [](const GemmPlan& q, int64_t m, int64_t n) {
+    return launchable(q.workgroups, q.few ? 64 * kFewWaves : 256) && (q.splits == 1 || launchable(ceil_div(m * ceil_div(n, 4), 256), 256));
+  };
+  if (!backward) return ok(plan(M, N, K, dtype, kForward), M, N);
+  const BwdPlan q = bwd_plan(M, K, N, dtype, act != 0);
+  return ok(q.dx, M, K) && ok(q.dw, N, K) && launchable(q.du.cols * q.du.strips, 256);
+}
+
+hipError_t launch_projection_fwd(const ProjArgs& a, hipStream_t st) { return a.dtype == 1 ? fwd<__bf16>(a, st) : fwd<float>(a, st); }
+hipError_t launch_projection_bwd(const ProjArgs& a, const ProjGrads& g, hipStream_t st) {
+  return a.dtype == 1 ? bwd<__bf16>(a, g, st) : bwd<float>(a, g, st);
+}
+
+}  // namespace ll

@@ -431,6 +431,52 @@ ll_status ll_group_norm_bwd(const void* x, int64_t x_batch_stride, int64_t x_tok
                             int64_t C, int64_t groups, int32_t act, int32_t dtype, void* workspace,
                             size_t workspace_bytes, void* stream);
 
+/* ---- Linear attention with a decay for each head -----------------------------------------------
+ *
+ * For sequence b, token t and head h, with g = exp(log_decay[h]) (the caller keeps log_decay <= 0; -infinity
+ * forgets everything) fixed for the head:
+ *   S_t = g S_(t-1) + k_t v_t^T,   o_t = scale S_t^T q_t.
+ * q, k [batch, T, qk_heads, d_k], v [batch, T, heads, d_v]; head h reads query/key head h / (heads / qk_heads).
+ * They may be columns of wider rows: each comes with the strides of a sequence (batch) and of a token in
+ * elements, >= 0, a token's below 2^24, heads adjacent.  o and the gradients are dense, states
+ * [batch, heads, d_k, d_v] float32.  d_k, d_v <= 256, any T; qk_heads divides heads (LL_ERR_BAD_SHAPE).
+ * Lengths, states, sums, rows and limits are as for the operators around a token mixer.  Sums and states are
+ * float32; for bf16 the scores and the states' values enter the products with v and q rounded to bf16.  A NaN or
+ * an infinity in a token may reach outputs of up to 63 tokens before it. */
+typedef struct ll_decay_inputs {
+  const void *q, *k, *v;
+  int64_t q_strides[2], k_strides[2], v_strides[2];  /* batch, token */
+  const float* log_decay;                            /* [heads] */
+  const int32_t* lengths;                            /* [batch] or NULL */
+  int64_t batch, T, heads, qk_heads, d_k, d_v;
+  float scale;
+  int32_t dtype;
+} ll_decay_inputs;
+
+/* Bytes of workspace of the forward (backward = 0; may be 0: then NULL is accepted) or of the backward (at least
+ * the forward's), and of the states that a forward leaves for the backward.  0 for invalid arguments. */
+size_t ll_decay_attention_workspace_size(int64_t B, int64_t T, int64_t H, int64_t H_qk, int64_t d_k,
+                                         int64_t d_v, int32_t backward);
+size_t ll_decay_attention_states_bytes(int64_t B, int64_t T, int64_t H, int64_t d_k, int64_t d_v);
+
+/* Forward: o [batch, T, heads, d_v] and the final state (NULL: not wanted).  states (16-byte aligned, NULL for
+ * inference) receives the states that ll_decay_attention_bwd starts from, in the library's own layout. */
+ll_status ll_decay_attention_fwd(const ll_decay_inputs* in, const float* initial_state, void* o,
+                                 float* final_state, float* states, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+
+/* One token (T = 1, no lengths): state is read and new_state written (the same buffer for decoding in place).
+ * Token strides are not used. */
+ll_status ll_decay_attention_step(const ll_decay_inputs* in, const float* state, float* new_state, void* o,
+                                  void* stream);
+
+/* Gradients of the forward that left `states`, on the same inputs, from d_o and d_final_state (NULL: zeros): dq, dk
+ * (sums over the heads that share one), dv, and d_initial_state (NULL: not wanted).  The decays are constants. */
+ll_status ll_decay_attention_bwd(const ll_decay_inputs* in, const float* states, const void* d_o,
+                                 const float* d_final_state, void* dq, void* dk, void* dv,
+                                 float* d_initial_state, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+
 /* ---- Projections ------------------------------------------------------------------------------
  *
  * Matrix products in front of and behind a mixer, with what follows them:

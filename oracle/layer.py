@@ -1,5 +1,5 @@
 """Float64 oracle of the operators around a token mixer: the short causal convolution, the selective state
-space scan, the group norm and the projections, each with its gradients.  Token by token and group by group, from the formulas;
+space scan, the group norm, the linear attention with a decay for each head and the projections, each with its gradients.  Token by token and group by group, from the formulas;
 `lengths` ends the sequences of a batch early."""
 
 import numpy as np
@@ -169,6 +169,50 @@ def norm_grad(x, G, d_y, w=None, b=None, z=None, eps=1e-5, silu=True):
     xg = xh.reshape(v.shape)
     dx = r * (g - g.mean((1, 3), keepdims=True) - xg * (g * xg).mean((1, 3), keepdims=True))
     return dx.reshape(N, S, C), (du * xh).sum((0, 1)), du.sum((0, 1)), dz
+
+
+# ------------------------------------------------------------------------------------ decay attention
+
+def _shared(x, H):
+    return np.repeat(x, H // x.shape[2], axis=2)
+
+
+def decay_attention(q, k, v, log_decay, scale=1.0, initial=None, lengths=None):
+    """(o, final state): S_t = g S_(t-1) + k_t v_t^T, o_t = scale S_t^T q_t; heads share q and k in groups."""
+    q, k, v, log_decay, initial = _f64(q, k, v, log_decay, initial)
+    B, T, H, dv = v.shape
+    q, k, g = _shared(q, H), _shared(k, H), np.exp(log_decay)[:, None, None]
+    o, final = np.zeros((B, T, H, dv)), np.zeros((B, H, q.shape[-1], dv))
+    for b, n in enumerate(_ends(lengths, B, T)):
+        S = final[b].copy() if initial is None else initial[b]
+        for t in range(n):
+            S = g * S + k[b, t, :, :, None] * v[b, t, :, None, :]
+            o[b, t] = scale * (q[b, t, :, :, None] * S).sum(1)
+        final[b] = S
+    return o, final
+
+
+def decay_attention_grad(q, k, v, log_decay, d_o, scale=1.0, initial=None, lengths=None, d_final=None):
+    """Gradients of sum(o d_o) + sum(final d_final): (dq, dk, dv, dinitial)."""
+    q, k, v, log_decay, d_o, initial, d_final = _f64(q, k, v, log_decay, d_o, initial, d_final)
+    B, T, H, dv = v.shape
+    heads, group = q.shape[2], H // q.shape[2]
+    q, k, g = _shared(q, H), _shared(k, H), np.exp(log_decay)[:, None, None]
+    dq, dk, dv_, di = np.zeros_like(q), np.zeros_like(k), np.zeros_like(v), np.zeros((B, H, q.shape[-1], dv))
+    for b, n in enumerate(_ends(lengths, B, T)):
+        S = np.zeros_like(di[b]) if initial is None else initial[b]
+        for t in range(n):
+            S = g * S + k[b, t, :, :, None] * v[b, t, :, None, :]
+            dq[b, t] = scale * (S * d_o[b, t, :, None, :]).sum(2)
+        D = np.zeros_like(di[b]) if d_final is None else d_final[b].copy()
+        for t in reversed(range(n)):
+            D = D + scale * q[b, t, :, :, None] * d_o[b, t, :, None, :]
+            dk[b, t] = (D * v[b, t, :, None, :]).sum(2)
+            dv_[b, t] = (D * k[b, t, :, :, None]).sum(1)
+            D = g * D
+        di[b] = D
+    dq, dk = (x.reshape(B, T, heads, group, -1).sum(3) for x in (dq, dk))
+    return dq, dk, dv_, di
 
 
 # ------------------------------------------------------------------------------------ projection

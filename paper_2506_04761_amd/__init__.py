@@ -15,8 +15,11 @@ from ._lib import (  # noqa: F401
     log_linear_mamba2,
 )
 from ._layer import (  # noqa: F401
-    LL_ACT_NONE, LL_ACT_SILU, ConvGrads, NormGrads, ProjectionGrads, ScanGrads, ll_causal_conv_bwd, ll_causal_conv_bwd_workspace,
-    ll_causal_conv_fwd, ll_causal_conv_step, ll_group_norm_bwd, ll_group_norm_fwd, ll_group_norm_stats,
-    ll_group_norm_workspace, ll_projection_bwd, ll_projection_fwd, ll_projection_workspace, ll_selective_scan_bwd, ll_selective_scan_fwd, ll_selective_scan_states,
-    ll_selective_scan_step, ll_selective_scan_workspace, causal_conv, group_norm, projection, selective_scan,
+    LL_ACT_NONE, LL_ACT_SILU, ConvGrads, DecayGrads, NormGrads, ProjectionGrads, ScanGrads, ll_causal_conv_bwd,
+    ll_causal_conv_bwd_workspace, ll_causal_conv_fwd, ll_causal_conv_step, ll_decay_attention_bwd,
+    ll_decay_attention_fwd, ll_decay_attention_states, ll_decay_attention_step, ll_decay_attention_workspace,
+    ll_group_norm_bwd, ll_group_norm_fwd, ll_group_norm_stats, ll_group_norm_workspace, ll_projection_bwd,
+    ll_projection_fwd, ll_projection_workspace, ll_selective_scan_bwd, ll_selective_scan_fwd, ll_selective_scan_states,
+    ll_selective_scan_step, ll_selective_scan_workspace, causal_conv, decay_attention, group_norm, projection,
+    selective_scan,
 )

@@ -1,0 +1,654 @@
+// Linear attention with a fixed decay g_h for each head, over a state of d_k x d_v a head:
+//   S_t = g S_(t-1) + k_t v_t^T,   o_t = scale S_t^T q_t.
+// Chunks of C tokens from the state S before them, with i, j the tokens of a chunk:
+//   o_i = scale (g^(i+1) S^T q_i + sum_{j <= i} g^(i-j) (q_i . k_j) v_j),   S' = g^C S + sum_j g^(C-1-j) k_j v_j^T.
+// The gradients are the same sums of other operands: with D_t = dL/dS_t,
+//   dq_t = scale S_t do_t                                  queries do, keys v, values k, over the transposed states
+//   dk_t = D_t v_t,  dv_t = D_t^T k_t                      in reversed time: queries v, keys do, values q, and k, q, do
+//   D_t = g D_(t+1) + scale q_t do_t^T                     the gradient of the final state enters without a decay
+// so one kernel, k_attend, serves all.  The length is split into segments where batch and heads are few: their own sums
+// come first (k_attend with STATE), are joined in order (k_join), and every segment starts from its state.
+//
+// Everything is computed transposed: P^T = K Q^T, O^T = S^T Q^T + V^T P^T, S += K^T V.  A result of one matrix instruction
+// then is an operand of the next as the lanes hold it (P^T through LDS, where other waves read it; S in place), since a
+// contraction only needs both operands to agree on which k a slot stands for.
+#include "ll_layer.hpp"
+#include "ll_layer_device.hpp"
+
+namespace ll {
+
+namespace {
+
+// Fragments of 16 bytes: lane (g, i) holds KF / 4 contracted values from KF / 4 * g on, of row i.
+template <typename T>
+struct Op;
+template <>
+struct Op<__bf16> {
+  static constexpr int KF = 32, C = 64;
+  typedef bf16x8 Frag;
+  __device__ static inline f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Op<float> {
+  static constexpr int KF = 16, C = 32;
+  typedef f32x4 Frag;
+  __device__ static inline f32x4 mma(Frag a, Frag b, f32x4 c) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[r], b[r], c, 0, 0, 0);
+    return c;
+  }
+};
+
+// Row i of result t that becomes an operand: results (two of bf16, one of fp32) fill a fragment's slots, so that those of
+// lane group g are KF / 4 adjacent rows.
+template <typename T>
+__device__ inline int row_of(int t, int i) {
+  return sizeof(T) == 2 ? 32 * (t >> 1) + 8 * (i >> 2) + 4 * (t & 1) + (i & 3) : 16 * t + i;
+}
+
+// An LDS tile of rows of W elements: chunk c of 16 bytes at c ^ key(row).  The keys keep apart, over the 256 bytes that
+// the banks span, what is read at once: a chunk of 8 rows (0 - 7, or 0 - 3 and 8 - 11), four chunks of four rows, and
+// (fp32) 16 columns of four rows 4 apart.
+template <typename T, int W>
+struct Tile {
+  static constexpr int E = 16 / sizeof(T), CH = W / E;
+  __device__ static inline int key(int row) {
+    if (sizeof(T) == 4) return (((row >> 2) & 3) << 2 | (row & 3)) & (CH - 1);
+    const int b = ((row >> 2) ^ (row >> 3)) & 1;
+    return CH == 8 ? ((row >> 1) & 1) << 2 | b : (row & 3) << 2 | b;
+  }
+  __device__ static inline int at(int row, int c) { return (row * CH + (c ^ key(row))) * E; }
+  // Fragment ks along the row.
+  __device__ static inline typename Op<T>::Frag along(const T* s, int row, int ks, int lane) {
+    return *reinterpret_cast<const typename Op<T>::Frag*>(s + at(row, 4 * ks + (lane >> 4)));
+  }
+  // Fragment u down the rows, of column `col` of lane i (four adjacent ones of lanes 4 n .. 4 n + 3; the caller gives
+  // the first of lane i & 3's four for bf16, the lane's own for fp32).
+  __device__ static inline typename Op<T>::Frag down(const T* s, int u, int col, int lane) {
+    const int g = lane >> 4, i = lane & 15;
+    if constexpr (sizeof(T) == 2) {
+      const int row = 32 * u + 8 * g + (i >> 2);
+      const bf16x4 lo = lds_read_tr(s + at(row, col >> 3) + (col & 7));
+      const bf16x4 hi = lds_read_tr(s + at(row + 4, col >> 3) + (col & 7));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      f32x4 f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) f[r] = s[at(16 * u + 4 * g + r, col >> 2) + (col & 3)];
+      return f;
+    }
+  }
+};
+
+// A tensor [B, T, heads, width] whose heads are adjacent: `group` heads of the call share one of it.
+struct Heads {
+  const void* p;
+  int64_t sb, st;
+  int width, group;
+  bool vec;  // rows of whole, aligned 16-byte vectors
+};
+
+struct DecayDev {
+  Heads a, b, c;         // queries and keys of d1 elements, values of d2
+  void* out;             // [B, T, H, d2] in the storage type, or fp32 (wide)
+  const float* first;    // states at the segments' starts, [B, H, S, rows, cols]; may be null: zeros
+  float* last;           // STATE: as first; else the final state [B, H, rows, cols]; may be null
+  const float* log_decay;
+  const int32_t* lengths;
+  int64_t T, L;          // L: tokens of a segment
+  int H, S, blocks;      // blocks: workgroups over d2
+  int64_t groups;        // workgroups
+  float in_scale, out_scale;  // of keys times values, of results
+  bool transposed;       // states are [d2, d1]
+  bool reversed, wide, vec_out;
+};
+
+__device__ inline int64_t live_tokens(const int32_t* lengths, int64_t b, int64_t T) {
+  if (!lengths) return T;
+  const int64_t n = lengths[b];
+  return n < 0 ? 0 : (n < T ? n : T);
+}
+// log2 of a head's decay, finite so that its zeroth power is 1.
+__device__ inline float log2_decay(const float* log_decay, int h) {
+  const float v = log_decay[h] * kLog2e;
+  return v < -1e30f ? -1e30f : v;
+}
+
+// Copies a chunk of rows of up to W elements to LDS through registers: rows of other tokens and elements beyond the
+// width are zeros.
+template <typename T, int W>
+struct Chunk {
+  typedef Tile<T, W> Tl;
+  typedef typename VecN<T, Tl::E>::type Vec;
+  static constexpr int E = Tl::E, C = Op<T>::C, ITS = C * Tl::CH / 256;
+  Vec held[ITS];
+  // `p`: element (0, col0) of the first token, `step` elements between tokens, `n` live ones
+  __device__ inline void load(const T* p, int64_t step, int64_t n, int left, bool vec) {
+#pragma unroll
+    for (int it = 0; it < ITS; ++it) {
+      const int q = it * 256 + threadIdx.x, row = q / Tl::CH, c = q % Tl::CH;
+      const int k = left - c * E;
+      held[it] = load_n<T, E>(p + row * step + c * E, row >= n || k <= 0 ? 0 : (k < E ? k : E), vec);
+    }
+  }
+  __device__ inline void store(T* s) const {
+#pragma unroll
+    for (int it = 0; it < ITS; ++it) {
+      const int q = it * 256 + threadIdx.x;
+      *reinterpret_cast<Vec*>(s + Tl::at(q / Tl::CH, q % Tl::CH)) = held[it];
+    }
+  }
+};
+
+template <typename T>
+__device__ inline typename Op<T>::Frag pack(const f32x4* v);
+template <>
+__device__ inline bf16x8 pack<__bf16>(const f32x4* v) {
+  bf16x8 f;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) f[r] = static_cast<__bf16>(v[0][r]), f[4 + r] = static_cast<__bf16>(v[1][r]);
+  return f;
+}
+template <>
+__device__ inline f32x4 pack<float>(const f32x4* v) {
+  return v[0];
+}
+
+// One segment of one head, 64 NV values a workgroup: a wave holds the state's rows of its 16 NV columns.  d1 <= DK.
+template <typename T, int DK, int NV, bool STATE>
+__global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
+  constexpr int KF = Op<T>::KF, C = Op<T>::C, E = 16 / sizeof(T), R = KF / 16, QT = C / 16, US = C / KF, KS = DK / KF, DT = DK / 16;
+  constexpr int DV = 64 * NV;
+  typedef typename Op<T>::Frag Frag;
+  typedef Tile<T, DK> TlK;
+  typedef Tile<T, DV> TlV;
+  __shared__ __attribute__((aligned(1024))) T sk[C * DK];
+  __shared__ __attribute__((aligned(1024))) T sv[C * DV];
+  __shared__ __attribute__((aligned(1024))) T sq[STATE ? 8 : C * DK];
+  __shared__ Frag sp[STATE ? 1 : QT][US][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i = lane & 15;
+
+  int64_t id = xcd_remap(blockIdx.x, p.groups);
+  const int blk = int(id % p.blocks);
+  id /= p.blocks;
+  const int seg = int(id % (STATE ? p.S - 1 : p.S));
+  id /= STATE ? p.S - 1 : p.S;
+  const int h = int(id % p.H);
+  const int64_t b = id / p.H;
+  const int d1 = p.a.width, d2 = p.c.width, col0 = blk * DV;
+  const int64_t live = live_tokens(p.lengths, b, p.T), t0 = seg * p.L;
+  int64_t n = live - t0 < p.L ? live - t0 : p.L;  // tokens of this segment
+  n = n < 0 ? 0 : n;
+  const float lg = log2_decay(p.log_decay, h);
+  const int rho = p.reversed ? 1 : 0;
+
+  // the wave's columns: value tile v, lane i
+  const int wcol = 16 * NV * wave;
+  auto vcol = [&](int v, int x) { return wcol + (NV == 2 ? 8 * (x >> 2) + 4 * v + (x & 3) : x); };
+
+  f32x4 S[DT][NV] = {};
+  if (!STATE && p.first && n > 0) {
+    const float* f = p.first + ((b * p.H + h) * p.S + seg) * int64_t(d1) * d2;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int row = row_of<T>(t, 4 * g + r), col = col0 + vcol(v, i);
+          if (row < d1 && col < d2) S[t][v][r] = f[p.transposed ? int64_t(col) * d1 + row : int64_t(row) * d2 + col];
+        }
+  }
+
+  // tokens by their order in time: the first of the segment, and the step between two
+  const int64_t tok = p.reversed ? live - 1 - t0 : t0, dir = p.reversed ? -1 : 1;
+  const T* kp = static_cast<const T*>(p.b.p) + b * p.b.sb + tok * p.b.st + (h / p.b.group) * d1;
+  const T* vp = static_cast<const T*>(p.c.p) + b * p.c.sb + tok * p.c.st + (h / p.c.group) * d2 + col0;
+  const T* qp = static_cast<const T*>(p.a.p) + b * p.a.sb + tok * p.a.st + (h / p.a.group) * d1;
+  const int64_t ks_ = dir * p.b.st, vs_ = dir * p.c.st, qs_ = dir * p.a.st;
+  Chunk<T, DK> ck, cq;
+  Chunk<T, DV> cv;
+  if (n > 0) {
+    ck.load(kp, ks_, n, d1, p.b.vec);
+    cv.load(vp, vs_, n, d2 - col0, p.c.vec);
+    if (!STATE) cq.load(qp, qs_, n, d1, p.a.vec);
+  }
+  for (int64_t c0 = 0; c0 < n; c0 += C) {
+    const int m = n - c0 < C ? int(n - c0) : C;  // tokens of this chunk
+    ck.store(sk);
+    cv.store(sv);
+    if (!STATE) cq.store(sq);
+    __syncthreads();
+    if (c0 + C < n) {
+      const int64_t at = c0 + C, more = n - at;
+      ck.load(kp + at * ks_, ks_, more, d1, p.b.vec);
+      cv.load(vp + at * vs_, vs_, more, d2 - col0, p.c.vec);
+      if (!STATE) cq.load(qp + at * qs_, qs_, more, d1, p.a.vec);
+    }
+    Frag vf[NV][US];
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int u = 0; u < US; ++u) vf[v][u] = TlV::down(sv, u, sizeof(T) == 2 ? vcol(v, 4 * (i & 3)) : vcol(v, i), lane);
+
+    if constexpr (!STATE) {
+      // P^T of 16 queries and the keys up to them
+      {
+        const int qt = wave % QT;
+        for (int u = wave / QT; u < US; u += 4 / QT) {
+          if (u * KF > 16 * qt + 15) continue;
+          f32x4 pt[R] = {};
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            const Frag q = TlK::along(sq, 16 * qt + i, ks, lane);
+#pragma unroll
+            for (int r = 0; r < R; ++r) pt[r] = Op<T>::mma(TlK::along(sk, row_of<T>(R * u + r, i), ks, lane), q, pt[r]);
+          }
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int gap = 16 * qt + i - row_of<T>(R * u + r, 4 * g + e);
+              pt[r][e] = gap >= 0 ? pt[r][e] * (p.in_scale * fast_exp2(lg * float(gap))) : 0.0f;
+            }
+          sp[qt][u][lane] = pack<T>(pt);
+        }
+      }
+      f32x4 o[QT][NV] = {};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        Frag s[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          f32x4 x[R];
+#pragma unroll
+          for (int r = 0; r < R; ++r) x[r] = S[R * ks + r][v];
+          s[v] = pack<T>(x);
+        }
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+          const Frag q = TlK::along(sq, 16 * qt + i, ks, lane);
+#pragma unroll
+          for (int v = 0; v < NV; ++v) o[qt][v] = Op<T>::mma(s[v], q, o[qt][v]);
+        }
+      }
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) {
+        const float w = fast_exp2(lg * float(16 * qt + i + 1 - rho));
+#pragma unroll
+        for (int v = 0; v < NV; ++v) o[qt][v] *= w;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+        for (int u = 0; u < US; ++u) {
+          if (u * KF > 16 * qt + 15) continue;
+          const Frag pf = sp[qt][u][lane];
+#pragma unroll
+          for (int v = 0; v < NV; ++v) o[qt][v] = Op<T>::mma(vf[v][u], pf, o[qt][v]);
+        }
+#pragma unroll
+      for (int qt = 0; qt < QT; ++qt) {
+        const int row = 16 * qt + i, col = col0 + wcol + 4 * NV * g;
+        if (row >= m || col >= d2) continue;
+        float f[4 * NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) f[4 * v + r] = o[qt][v][r] * p.out_scale;
+        const int64_t e = ((b * p.T + tok + dir * (c0 + row)) * p.H + h) * d2 + col;
+        const int count = d2 - col < 4 * NV ? d2 - col : 4 * NV;
+        if (p.wide) store_n<float, 4 * NV>(static_cast<float*>(p.out) + e, f, count, false);
+        else store_n<T, 4 * NV>(static_cast<T*>(p.out) + e, f, count, p.vec_out);
+      }
+    }
+
+    // the state after the chunk; values times powers of the decay in three bf16 parts, which hold all of fp32's bits
+    const float carry = fast_exp2(lg * float(m));
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int v = 0; v < NV; ++v) S[t][v] *= carry;
+#pragma unroll
+    for (int u = 0; u < US; ++u) {
+      constexpr int PARTS = sizeof(T) == 2 ? 3 : 1;
+      Frag part[NV][PARTS];
+#pragma unroll
+      for (int x = 0; x < KF / 4; ++x) {
+        const int left = m - 1 - (KF * u + KF / 4 * g + x);
+        const float w = left >= 0 ? p.in_scale * fast_exp2(lg * float(left + rho)) : 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          float f = to_f32(T(vf[v][u][x])) * w;
+#pragma unroll
+          for (int k = 0; k < PARTS; ++k) {
+            const T y = from_f32<T>(f);
+            part[v][k][x] = y;
+            f -= to_f32(y);
+          }
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        const Frag k = TlK::down(sk, u, sizeof(T) == 2 ? row_of<T>(t, 4 * (i & 3)) : row_of<T>(t, i), lane);
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int x = 0; x < PARTS; ++x) S[t][v] = Op<T>::mma(k, part[v][x], S[t][v]);
+      }
+    }
+    __syncthreads();
+  }
+
+  // STATE: this segment's own sums, where the next one starts.  Else the final state, of the segment that ends there.
+  float* to = nullptr;
+  if (STATE) to = p.last + ((b * p.H + h) * p.S + seg + 1) * int64_t(d1) * d2;
+  else if (p.last && seg == (live > 0 ? (live - 1) / p.L : 0)) to = p.last + (b * p.H + h) * int64_t(d1) * d2;
+  if (to) {
+    const bool keep = !STATE && n == 0 && p.first;  // an empty sequence ends where it begins
+    const float* f = p.first + (b * p.H + h) * p.S * int64_t(d1) * d2;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int row = row_of<T>(t, 4 * g + r), col = col0 + vcol(v, i);
+          if (row < d1 && col < d2) {
+            const int64_t e = p.transposed ? int64_t(col) * d1 + row : int64_t(row) * d2 + col;
+            to[e] = keep ? f[e] : S[t][v][r];
+          }
+        }
+  }
+  // rows after the sequence's end
+  if (!STATE) {
+    const int64_t end = t0 + p.L < p.T ? t0 + p.L : p.T, from = live > t0 ? live : t0;
+    const int cols = d2 - col0 < DV ? d2 - col0 : DV;
+    for (int64_t q = threadIdx.x; q < (end - from) * cols; q += 256) {
+      const int64_t e = ((b * p.T + from + q / cols) * p.H + h) * d2 + col0 + q % cols;
+      if (p.wide) static_cast<float*>(p.out)[e] = 0.0f;
+      else static_cast<T*>(p.out)[e] = from_f32<T>(0.0f);
+    }
+  }
+}
+
+// The states at the segments' starts, in place of the segments' own sums: h_0 = first, h_(s+1) = g^(n_s) h_s + u_s.
+__global__ __launch_bounds__(256) void k_join(float* h, const float* first, const float* log_decay, const int32_t* lengths,
+                                              int64_t T, int64_t L, int H, int S, int64_t size, int64_t total) {
+  const int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (id >= total) return;
+  const int64_t bh = id / size, e = id % size;
+  const int64_t live = live_tokens(lengths, bh / H, T);
+  const float lg = log2_decay(log_decay, int(bh % H));
+  float* p = h + bh * S * size + e;
+  float v = first ? first[id] : 0.0f;
+  p[0] = v;
+  const float w = fast_exp2(lg * float(L));  // a segment with one after it is whole
+#pragma unroll 4
+  for (int s = 1; s < S; ++s) {
+    if (s * L >= live) break;
+    v = fmaf(w, v, p[s * size]);
+    p[s * size] = v;
+  }
+}
+
+// One token of 256 / LV rows at a time: o = scale (g S + k v^T)^T q, the state passed through.
+struct StepDev {
+  Heads q, k, v;
+  const float* state;
+  float* next;
+  void* out;
+  const float* log_decay;
+  int H, dk, dv;
+  float scale;
+  bool vec;
+};
+template <typename T, int LV>
+__global__ __launch_bounds__(256) void k_decay_step(StepDev p) {
+  constexpr int RS = 256 / LV;
+  __shared__ float s[RS][LV][5];
+  const int c = threadIdx.x % LV, r0 = threadIdx.x / LV;
+  const int64_t bh = blockIdx.x, b = bh / p.H;
+  const int h = int(bh % p.H);
+  const int col = 4 * c, count = p.dv - col < 4 ? (p.dv > col ? p.dv - col : 0) : 4;
+  const T* q = static_cast<const T*>(p.q.p) + b * p.q.sb + (h / p.q.group) * p.dk;
+  const T* k = static_cast<const T*>(p.k.p) + b * p.k.sb + (h / p.k.group) * p.dk;
+  const T* v = static_cast<const T*>(p.v.p) + b * p.v.sb + h * p.dv + col;
+  const float decay = fast_exp2(log2_decay(p.log_decay, h));
+  const auto vr = load_n<T, 4>(v, count, false);
+  float vf[4], o[4] = {};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) vf[i] = to_f32(T(vr[i]));
+  const int64_t base = bh * p.dk * p.dv + col;
+  if (count > 0) {
+    // rows are loaded ahead of the stores, which could be the same memory
+    constexpr int U = 8;
+    for (int r = r0; r < p.dk; r += U * RS) {
+      typename VecN<float, 4>::type st[U];
+      float kr[U], qr[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int at = r + u * RS, n = at < p.dk ? count : 0;
+        st[u] = load_n<float, 4>(p.state + base + int64_t(at) * p.dv, n, p.vec);
+        kr[u] = n ? to_f32(k[at]) : 0.0f, qr[u] = n ? to_f32(q[at]) : 0.0f;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[i] = fmaf(decay, st[u][i], kr[u] * vf[i]);
+          o[i] = fmaf(qr[u], x[i], o[i]);
+        }
+        store_n<float, 4>(p.next + base + int64_t(r + u * RS) * p.dv, x, r + u * RS < p.dk ? count : 0, p.vec);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s[r0][c][i] = o[i];
+  __syncthreads();
+  for (int e = threadIdx.x; e < p.dv; e += 256) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < RS; ++r) sum += s[r][e / 4][e % 4];
+    static_cast<T*>(p.out)[bh * p.dv + e] = from_f32<T>(p.scale * sum);
+  }
+}
+
+// Gradients of shared heads: the sum of each group's, in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void k_group_sum(const float* x, void* out, int group, int width, int64_t total) {
+  const int64_t id = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (id >= total) return;
+  const float* q = x + id / width * group * width + id % width;
+  float v = 0.0f;
+#pragma unroll 4
+  for (int i = 0; i < group; ++i) v += q[int64_t(i) * width];
+  static_cast<T*>(out)[id] = from_f32<T>(v);
+}
+
+// ------------------------------------------------------------------------------------ plans
+
+int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
+
+struct Split {
+  int64_t L, S;
+};
+// Segments of whole chunks: enough for 1024 workgroups of a head each, of 512 tokens at least.
+Split split_of(int64_t B, int64_t T, int64_t H) {
+  int64_t S = ceil_div(1024, B * H);
+  S = S < T / 512 ? S : T / 512;
+  S = S < 1 ? 1 : S;
+  Split q;
+  q.L = ceil_div(ceil_div(T, S), 64) * 64;
+  q.S = ceil_div(T, q.L);
+  return q;
+}
+
+int64_t state_bytes(const DecayArgs& a) { return a.B * a.H * a.dk * a.dv * 4; }
+
+Heads heads_of(const Rows& r, int64_t heads, int64_t H, int64_t width, int esize) {
+  const int n = 16 / esize;
+  return {r.p, r.sb, r.st, int(width), int(H / heads), rows_aligned(r, esize, n) && width % n == 0};
+}
+
+int value_tiles(int64_t d1, int64_t d2) { return d1 <= 128 && d2 > 64 ? 2 : 1; }
+
+template <typename T, int DK, int NV>
+hipError_t launch_attend(const DecayDev& p, bool state, hipStream_t st) {
+  const dim3 grid(uint32_t(p.groups)), block(256);
+  if (state) k_attend<T, DK, NV, true><<<grid, block, 0, st>>>(p);
+  else k_attend<T, DK, NV, false><<<grid, block, 0, st>>>(p);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t attend(DecayDev p, int64_t B, bool state, hipStream_t st) {
+  const int nv = value_tiles(p.a.width, p.c.width);
+  p.blocks = int(ceil_div(p.c.width, 64 * nv));
+  p.groups = B * p.H * p.blocks * (state ? p.S - 1 : p.S);
+  p.vec_out = p.c.width % (4 * nv) == 0 && reinterpret_cast<uintptr_t>(p.out) % (4 * nv * sizeof(T)) == 0;
+  if (p.a.width <= 64) return nv == 2 ? launch_attend<T, 64, 2>(p, state, st) : launch_attend<T, 64, 1>(p, state, st);
+  if (p.a.width <= 128) return nv == 2 ? launch_attend<T, 128, 2>(p, state, st) : launch_attend<T, 128, 1>(p, state, st);
+  return launch_attend<T, 256, 1>(p, state, st);
+}
+
+// The states at the segments' starts into `h`: the segments' own sums, then their join.
+template <typename T>
+hipError_t states(DecayDev p, int64_t B, float* h, const float* first, hipStream_t st) {
+  hipError_t e = hipSuccess;
+  p.last = h, p.first = nullptr;
+  if (p.S > 1) e = attend<T>(p, B, true, st);
+  if (e != hipSuccess) return e;
+  const int64_t size = int64_t(p.a.width) * p.c.width, total = B * p.H * size;
+  k_join<<<dim3(uint32_t(ceil_div(total, 256))), dim3(256), 0, st>>>(h, first, p.log_decay, p.lengths, p.T, p.L, p.H, p.S,
+                                                                     size, total);
+  return hipGetLastError();
+}
+
+DecayDev common(const DecayArgs& a, const Split& s) {
+  DecayDev p = {};
+  p.log_decay = a.log_decay, p.lengths = a.lengths, p.T = a.T, p.L = s.L, p.H = int(a.H), p.S = int(s.S);
+  p.in_scale = 1.0f, p.out_scale = 1.0f;
+  return p;
+}
+
+template <typename T>
+hipError_t fwd(const DecayArgs& a, hipStream_t st) {
+  const Split s = split_of(a.B, a.T, a.H);
+  DecayDev p = common(a, s);
+  p.a = heads_of(a.q, a.Hqk, a.H, a.dk, sizeof(T)), p.b = heads_of(a.k, a.Hqk, a.H, a.dk, sizeof(T));
+  p.c = heads_of(a.v, a.H, a.H, a.dv, sizeof(T));
+  p.out = a.o, p.out_scale = a.scale;
+  const float* first = a.initial;
+  if (a.states || s.S > 1) {
+    float* h = a.states ? a.states : static_cast<float*>(a.workspace);
+    const hipError_t e = states<T>(p, a.B, h, a.initial, st);
+    if (e != hipSuccess) return e;
+    first = h;
+  }
+  p.first = first, p.last = a.final_state;
+  return attend<T>(p, a.B, false, st);
+}
+
+struct BwdPlan {
+  Split s;
+  int64_t o_states = 0, o_wide = 0, total = 0;  // reversed states; fp32 gradients of shared heads
+};
+BwdPlan bwd_plan(int64_t B, int64_t T, int64_t H, int64_t Hqk, int64_t dk, int64_t dv) {
+  BwdPlan q;
+  q.s = split_of(B, T, H);
+  q.o_wide = q.s.S > 1 ? up256(B * H * dk * dv * 4 * q.s.S) : 0;
+  q.total = q.o_wide + (Hqk < H ? up256(B * T * H * dk * 4) : 0);
+  return q;
+}
+
+template <typename T>
+hipError_t bwd(const DecayArgs& a, const DecayGrads& g, hipStream_t st) {
+  const BwdPlan q = bwd_plan(a.B, a.T, a.H, a.Hqk, a.dk, a.dv);
+  char* ws = static_cast<char*>(a.workspace);
+  const bool shared = a.Hqk < a.H;
+  void* wide = ws + q.o_wide;
+  const Rows dout = {g.d_o, a.T * a.H * a.dv, a.H * a.dv};
+  const Heads hq = heads_of(a.q, a.Hqk, a.H, a.dk, sizeof(T)), hk = heads_of(a.k, a.Hqk, a.H, a.dk, sizeof(T));
+  const Heads hv = heads_of(a.v, a.H, a.H, a.dv, sizeof(T)), hd = heads_of(dout, a.H, a.H, a.dv, sizeof(T));
+  const int64_t n = a.B * a.T * a.Hqk * a.dk;
+  auto group_sum = [&](void* out) {
+    k_group_sum<T><<<dim3(uint32_t(ceil_div(n, 256))), dim3(256), 0, st>>>(static_cast<const float*>(wide), out, int(a.H / a.Hqk),
+                                                                           int(a.dk), n);
+    return hipGetLastError();
+  };
+  const DecayDev base = common(a, q.s);
+  hipError_t e = hipSuccess;
+  {
+    DecayDev p = base;
+    p.a = hd, p.b = hv, p.c = hk, p.first = a.states, p.transposed = true, p.out_scale = a.scale;
+    p.out = shared ? wide : g.dq, p.wide = shared;
+    e = attend<T>(p, a.B, false, st);
+    if (e == hipSuccess && shared) e = group_sum(g.dq);
+  }
+  DecayDev p = base;  // dv, with the state D
+  p.a = hk, p.b = hq, p.c = hd, p.in_scale = a.scale, p.reversed = true;
+  const float* first = g.d_final;
+  if (e == hipSuccess && q.s.S > 1) {
+    float* h = reinterpret_cast<float*>(ws + q.o_states);
+    e = states<T>(p, a.B, h, g.d_final, st);
+    first = h;
+  }
+  if (e == hipSuccess) {
+    p.first = first, p.last = nullptr, p.out = g.dv;
+    e = attend<T>(p, a.B, false, st);
+  }
+  if (e == hipSuccess) {  // dk, with its transpose
+    p.a = hv, p.b = hd, p.c = hq, p.transposed = true;
+    p.last = g.d_initial, p.out = shared ? wide : g.dk, p.wide = shared;
+    e = attend<T>(p, a.B, false, st);
+    if (e == hipSuccess && shared) e = group_sum(g.dk);
+  }
+  return e;
+}
+
+template <typename T>
+hipError_t step(const DecayArgs& a, hipStream_t st) {
+  StepDev p = {};
+  p.q = heads_of(a.q, a.Hqk, a.H, a.dk, sizeof(T)), p.k = heads_of(a.k, a.Hqk, a.H, a.dk, sizeof(T));
+  p.v = heads_of(a.v, a.H, a.H, a.dv, sizeof(T));
+  p.state = a.initial, p.next = a.final_state, p.out = a.o, p.log_decay = a.log_decay;
+  p.H = int(a.H), p.dk = int(a.dk), p.dv = int(a.dv), p.scale = a.scale;
+  p.vec = a.dv % 4 == 0 && reinterpret_cast<uintptr_t>(a.initial) % 16 == 0 && reinterpret_cast<uintptr_t>(a.final_state) % 16 == 0;
+  const dim3 grid(uint32_t(a.B * a.H)), block(256);
+  if (a.dv <= 64) k_decay_step<T, 16><<<grid, block, 0, st>>>(p);
+  else if (a.dv <= 128) k_decay_step<T, 32><<<grid, block, 0, st>>>(p);
+  else k_decay_step<T, 64><<<grid, block, 0, st>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t decay_states_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv) {
+  return B * H * dk * dv * 4 * split_of(B, T, H).S;
+}
+int64_t decay_workspace(int64_t B, int64_t T, int64_t H, int64_t Hqk, int64_t dk, int64_t dv, bool backward) {
+  const int64_t S = split_of(B, T, H).S, f = S > 1 ? up256(B * H * dk * dv * 4 * S) : 0;
+  if (!backward) return f;
+  const int64_t b = bwd_plan(B, T, H, Hqk, dk, dv).total;
+  return b > f ? b : f;
+}
+bool decay_launchable(const DecayArgs& a, bool backward) {
+  const int64_t S = split_of(a.B, a.T, a.H).S, heads = a.B * a.H;
+  auto blocks = [](int64_t d1, int64_t d2) { return ceil_div(d2, 64 * value_tiles(d1, d2)); };
+  if (!launchable(heads * S * blocks(a.dk, a.dv), 256) || !launchable(ceil_div(heads * a.dk * a.dv, 256), 256)) return false;
+  if (!backward) return true;
+  return launchable(heads * S * blocks(a.dv, a.dk), 256) &&
+         (a.Hqk == a.H || launchable(ceil_div(a.B * a.T * a.Hqk * a.dk, 256), 256));
+}
+bool decay_step_launchable(const DecayArgs& a) { return launchable(a.B * a.H, 256); }
+
+hipError_t launch_decay_fwd(const DecayArgs& a, hipStream_t st) { return a.dtype == 1 ? fwd<__bf16>(a, st) : fwd<float>(a, st); }
+hipError_t launch_decay_bwd(const DecayArgs& a, const DecayGrads& g, hipStream_t st) {
+  return a.dtype == 1 ? bwd<__bf16>(a, g, st) : bwd<float>(a, g, st);
+}
+hipError_t launch_decay_step(const DecayArgs& a, hipStream_t st) { return a.dtype == 1 ? step<__bf16>(a, st) : step<float>(a, st); }
+
+}  // namespace ll

@@ -1,5 +1,5 @@
 // Host-side argument bundles of the operators around a token mixer (short causal convolution,
-// selective state space scan, group norm) and of the projections, shared by their C ABI (ll_layer_api.hip) and kernels.
+// selective state space scan, group norm), of the linear attention with a decay for each head and of the projections, shared by their C ABI (ll_layer_api.hip) and kernels.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -137,6 +137,37 @@ int64_t norm_workspace(int64_t N, int64_t S, int64_t C, int64_t G, int dtype, bo
 bool norm_launchable(const NormArgs& a, bool backward);
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t st);
 hipError_t launch_norm_bwd(const NormArgs& a, const NormGrads& g, hipStream_t st);
+
+// ---- linear attention with a decay for each head
+struct DecayArgs {
+  Rows q, k, v;            // heads adjacent
+  const float* log_decay;
+  const int32_t* lengths;  // may be null
+  int64_t B, T, H, Hqk, dk, dv;
+  float scale;
+  int dtype;
+  const float* initial;    // may be null: zeros
+  float* final_state;      // may be null
+  float* states;           // forward: may be null; backward: the forward's
+  void* o;
+  void* workspace;
+};
+struct DecayGrads {
+  const void* d_o;
+  const float* d_final;    // may be null: zeros
+  void* dq;
+  void* dk;
+  void* dv;
+  float* d_initial;        // may be null
+};
+constexpr int kDecayMaxWidth = 256;
+int64_t decay_states_bytes(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv);
+int64_t decay_workspace(int64_t B, int64_t T, int64_t H, int64_t Hqk, int64_t dk, int64_t dv, bool backward);
+bool decay_launchable(const DecayArgs& a, bool backward);
+bool decay_step_launchable(const DecayArgs& a);
+hipError_t launch_decay_fwd(const DecayArgs& a, hipStream_t st);
+hipError_t launch_decay_bwd(const DecayArgs& a, const DecayGrads& g, hipStream_t st);
+hipError_t launch_decay_step(const DecayArgs& a, hipStream_t st);  // initial -> final_state, one token
 
 // ---- projection
 struct ProjArgs {

@@ -91,6 +91,29 @@ ll_status norm_args(const void* x, int64_t xbs, int64_t xts, const void* gate, i
   return LL_OK;
 }
 
+ll_status decay_sizes(int64_t B, int64_t T, int64_t H, int64_t Hqk, int64_t dk, int64_t dv) {
+  if (H < 1 || Hqk < 1 || dk < 1 || dv < 1 || H % Hqk != 0) return LL_ERR_BAD_SHAPE;
+  if (H >= kMaxChannels || dk > ll::kDecayMaxWidth || dv > ll::kDecayMaxWidth) return LL_ERR_UNSUPPORTED;
+  LL_TRY(check_sizes(B, T, H * (dk > dv ? dk : dv)));
+  return B <= kMaxElements / (H * dk * dv) ? LL_OK : LL_ERR_UNSUPPORTED;
+}
+
+ll_status decay_args(const ll_decay_inputs* in, ll::DecayArgs* a) {
+  if (!in || !in->q || !in->k || !in->v || !in->log_decay) return LL_ERR_NULL_ARG;
+  LL_TRY(decay_sizes(in->batch, in->T, in->heads, in->qk_heads, in->d_k, in->d_v));
+  LL_TRY(check_strides(in->q_strides[0], in->q_strides[1]));
+  LL_TRY(check_strides(in->k_strides[0], in->k_strides[1]));
+  LL_TRY(check_strides(in->v_strides[0], in->v_strides[1]));
+  if (!known_dtype(in->dtype)) return LL_ERR_UNSUPPORTED;
+  a->q = {in->q, in->q_strides[0], in->q_strides[1]};
+  a->k = {in->k, in->k_strides[0], in->k_strides[1]};
+  a->v = {in->v, in->v_strides[0], in->v_strides[1]};
+  a->log_decay = in->log_decay, a->lengths = in->lengths;
+  a->B = in->batch, a->T = in->T, a->H = in->heads, a->Hqk = in->qk_heads, a->dk = in->d_k, a->dv = in->d_v;
+  a->scale = in->scale, a->dtype = in->dtype;
+  return LL_OK;
+}
+
 // x [M, K] and W [N, K] to [M, N].
 ll_status projection_sizes(int64_t M, int64_t K, int64_t N, int32_t act, int32_t dtype) {
   LL_TRY(check_sizes(M, 1, K));
@@ -231,6 +254,54 @@ ll_status ll_group_norm_bwd(const void* x, int64_t x_batch_stride, int64_t x_tok
   a.weight = weight, a.bias = bias, a.stats = const_cast<float*>(stats), a.workspace = workspace;
   const ll::NormGrads g = {d_y, dx, gate ? dgate : nullptr, dweight, dbias};
   return launched(ll::launch_norm_bwd(a, g, static_cast<hipStream_t>(stream)));
+}
+
+size_t ll_decay_attention_workspace_size(int64_t B, int64_t T, int64_t H, int64_t H_qk, int64_t d_k, int64_t d_v,
+                                         int32_t backward) {
+  if (decay_sizes(B, T, H, H_qk, d_k, d_v) != LL_OK) return 0;
+  return (size_t)ll::decay_workspace(B, T, H, H_qk, d_k, d_v, backward != 0);
+}
+
+size_t ll_decay_attention_states_bytes(int64_t B, int64_t T, int64_t H, int64_t d_k, int64_t d_v) {
+  return decay_sizes(B, T, H, H, d_k, d_v) == LL_OK ? (size_t)ll::decay_states_bytes(B, T, H, d_k, d_v) : 0;
+}
+
+ll_status ll_decay_attention_fwd(const ll_decay_inputs* in, const float* initial_state, void* o, float* final_state,
+                                 float* states, void* workspace, size_t workspace_bytes, void* stream) {
+  ll::DecayArgs a = {};
+  LL_TRY(decay_args(in, &a));
+  if (!o) return LL_ERR_NULL_ARG;
+  if (!ll::decay_launchable(a, false)) return LL_ERR_UNSUPPORTED;
+  // states of the caller's serve as workspace
+  if (!states) LL_TRY(check_workspace(workspace, workspace_bytes, ll::decay_workspace(a.B, a.T, a.H, a.Hqk, a.dk, a.dv, false)));
+  if (!aligned(states, 16)) return LL_ERR_WORKSPACE;
+  a.initial = initial_state, a.final_state = final_state, a.states = states, a.o = o, a.workspace = workspace;
+  return launched(ll::launch_decay_fwd(a, static_cast<hipStream_t>(stream)));
+}
+
+ll_status ll_decay_attention_step(const ll_decay_inputs* in, const float* state, float* new_state, void* o,
+                                  void* stream) {
+  ll::DecayArgs a = {};
+  LL_TRY(decay_args(in, &a));
+  if (!state || !new_state || !o) return LL_ERR_NULL_ARG;
+  if (a.T != 1 || a.lengths) return LL_ERR_BAD_SHAPE;
+  if (!ll::decay_step_launchable(a)) return LL_ERR_UNSUPPORTED;
+  a.initial = state, a.final_state = new_state, a.o = o;
+  return launched(ll::launch_decay_step(a, static_cast<hipStream_t>(stream)));
+}
+
+ll_status ll_decay_attention_bwd(const ll_decay_inputs* in, const float* states, const void* d_o,
+                                 const float* d_final_state, void* dq, void* dk, void* dv, float* d_initial_state,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+  ll::DecayArgs a = {};
+  LL_TRY(decay_args(in, &a));
+  if (!states || !d_o || !dq || !dk || !dv) return LL_ERR_NULL_ARG;
+  if (!ll::decay_launchable(a, true)) return LL_ERR_UNSUPPORTED;
+  LL_TRY(check_workspace(workspace, workspace_bytes, ll::decay_workspace(a.B, a.T, a.H, a.Hqk, a.dk, a.dv, true)));
+  if (!aligned(states, 16)) return LL_ERR_WORKSPACE;
+  a.states = const_cast<float*>(states), a.workspace = workspace;
+  const ll::DecayGrads g = {d_o, d_final_state, dq, dk, dv, d_initial_state};
+  return launched(ll::launch_decay_bwd(a, g, static_cast<hipStream_t>(stream)));
 }
 
 size_t ll_projection_workspace_size(int32_t dtype, int64_t M, int64_t K, int64_t N, int32_t act, int32_t backward) {

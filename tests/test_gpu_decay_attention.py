@@ -1,0 +1,321 @@
+"""Linear attention with a decay for each head, on the GPU against the float64 oracle: prompts, gradients, single tokens;
+lengths from none to several chunks and segments, odd head sizes, shared query/key heads, columns of wider rows at any
+start, sequences that end early with NaN behind their ends, states continued in place, decays from none to all.
+
+Tolerances are bounds, element by element.  With e = 2^-8 (bf16) or 2^-24 (fp32), half a step of the storage type, and A
+the same sums of absolute values:
+  sums and decays  (2 T + 64) 2^-24 A: a rounding for each token's product and sum, the powers' own (their exponents are
+                   off by 2^-23 of themselves, which matters while a power is not small), and a chunk's few
+  bf16 products    2^-8 A: scores and states enter them rounded once
+  results          e |want|, but states and their gradients are fp32 in either case, of products that keep fp32's bits"""
+
+import numpy as np
+import pytest
+
+from oracle import layer
+from tests.gpu_util import to_dev
+
+pytestmark = pytest.mark.gpu
+
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _device():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2506_04761_amd  # noqa: F401  (fails loudly if the library is missing)
+
+
+def _np(t):
+    return None if t is None else t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def _within(got, want, bound, dtype, T, name, state=False):
+    got = _np(got)
+    assert got.shape == want.shape, (name, got.shape)
+    tol = (2 * T + 64) * 2.0 ** -24 * bound
+    if not state:
+        tol += (HALF["bf16"] * bound if dtype == "bf16" else 0) + HALF[dtype] * (np.abs(want) + tol)
+    bad = ~(np.abs(got - want) <= tol + 1e-36)
+    assert not bad.any(), (name, int(bad.sum()), float(np.nanmax(np.abs(got - want) / (tol + 1e-36))))
+
+
+def _ends(ns):
+    import torch
+    return None if ns is None else torch.tensor(ns, dtype=torch.int32, device="cuda")
+
+
+class _Case:
+    def __init__(self, seed, B, T, H, Hqk, dk, dv, dtype, ends=None, off=None, decays=None, state=True):
+        import torch
+        r = np.random.default_rng(seed)
+        self.T, self.dtype, self.scale = T, dtype, 0.37
+        n = 2 * Hqk * dk + H * dv
+        pad = 0 if off is None else off + 5
+        rows = to_dev(r.standard_normal((B, T, n + pad)), dtype)
+        if ends is not None:
+            for b, e in enumerate(ends):
+                rows[b, e:] = float("nan")
+        lo = 0 if off is None else off
+        self.q = rows[..., lo:lo + Hqk * dk].unflatten(-1, (Hqk, dk))
+        self.k = rows[..., lo + Hqk * dk:lo + 2 * Hqk * dk].unflatten(-1, (Hqk, dk))
+        self.v = rows[..., lo + 2 * Hqk * dk:lo + n].unflatten(-1, (H, dv))
+        self.ld = to_dev(-np.exp2(r.uniform(-9, -2, H)) if decays is None else np.resize(decays, H))
+        self.initial = to_dev(r.standard_normal((B, H, dk, dv))) if state else None
+        self.d_final = to_dev(r.standard_normal((B, H, dk, dv))) if state else None
+        self.d_o = to_dev(r.standard_normal((B, T, H, dv)), dtype)
+        if ends is not None:
+            for b, e in enumerate(ends):
+                self.d_o[b, e:] = float("nan")
+        self.ends, self.lengths = ends, _ends(ends)
+        self.q, self.k = self.q.detach(), self.k.detach()
+        assert torch.is_tensor(self.v)
+
+    def run(self):
+        """(o, final state, gradients) into memory full of NaN."""
+        import paper_2506_04761_amd as ll
+        import torch
+        nan = float("nan")
+        out = torch.full(self.v.shape, nan, device="cuda", dtype=self.v.dtype)
+        final = torch.full((self.v.shape[0], self.v.shape[2], self.q.shape[3], self.v.shape[3]), nan, device="cuda")
+        states = ll.ll_decay_attention_states(self.q, self.v)
+        states.fill_(255)
+        ws = ll.ll_decay_attention_workspace(self.q, self.v, backward=True)
+        ws.fill_(255)
+        a = (self.q, self.k, self.v, self.ld)
+        ll.ll_decay_attention_fwd(*a, self.scale, self.initial, final, self.lengths, states, out, ws)
+        plain = ll.ll_decay_attention_fwd(*a, self.scale, self.initial, None, self.lengths)
+        assert torch.equal(plain, out)
+        g = ll.ll_decay_attention_bwd(*a, states, self.d_o, self.scale, self.lengths, self.d_final,
+                                      self.initial is not None, workspace=ws)
+        return out, final, g
+
+    def check(self):
+        h = [np.nan_to_num(_np(t)) for t in (self.q, self.k, self.v)] + [_np(self.ld)]
+        d = np.nan_to_num(_np(self.d_o))
+        i, f = _np(self.initial), _np(self.d_final)
+        mag = [np.abs(x) for x in h[:3]] + [h[3]]
+        o, final, g = self.run()
+        want, end = layer.decay_attention(*h, self.scale, i, self.ends)
+        bound, end_bound = layer.decay_attention(*mag, self.scale, None if i is None else np.abs(i), self.ends)
+        _within(o, want, bound, self.dtype, self.T, "o")
+        _within(final, end, end_bound, self.dtype, self.T, "final", state=True)
+        wants = layer.decay_attention_grad(*h, d, self.scale, i, self.ends, f)
+        bounds = layer.decay_attention_grad(*mag, np.abs(d), self.scale, None if i is None else np.abs(i), self.ends,
+                                            None if f is None else np.abs(f))
+        for name, got, w, b in zip(("dq", "dk", "dv"), g, wants, bounds):
+            _within(got, w, b, self.dtype, self.T, name)
+        if i is not None:
+            _within(g.initial_state, wants[3], bounds[3], self.dtype, self.T, "d_initial", state=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dk,dv", [(1, 1), (8, 24), (16, 16), (64, 64), (33, 65), (40, 72), (128, 64), (64, 128), (128, 128),
+                                   (129, 16), (200, 100), (256, 256)])
+def test_head_sizes(dk, dv, dtype):
+    _Case(dk + dv, 2, 150, 4, 2, dk, dv, dtype, ends=[150, 77]).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1, 2, 16, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200])
+@pytest.mark.parametrize("state", [True, False])
+def test_lengths(T, state, dtype):
+    _Case(T, 1, T, 3, 3, 24, 40, dtype, state=state).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("off", [8, 3])
+@pytest.mark.parametrize("dk,dv", [(64, 64), (20, 36), (7, 9)])
+def test_columns_of_wider_rows(dk, dv, off, dtype):
+    _Case(off, 2, 100, 6, 2, dk, dv, dtype, ends=[100, 40], off=off).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("ends", [[0, 1, 64], [65, 0, 130], [130, 129, 128]])
+def test_sequences_that_end_early(ends, dtype):
+    _Case(1, 3, 130, 2, 1, 32, 48, dtype, ends=ends).check()
+
+
+# one segment to 512 tokens or more where batch and heads are few
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,ends,state", [(1100, None, True), (1536, [1536, 0, 640], True), (2111, [1, 2111, 1087], False),
+                                          (1024, [512, 513, 1024], True)])
+def test_segments(T, ends, state, dtype):
+    _Case(T, 3 if ends else 1, T, 2, 1, 16, 24, dtype, ends=ends, state=state).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("decays", [[0.0], [float("-inf")], [-1e-7, -5.0, -80.0, -1e30]])
+@pytest.mark.parametrize("T", [70, 1100])
+def test_decays_from_none_to_all(decays, T, dtype):
+    _Case(5, 1, T, 4, 4, 16, 16, dtype, decays=decays).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dk,dv", [(1, 1), (16, 16), (40, 72), (128, 128), (72, 33), (256, 200)])
+@pytest.mark.parametrize("inplace", [False, True])
+def test_step(dk, dv, inplace, dtype):
+    import paper_2506_04761_amd as ll
+    import torch
+    c = _Case(dk, 3, 1, 4, 2, dk, dv, dtype, off=3)
+    h = [_np(t) for t in (c.q, c.k, c.v, c.ld)]
+    want, end = layer.decay_attention(*h, c.scale, _np(c.initial))
+    bound, _ = layer.decay_attention(*(np.abs(x) for x in h[:3]), h[3], c.scale, np.abs(_np(c.initial)))
+    state = c.initial.clone()
+    new = None if inplace else torch.full_like(state, float("nan"))
+    o = ll.ll_decay_attention_step(c.q[:, 0], c.k[:, 0], c.v[:, 0], c.ld, state, c.scale, new)
+    # a sum over d_k in fp32, without rounded products
+    tol = (dk + 16) * 2.0 ** -24 * bound[:, 0] + HALF[dtype] * np.abs(want[:, 0])
+    assert (np.abs(_np(o) - want[:, 0]) <= tol * (1 + 1e-5)).all()
+    got = state if inplace else new
+    assert (np.abs(_np(got) - end) <= 8 * 2.0 ** -24 * (np.abs(end) + np.abs(_np(c.initial)) + np.abs(end - _np(c.initial)))).all()
+    assert inplace or torch.equal(state, c.initial)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_prompt_is_continued_in_place_and_by_tokens(dtype):
+    import paper_2506_04761_amd as ll
+    import torch
+    B, T, H, dk, dv = 3, 90, 4, 32, 48
+    c = _Case(8, B, T, H, 2, dk, dv, dtype, state=False)
+    ends = [50, 0, 37]
+    whole = torch.zeros((B, H, dk, dv), device="cuda")
+    n = _ends([e + 30 for e in ends])
+    want = ll.ll_decay_attention_fwd(c.q, c.k, c.v, c.ld, c.scale, None, whole, n)
+    state = torch.zeros_like(whole)
+    ll.ll_decay_attention_fwd(c.q, c.k, c.v, c.ld, c.scale, state, state, _ends(ends))
+    got = []
+    for t in range(30):
+        q, k, v = (torch.stack([x[b, e + t] for b, e in enumerate(ends)]) for x in (c.q, c.k, c.v))
+        got.append(ll.ll_decay_attention_step(q, k, v, c.ld, state, c.scale))
+    h = [_np(t) for t in (c.q, c.k, c.v, c.ld)]
+    bound, end_bound = layer.decay_attention(*(np.abs(x) for x in h[:3]), h[3], c.scale, None, [e + 30 for e in ends])
+    for b, e in enumerate(ends):
+        one = torch.stack([g[b] for g in got])
+        _within(one, _np(want[b, e:e + 30]), 2 * bound[b, e:e + 30], dtype, T, "tokens")
+    _within(state, _np(whole), 2 * end_bound, dtype, T, "state", state=True)
+
+
+def test_differentiable_against_differences():
+    import paper_2506_04761_amd as ll
+    import torch
+    r = np.random.default_rng(2)
+    q, k = (to_dev(r.standard_normal((2, 5, 1, 3))).requires_grad_() for _ in "qk")
+    v = to_dev(r.standard_normal((2, 5, 2, 4))).requires_grad_()
+    first = to_dev(r.standard_normal((2, 2, 3, 4))).requires_grad_()
+    ld, n = to_dev(np.array([-0.1, -0.5])), _ends([5, 3])
+    do, df = to_dev(r.standard_normal((2, 5, 2, 4))), to_dev(r.standard_normal((2, 2, 3, 4)))
+
+    def loss():
+        o, final = ll.decay_attention(q, k, v, ld, 0.5, first, n, return_final_state=True)
+        return (o * do).double().sum() + (final * df).double().sum()
+
+    loss().backward()
+    step = 2.0 ** -4  # the loss is of degree three in each element at most and linear in one: no error but rounding
+    for t in (q, k, v, first):
+        flat, grad = t.data.view(-1), t.grad.view(-1)
+        for i in range(0, flat.numel(), 2):
+            at = flat[i].item()
+            ends = []
+            for s in (step, -step):
+                flat[i] = at + s
+                ends.append(loss().item())
+            flat[i] = at
+            # 40 values of up to 2^5 rounded at 2^-24 over 2 step
+            assert abs((ends[0] - ends[1]) / (2 * step) - grad[i].item()) <= 1e-3
+
+
+def test_differentiable_takes_any_strides_and_refuses_what_it_cannot_give():
+    import paper_2506_04761_amd as ll
+    import torch
+    c = _Case(3, 2, 80, 4, 2, 24, 16, "f32")
+    leaves = [x.transpose(1, 2).contiguous().requires_grad_() for x in (c.q, c.k, c.v)]  # heads before tokens
+    o = ll.decay_attention(*(x.transpose(1, 2) for x in leaves), c.ld, c.scale)
+    o.backward(c.d_o.transpose(1, 2).contiguous().transpose(1, 2))
+    states = ll.ll_decay_attention_states(c.q, c.v)
+    assert torch.equal(o, ll.ll_decay_attention_fwd(c.q, c.k, c.v, c.ld, c.scale, states=states))
+    g = ll.ll_decay_attention_bwd(c.q, c.k, c.v, c.ld, states, c.d_o, c.scale)
+    for x, want in zip(leaves, g):
+        assert torch.equal(x.grad.transpose(1, 2), want)
+    assert g.initial_state is None
+    with pytest.raises(ValueError, match="constants"):
+        ll.decay_attention(c.q, c.k, c.v, c.ld.clone().requires_grad_())
+    q = c.q.clone().requires_grad_()
+    d, = torch.autograd.grad(ll.decay_attention(q, c.k, c.v, c.ld).square().sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        d.sum().backward()
+
+
+def test_on_another_stream_and_in_a_graph():
+    import paper_2506_04761_amd as ll
+    import torch
+    c = _Case(4, 2, 1100, 4, 2, 64, 64, "bf16", ends=[1100, 700])
+    a = (c.q, c.k, c.v, c.ld)
+    out, final, g = c.run()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    states = ll.ll_decay_attention_states(c.q, c.v)
+    again = ll.ll_decay_attention_fwd(*a, c.scale, c.initial, None, c.lengths, states, stream=side)
+    grads = ll.ll_decay_attention_bwd(*a, states, c.d_o, c.scale, c.lengths, c.d_final, True, stream=side)
+    side.synchronize()
+    assert torch.equal(again, out) and all(torch.equal(x, y) for x, y in zip(grads, g))
+    ws = ll.ll_decay_attention_workspace(c.q, c.v, backward=True)
+    made = ll.DecayGrads(*(torch.empty_like(t) for t in g))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ll.ll_decay_attention_fwd(*a, c.scale, c.initial, final, c.lengths, states, out, ws)
+        ll.ll_decay_attention_bwd(*a, states, c.d_o, c.scale, c.lengths, c.d_final, grads=made, workspace=ws)
+        ll.ll_decay_attention_step(*(x[:, 5] for x in a[:3]), c.ld, final, c.scale, out=out[:, 1099].contiguous())
+    for scale in (1.0, -0.5, 2.0):
+        c.initial.mul_(scale)
+        for t in (out, final, *made):
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        want, end, g = c.run()
+        ll.ll_decay_attention_step(*(x[:, 5] for x in a[:3]), c.ld, end, c.scale)
+        assert torch.equal(out, want) and torch.equal(final, end)
+        assert all(torch.equal(x, y) for x, y in zip(made, g))
+
+
+def test_refusals():
+    import paper_2506_04761_amd as ll
+    import torch
+    c = _Case(1, 2, 8, 4, 2, 16, 24, "bf16")
+    f, a = ll.ll_decay_attention_fwd, (c.q, c.k, c.v, c.ld)
+    with pytest.raises(ValueError, match="k has shape"):
+        f(c.q, c.k[:, :, :1], c.v, c.ld)
+    with pytest.raises(ValueError, match="v has shape"):
+        f(c.q, c.k, c.v[:, :7], c.ld)
+    with pytest.raises(TypeError, match="v must be"):
+        f(c.q, c.k, c.v.float(), c.ld)
+    with pytest.raises(TypeError, match="unsupported dtype"):
+        f(c.q.half(), c.k.half(), c.v.half(), c.ld)
+    with pytest.raises(ValueError, match="log_decay has shape"):
+        f(c.q, c.k, c.v, c.ld[:3].contiguous())
+    with pytest.raises(ValueError, match="adjacent heads"):
+        f(c.q, c.k.transpose(1, 2).contiguous().transpose(1, 2), c.v, c.ld)
+    with pytest.raises(ValueError, match="adjacent channels"):
+        f(c.q, c.k, c.v.transpose(2, 3).contiguous().transpose(2, 3), c.ld)
+    with pytest.raises(ValueError, match="initial_state has shape"):
+        f(*a, initial_state=c.initial[:1])
+    with pytest.raises(TypeError, match="lengths must be"):
+        f(*a, lengths=torch.tensor([1, 2], device="cuda"))
+    with pytest.raises(ValueError, match="states is smaller"):
+        f(*a, states=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(ll.LLError):  # heads that do not divide
+        f(c.q, c.k, c.v[:, :, :3].contiguous(), c.ld[:3].contiguous())
+    with pytest.raises(ValueError, match="4 axes"):
+        f(c.q[0], c.k[0], c.v[0], c.ld)
+    wide = torch.zeros((1, 2, 1, 257), device="cuda")
+    with pytest.raises(ll.LLError):
+        f(wide, wide, wide[..., :16].contiguous(), c.ld[:1].contiguous())
+    with pytest.raises(ValueError, match="state has shape"):
+        ll.ll_decay_attention_step(c.q[:, 0], c.k[:, 0], c.v[:, 0], c.ld, c.initial[..., :5].contiguous())
+    with pytest.raises(ValueError, match="d_o has shape"):
+        ll.ll_decay_attention_bwd(*a, ll.ll_decay_attention_states(c.q, c.v), c.d_o[:, 1:].contiguous())
+    long = torch.zeros((1, 2048, 1, 16), device="cuda")
+    with pytest.raises(ll.LLError):
+        f(long, long, long, c.ld[:1].contiguous(), workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))

@@ -1,6 +1,7 @@
 """libloglinear: log-linear attention (forward, backward and decoding) (Guo et al., "Log-Linear
 Attention") on MI355X, and the operators around such a mixer: short causal
-convolution, selective state space scan, group norm.
+convolution, selective state space scan, group norm; and, in `block`, linear attention with a
+decay for each head and projections.
 
 The computation lives in the HIP library libloglinear.so (C ABI: include/libloglinear.h);
 this package is its Python binding.
@@ -15,11 +16,10 @@ from ._lib import (  # noqa: F401
     log_linear_mamba2,
 )
 from ._layer import (  # noqa: F401
-    LL_ACT_NONE, LL_ACT_SILU, ConvGrads, DecayGrads, NormGrads, ProjectionGrads, ScanGrads, ll_causal_conv_bwd,
-    ll_causal_conv_bwd_workspace, ll_causal_conv_fwd, ll_causal_conv_step, ll_decay_attention_bwd,
-    ll_decay_attention_fwd, ll_decay_attention_states, ll_decay_attention_step, ll_decay_attention_workspace,
-    ll_group_norm_bwd, ll_group_norm_fwd, ll_group_norm_stats, ll_group_norm_workspace, ll_projection_bwd,
-    ll_projection_fwd, ll_projection_workspace, ll_selective_scan_bwd, ll_selective_scan_fwd, ll_selective_scan_states,
-    ll_selective_scan_step, ll_selective_scan_workspace, causal_conv, decay_attention, group_norm, projection,
-    selective_scan,
+    LL_ACT_NONE, LL_ACT_SILU, ConvGrads, NormGrads, ScanGrads, ll_causal_conv_bwd, ll_causal_conv_bwd_workspace,
+    ll_causal_conv_fwd, ll_causal_conv_step, ll_group_norm_bwd, ll_group_norm_fwd, ll_group_norm_stats,
+    ll_group_norm_workspace, ll_selective_scan_bwd, ll_selective_scan_fwd, ll_selective_scan_states,
+    ll_selective_scan_step, ll_selective_scan_workspace, causal_conv, group_norm, selective_scan,
 )
+from . import block  # noqa: F401
+from .block import DecayGrads, ProjectionGrads, decay_attention, projection  # noqa: F401

@@ -17,7 +17,7 @@ BIG = 1 << 50
 
 
 def _inputs(**kw):
-    s = ll._layer._DecayInputs()
+    s = ll.block._DecayInputs()
     for n in ("q", "k", "v", "log_decay"):
         setattr(s, n, 4096)
     s.batch, s.T, s.heads, s.qk_heads, s.d_k, s.d_v, s.scale, s.dtype = 2, 4096, 4, 2, 64, 32, 1.0, 1

@@ -75,7 +75,7 @@ class _Case:
 
     def run(self):
         """(o, final state, gradients) into memory full of NaN."""
-        import paper_2506_04761_amd as ll
+        from paper_2506_04761_amd import block as ll
         import torch
         nan = float("nan")
         out = torch.full(self.v.shape, nan, device="cuda", dtype=self.v.dtype)
@@ -157,7 +157,7 @@ def test_decays_from_none_to_all(decays, T, dtype):
 @pytest.mark.parametrize("dk,dv", [(1, 1), (16, 16), (40, 72), (128, 128), (72, 33), (256, 200)])
 @pytest.mark.parametrize("inplace", [False, True])
 def test_step(dk, dv, inplace, dtype):
-    import paper_2506_04761_amd as ll
+    from paper_2506_04761_amd import block as ll
     import torch
     c = _Case(dk, 3, 1, 4, 2, dk, dv, dtype, off=3)
     h = [_np(t) for t in (c.q, c.k, c.v, c.ld)]
@@ -176,7 +176,7 @@ def test_step(dk, dv, inplace, dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_a_prompt_is_continued_in_place_and_by_tokens(dtype):
-    import paper_2506_04761_amd as ll
+    from paper_2506_04761_amd import block as ll
     import torch
     B, T, H, dk, dv = 3, 90, 4, 32, 48
     c = _Case(8, B, T, H, 2, dk, dv, dtype, state=False)
@@ -199,7 +199,7 @@ def test_a_prompt_is_continued_in_place_and_by_tokens(dtype):
 
 
 def test_differentiable_against_differences():
-    import paper_2506_04761_amd as ll
+    from paper_2506_04761_amd import block as ll
     import torch
     r = np.random.default_rng(2)
     q, k = (to_dev(r.standard_normal((2, 5, 1, 3))).requires_grad_() for _ in "qk")
@@ -228,7 +228,7 @@ def test_differentiable_against_differences():
 
 
 def test_differentiable_takes_any_strides_and_refuses_what_it_cannot_give():
-    import paper_2506_04761_amd as ll
+    from paper_2506_04761_amd import block as ll
     import torch
     c = _Case(3, 2, 80, 4, 2, 24, 16, "f32")
     leaves = [x.transpose(1, 2).contiguous().requires_grad_() for x in (c.q, c.k, c.v)]  # heads before tokens
@@ -249,7 +249,7 @@ def test_differentiable_takes_any_strides_and_refuses_what_it_cannot_give():
 
 
 def test_on_another_stream_and_in_a_graph():
-    import paper_2506_04761_amd as ll
+    from paper_2506_04761_amd import block as ll
     import torch
     c = _Case(4, 2, 1100, 4, 2, 64, 64, "bf16", ends=[1100, 700])
     a = (c.q, c.k, c.v, c.ld)
@@ -281,7 +281,7 @@ def test_on_another_stream_and_in_a_graph():
 
 
 def test_refusals():
-    import paper_2506_04761_amd as ll
+    from paper_2506_04761_amd import block as ll
     import torch
     c = _Case(1, 2, 8, 4, 2, 16, 24, "bf16")
     f, a = ll.ll_decay_attention_fwd, (c.q, c.k, c.v, c.ld)

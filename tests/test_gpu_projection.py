@@ -106,7 +106,7 @@ SIZES = [(1, 1, 1), (1, 8, 16), (1, 2048, 40), (5, 40, 24), (16, 64, 64), (17, 1
 @pytest.mark.parametrize("M,K,N", SIZES)
 @pytest.mark.parametrize("off", [None, 8, 3])
 def test_sizes(M, K, N, dtype, off):
-    import paper_2506_04761_amd as ll
+    from paper_2506_04761_amd import block as ll
     import torch
     i = _inputs(M + K + N, M, K, N, dtype, off)
     h = _host(i)
@@ -121,7 +121,7 @@ def test_sizes(M, K, N, dtype, off):
 @pytest.mark.parametrize("silu,bias,residual", [(False, False, False), (False, True, False), (True, False, True),
                                                 (False, False, True), (True, True, False)])
 def test_epilogue(M, K, N, dtype, silu, bias, residual):
-    import paper_2506_04761_amd as ll
+    from paper_2506_04761_amd import block as ll
     import torch
     i = _inputs(7, M, K, N, dtype, None, bias, residual)
     h = _host(i)
@@ -138,7 +138,7 @@ def test_epilogue(M, K, N, dtype, silu, bias, residual):
 
 
 def test_only_the_gradients_that_are_wanted():
-    import paper_2506_04761_amd as ll
+    from paper_2506_04761_amd import block as ll
     import torch
     i = _inputs(9, 90, 64, 72, "bf16", None)
     full = ll.ll_projection_bwd(i["x"], i["w"], i["b"], i["dy"])
@@ -151,7 +151,7 @@ def test_only_the_gradients_that_are_wanted():
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("M", [7, 200])
 def test_inf_and_nan_stay_in_their_rows(dtype, M):
-    import paper_2506_04761_amd as ll
+    from paper_2506_04761_amd import block as ll
     import torch
     i = _inputs(3, M, 100, 50, dtype, None)
     y = ll.ll_projection_fwd(i["x"], i["w"], i["b"], i["r"])
@@ -166,7 +166,7 @@ def test_inf_and_nan_stay_in_their_rows(dtype, M):
 
 
 def test_differentiable_over_leading_axes():
-    import paper_2506_04761_amd as ll
+    from paper_2506_04761_amd import block as ll
     import torch
     r = np.random.default_rng(5)
     wide = to_dev(r.standard_normal((3, 7, 96))).requires_grad_()
@@ -185,7 +185,7 @@ def test_differentiable_over_leading_axes():
 
 
 def test_gradients_against_differences():
-    import paper_2506_04761_amd as ll
+    from paper_2506_04761_amd import block as ll
     import torch
     r = np.random.default_rng(6)
     x, w, b = (to_dev(r.standard_normal(s)).requires_grad_() for s in ((6, 5), (4, 5), (4,)))
@@ -210,7 +210,7 @@ def test_gradients_against_differences():
 
 
 def test_second_derivatives_are_refused_but_the_residual_is_linear():
-    import paper_2506_04761_amd as ll
+    from paper_2506_04761_amd import block as ll
     import torch
     x, w = (torch.randn(s, device="cuda", requires_grad=True) for s in ((4, 8), (8, 8)))
     y = ll.projection(x, w, residual=x)
@@ -220,7 +220,7 @@ def test_second_derivatives_are_refused_but_the_residual_is_linear():
 
 
 def test_on_another_stream_and_in_a_graph():
-    import paper_2506_04761_amd as ll
+    from paper_2506_04761_amd import block as ll
     import torch
     i = _inputs(11, 300, 1032, 136, "bf16", None)
     pre = torch.empty((300, 136), device="cuda")
@@ -251,7 +251,7 @@ def test_on_another_stream_and_in_a_graph():
 
 
 def test_refusals():
-    import paper_2506_04761_amd as ll
+    from paper_2506_04761_amd import block as ll
     import torch
     i = _inputs(1, 4, 8, 16, "bf16", None)
     f = ll.ll_projection_fwd

@@ -178,7 +178,7 @@ def prepare(case, seed):
 
 def _prepare_own(s):
     """The buffers that a program keeps from call to call: outputs, states and workspaces."""
-    import paper_2506_04761_amd as ll
+    from paper_2506_04761_amd import block as ll
     case = s["case"]
     kind, s["ll"] = case["kind"], ll
     if case["op"] == "attn":

@@ -114,29 +114,44 @@ __device__ inline float log2_decay(const float* log_decay, int h) {
   return v < -1e30f ? -1e30f : v;
 }
 
-// Copies a chunk of rows of up to W elements to LDS through registers: rows of other tokens and elements beyond the
-// width are zeros.
-template <typename T, int W>
-struct Chunk {
+__device__ const uint4 kZeros = {0, 0, 0, 0};  // rows before the first token, elements beyond the width
+
+// Copies chunks of C rows of up to W elements to LDS, 16 bytes a thread at a time: straight there (VEC: rows of whole,
+// aligned vectors), or through registers.
+template <typename T, int W, bool VEC>
+struct Stage {
   typedef Tile<T, W> Tl;
   typedef typename VecN<T, Tl::E>::type Vec;
-  static constexpr int E = Tl::E, C = Op<T>::C, ITS = C * Tl::CH / 256;
-  Vec held[ITS];
-  // `p`: element (0, col0) of the first token, `step` elements between tokens, `n` live ones
-  __device__ inline void load(const T* p, int64_t step, int64_t n, int left, bool vec) {
-#pragma unroll
-    for (int it = 0; it < ITS; ++it) {
-      const int q = it * 256 + threadIdx.x, row = q / Tl::CH, c = q % Tl::CH;
-      const int k = left - c * E;
-      held[it] = load_n<T, E>(p + row * step + c * E, row >= n || k <= 0 ? 0 : (k < E ? k : E), vec);
-    }
+  static constexpr int E = Tl::E, CH = Tl::CH, C = Op<T>::C, ITS = C * CH / 256, ROWS = 256 / CH;
+  const T* at;   // this thread's first piece of the next chunk
+  int64_t step;  // elements between tokens
+  int left;      // elements of a row
+  // `p`: element 0 of the first chunk's row 0
+  __device__ inline void start(const T* p, int64_t step_, int left_) {
+    step = step_, left = left_;
+    const int row = threadIdx.x / CH;
+    at = p + row * step + ((threadIdx.x % CH) ^ Tl::key(row)) * E;
   }
-  __device__ inline void store(T* s) const {
+  // The next chunk, of which rows before `first` are zeros.
+  __device__ inline void load(T* s, int first) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = threadIdx.x / CH;
+    const int c0 = (threadIdx.x % CH) ^ Tl::key(row0);
+    const bool edge = first > 0 || left < W;
 #pragma unroll
     for (int it = 0; it < ITS; ++it) {
-      const int q = it * 256 + threadIdx.x;
-      *reinterpret_cast<Vec*>(s + Tl::at(q / Tl::CH, q % Tl::CH)) = held[it];
+      const int row = row0 + it * ROWS, c = (threadIdx.x % CH) ^ Tl::key(row);
+      const T* src = at + it * ROWS * step + (c - c0) * E;
+      T* to = s + (it * 256 + wave * 64) * E;
+      const int k = row < first ? 0 : left - c * E;
+      if constexpr (VEC) {
+        const void* from = src;
+        if (edge && k <= 0) from = &kZeros;
+        __builtin_amdgcn_global_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+      } else {
+        reinterpret_cast<Vec*>(to)[threadIdx.x & 63] = load_n<T, E>(src, k <= 0 ? 0 : (k < E ? k : E), false);
+      }
     }
+    at += C * step;
   }
 };
 
@@ -155,10 +170,11 @@ __device__ inline f32x4 pack<float>(const f32x4* v) {
 }
 
 // One segment of one head, 64 NV values a workgroup: a wave holds the state's rows of its 16 NV columns.  d1 <= DK.
-template <typename T, int DK, int NV, bool STATE>
+// Chunks end with the segment: the first may begin with rows of zeros, and powers of the decay are the same in all others.
+template <typename T, int DK, int NV, bool STATE, bool VEC>
 __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
-  constexpr int KF = Op<T>::KF, C = Op<T>::C, E = 16 / sizeof(T), R = KF / 16, QT = C / 16, US = C / KF, KS = DK / KF, DT = DK / 16;
-  constexpr int DV = 64 * NV;
+  constexpr int KF = Op<T>::KF, C = Op<T>::C, R = KF / 16, QT = C / 16, US = C / KF, KS = DK / KF, DT = DK / 16;
+  constexpr int DV = 64 * NV, NU = US * QT / 4;  // NU: fragments of P^T that a wave forms
   typedef typename Op<T>::Frag Frag;
   typedef Tile<T, DK> TlK;
   typedef Tile<T, DV> TlV;
@@ -166,25 +182,43 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
   __shared__ __attribute__((aligned(1024))) T sv[C * DV];
   __shared__ __attribute__((aligned(1024))) T sq[STATE ? 8 : C * DK];
   __shared__ Frag sp[STATE ? 1 : QT][US][64];
+  __shared__ __attribute__((aligned(16))) float sw[C];  // what a token's product counts in the state after the chunk
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i = lane & 15;
 
-  int64_t id = xcd_remap(blockIdx.x, p.groups);
-  const int blk = int(id % p.blocks);
-  id /= p.blocks;
-  const int seg = int(id % (STATE ? p.S - 1 : p.S));
-  id /= STATE ? p.S - 1 : p.S;
-  const int h = int(id % p.H);
-  const int64_t b = id / p.H;
+  unsigned id = unsigned(xcd_remap(blockIdx.x, p.groups));
+  const unsigned segs = STATE ? p.S - 1 : p.S;
+  const int blk = int(id % unsigned(p.blocks));
+  id /= unsigned(p.blocks);
+  const int seg = int(id % segs);
+  id /= segs;
+  const int h = int(id % unsigned(p.H));
+  const int64_t b = id / unsigned(p.H);
   const int d1 = p.a.width, d2 = p.c.width, col0 = blk * DV;
   const int64_t live = live_tokens(p.lengths, b, p.T), t0 = seg * p.L;
   int64_t n = live - t0 < p.L ? live - t0 : p.L;  // tokens of this segment
   n = n < 0 ? 0 : n;
+  const int64_t chunks = (n + C - 1) / C;
+  int first = int(chunks * C - n);  // rows of zeros
   const float lg = log2_decay(p.log_decay, h);
   const int rho = p.reversed ? 1 : 0;
 
   // the wave's columns: value tile v, lane i
   const int wcol = 16 * NV * wave;
   auto vcol = [&](int v, int x) { return wcol + (NV == 2 ? 8 * (x >> 2) + 4 * v + (x & 3) : x); };
+
+  // tokens by their order in time: that of the first chunk's row 0, and the step between two
+  const int64_t tok = p.reversed ? live - 1 - (t0 - first) : t0 - first, dir = p.reversed ? -1 : 1;
+  Stage<T, DK, VEC> lk, lq;
+  Stage<T, DV, VEC> lv;
+  lk.start(static_cast<const T*>(p.b.p) + b * p.b.sb + tok * p.b.st + (h / p.b.group) * d1, dir * p.b.st, d1);
+  lv.start(static_cast<const T*>(p.c.p) + b * p.c.sb + tok * p.c.st + (h / p.c.group) * d2 + col0, dir * p.c.st, d2 - col0);
+  if (!STATE) lq.start(static_cast<const T*>(p.a.p) + b * p.a.sb + tok * p.a.st + (h / p.a.group) * d1, dir * p.a.st, d1);
+  if (n > 0) {
+    lk.load(sk, first);
+    if (!STATE) lq.load(sq, first);
+    lv.load(sv, first);
+  }
+  if (threadIdx.x < C) sw[threadIdx.x] = p.in_scale * fast_exp2(lg * float(C - 1 - int(threadIdx.x) + rho));
 
   f32x4 S[DT][NV] = {};
   if (!STATE && p.first && n > 0) {
@@ -196,35 +230,28 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int row = row_of<T>(t, 4 * g + r), col = col0 + vcol(v, i);
-          if (row < d1 && col < d2) S[t][v][r] = f[p.transposed ? int64_t(col) * d1 + row : int64_t(row) * d2 + col];
+          if (row < d1 && col < d2) S[t][v][r] = f[p.transposed ? col * d1 + row : row * d2 + col];
         }
   }
+  // g^(i-j) of the wave's scores, nothing where j > i
+  float pw[NU][R][4];
+  const int qt0 = wave % QT;
+#pragma unroll
+  for (int x = 0; x < NU; ++x)
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int gap = 16 * qt0 + i - row_of<T>(R * (wave / QT + x * (4 / QT)) + r, 4 * g + e);
+        pw[x][r][e] = gap >= 0 ? p.in_scale * fast_exp2(lg * float(gap)) : 0.0f;
+      }
+  const int ocol = col0 + wcol + 4 * NV * g, ocount = d2 - ocol < 4 * NV ? d2 - ocol : 4 * NV;
+  int64_t orow = ((b * p.T + tok + dir * i) * p.H + h) * d2 + ocol;
+  const int64_t ostep = dir * p.H * d2;
 
-  // tokens by their order in time: the first of the segment, and the step between two
-  const int64_t tok = p.reversed ? live - 1 - t0 : t0, dir = p.reversed ? -1 : 1;
-  const T* kp = static_cast<const T*>(p.b.p) + b * p.b.sb + tok * p.b.st + (h / p.b.group) * d1;
-  const T* vp = static_cast<const T*>(p.c.p) + b * p.c.sb + tok * p.c.st + (h / p.c.group) * d2 + col0;
-  const T* qp = static_cast<const T*>(p.a.p) + b * p.a.sb + tok * p.a.st + (h / p.a.group) * d1;
-  const int64_t ks_ = dir * p.b.st, vs_ = dir * p.c.st, qs_ = dir * p.a.st;
-  Chunk<T, DK> ck, cq;
-  Chunk<T, DV> cv;
-  if (n > 0) {
-    ck.load(kp, ks_, n, d1, p.b.vec);
-    cv.load(vp, vs_, n, d2 - col0, p.c.vec);
-    if (!STATE) cq.load(qp, qs_, n, d1, p.a.vec);
-  }
-  for (int64_t c0 = 0; c0 < n; c0 += C) {
-    const int m = n - c0 < C ? int(n - c0) : C;  // tokens of this chunk
-    ck.store(sk);
-    cv.store(sv);
-    if (!STATE) cq.store(sq);
+  for (int64_t ch = 0; ch < chunks; ++ch) {
+    if (VEC) wait_vmem();
     __syncthreads();
-    if (c0 + C < n) {
-      const int64_t at = c0 + C, more = n - at;
-      ck.load(kp + at * ks_, ks_, more, d1, p.b.vec);
-      cv.load(vp + at * vs_, vs_, more, d2 - col0, p.c.vec);
-      if (!STATE) cq.load(qp + at * qs_, qs_, more, d1, p.a.vec);
-    }
     Frag vf[NV][US];
 #pragma unroll
     for (int v = 0; v < NV; ++v)
@@ -233,26 +260,22 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
 
     if constexpr (!STATE) {
       // P^T of 16 queries and the keys up to them
-      {
-        const int qt = wave % QT;
-        for (int u = wave / QT; u < US; u += 4 / QT) {
-          if (u * KF > 16 * qt + 15) continue;
-          f32x4 pt[R] = {};
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) {
-            const Frag q = TlK::along(sq, 16 * qt + i, ks, lane);
+      for (int x = 0; x < NU; ++x) {
+        const int u = wave / QT + x * (4 / QT);
+        if (u * KF > 16 * qt0 + 15) continue;
+        f32x4 pt[R] = {};
 #pragma unroll
-            for (int r = 0; r < R; ++r) pt[r] = Op<T>::mma(TlK::along(sk, row_of<T>(R * u + r, i), ks, lane), q, pt[r]);
-          }
+        for (int ks = 0; ks < KS; ++ks) {
+          const Frag q = TlK::along(sq, 16 * qt0 + i, ks, lane);
 #pragma unroll
-          for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int gap = 16 * qt + i - row_of<T>(R * u + r, 4 * g + e);
-              pt[r][e] = gap >= 0 ? pt[r][e] * (p.in_scale * fast_exp2(lg * float(gap))) : 0.0f;
-            }
-          sp[qt][u][lane] = pack<T>(pt);
+          for (int r = 0; r < R; ++r) pt[r] = Op<T>::mma(TlK::along(sk, row_of<T>(R * u + r, i), ks, lane), q, pt[r]);
         }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) pt[r][e] *= pw[x][r][e];
+        sp[qt0][u][lane] = pack<T>(pt);
       }
       f32x4 o[QT][NV] = {};
 #pragma unroll
@@ -274,7 +297,8 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
       }
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
-        const float w = fast_exp2(lg * float(16 * qt + i + 1 - rho));
+        const int after = 16 * qt + i + 1 - rho - first;
+        const float w = fast_exp2(lg * float(after > 0 ? after : 0));
 #pragma unroll
         for (int v = 0; v < NV; ++v) o[qt][v] *= w;
       }
@@ -290,22 +314,22 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
         }
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
-        const int row = 16 * qt + i, col = col0 + wcol + 4 * NV * g;
-        if (row >= m || col >= d2) continue;
+        if (16 * qt + i < first || ocount <= 0) continue;
         float f[4 * NV];
 #pragma unroll
         for (int v = 0; v < NV; ++v)
 #pragma unroll
           for (int r = 0; r < 4; ++r) f[4 * v + r] = o[qt][v][r] * p.out_scale;
-        const int64_t e = ((b * p.T + tok + dir * (c0 + row)) * p.H + h) * d2 + col;
-        const int count = d2 - col < 4 * NV ? d2 - col : 4 * NV;
-        if (p.wide) store_n<float, 4 * NV>(static_cast<float*>(p.out) + e, f, count, false);
-        else store_n<T, 4 * NV>(static_cast<T*>(p.out) + e, f, count, p.vec_out);
+        const int64_t e = orow + 16 * qt * ostep;
+        if (VEC && p.vec_out) store_n<T, 4 * NV>(static_cast<T*>(p.out) + e, f, ocount, true);
+        else if (p.wide) store_n<float, 4 * NV>(static_cast<float*>(p.out) + e, f, ocount, false);
+        else store_n<T, 4 * NV>(static_cast<T*>(p.out) + e, f, ocount, false);
       }
+      orow += C * ostep;
     }
 
     // the state after the chunk; values times powers of the decay in three bf16 parts, which hold all of fp32's bits
-    const float carry = fast_exp2(lg * float(m));
+    const float carry = fast_exp2(lg * float(C - first));
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -314,13 +338,18 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
     for (int u = 0; u < US; ++u) {
       constexpr int PARTS = sizeof(T) == 2 ? 3 : 1;
       Frag part[NV][PARTS];
+      float w[KF / 4];
 #pragma unroll
-      for (int x = 0; x < KF / 4; ++x) {
-        const int left = m - 1 - (KF * u + KF / 4 * g + x);
-        const float w = left >= 0 ? p.in_scale * fast_exp2(lg * float(left + rho)) : 0.0f;
+      for (int x = 0; x < KF / 4; x += 4) {
+        const f32x4 y = *reinterpret_cast<const f32x4*>(sw + KF * u + KF / 4 * g + x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[x + e] = y[e];
+      }
+#pragma unroll
+      for (int x = 0; x < KF / 4; ++x)
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-          float f = to_f32(T(vf[v][u][x])) * w;
+          float f = to_f32(T(vf[v][u][x])) * w[x];
 #pragma unroll
           for (int k = 0; k < PARTS; ++k) {
             const T y = from_f32<T>(f);
@@ -328,7 +357,6 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
             f -= to_f32(y);
           }
         }
-      }
 #pragma unroll
       for (int t = 0; t < DT; ++t) {
         const Frag k = TlK::down(sk, u, sizeof(T) == 2 ? row_of<T>(t, 4 * (i & 3)) : row_of<T>(t, i), lane);
@@ -339,6 +367,12 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
       }
     }
     __syncthreads();
+    first = 0;
+    if (ch + 1 < chunks) {
+      lk.load(sk, 0);
+      if (!STATE) lq.load(sq, 0);
+      lv.load(sv, 0);
+    }
   }
 
   // STATE: this segment's own sums, where the next one starts.  Else the final state, of the segment that ends there.
@@ -356,7 +390,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
         for (int r = 0; r < 4; ++r) {
           const int row = row_of<T>(t, 4 * g + r), col = col0 + vcol(v, i);
           if (row < d1 && col < d2) {
-            const int64_t e = p.transposed ? int64_t(col) * d1 + row : int64_t(row) * d2 + col;
+            const int e = p.transposed ? col * d1 + row : row * d2 + col;
             to[e] = keep ? f[e] : S[t][v][r];
           }
         }
@@ -365,10 +399,12 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
   if (!STATE) {
     const int64_t end = t0 + p.L < p.T ? t0 + p.L : p.T, from = live > t0 ? live : t0;
     const int cols = d2 - col0 < DV ? d2 - col0 : DV;
-    for (int64_t q = threadIdx.x; q < (end - from) * cols; q += 256) {
-      const int64_t e = ((b * p.T + from + q / cols) * p.H + h) * d2 + col0 + q % cols;
-      if (p.wide) static_cast<float*>(p.out)[e] = 0.0f;
-      else static_cast<T*>(p.out)[e] = from_f32<T>(0.0f);
+    for (int64_t t = from + wave; t < end; t += 4) {
+      const int64_t e = ((b * p.T + t) * p.H + h) * d2 + col0;
+      for (int c = lane; c < cols; c += 64) {
+        if (p.wide) static_cast<float*>(p.out)[e + c] = 0.0f;
+        else static_cast<T*>(p.out)[e + c] = from_f32<T>(0.0f);
+      }
     }
   }
 }
@@ -380,16 +416,21 @@ __global__ __launch_bounds__(256) void k_join(float* h, const float* first, cons
   if (id >= total) return;
   const int64_t bh = id / size, e = id % size;
   const int64_t live = live_tokens(lengths, bh / H, T);
-  const float lg = log2_decay(log_decay, int(bh % H));
+  const int used = live > 0 ? int((live - 1) / L) + 1 : 1;  // segments that hold tokens
   float* p = h + bh * S * size + e;
   float v = first ? first[id] : 0.0f;
   p[0] = v;
-  const float w = fast_exp2(lg * float(L));  // a segment with one after it is whole
-#pragma unroll 4
-  for (int s = 1; s < S; ++s) {
-    if (s * L >= live) break;
-    v = fmaf(w, v, p[s * size]);
-    p[s * size] = v;
+  const float w = fast_exp2(log2_decay(log_decay, int(bh % H)) * float(L));  // a segment with one after it is whole
+  constexpr int U = 8;  // loads ahead of the stores
+  for (int s = 1; s < used; s += U) {
+    float u[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) u[k] = s + k < used ? p[(s + k) * size] : 0.0f;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      v = fmaf(w, v, u[k]);
+      if (s + k < used) p[(s + k) * size] = v;
+    }
   }
 }
 
@@ -498,8 +539,9 @@ int value_tiles(int64_t d1, int64_t d2) { return d1 <= 128 && d2 > 64 ? 2 : 1; }
 template <typename T, int DK, int NV>
 hipError_t launch_attend(const DecayDev& p, bool state, hipStream_t st) {
   const dim3 grid(uint32_t(p.groups)), block(256);
-  if (state) k_attend<T, DK, NV, true><<<grid, block, 0, st>>>(p);
-  else k_attend<T, DK, NV, false><<<grid, block, 0, st>>>(p);
+  const bool vec = p.b.vec && p.c.vec && (state || p.a.vec);
+  if (state) vec ? k_attend<T, DK, NV, true, true><<<grid, block, 0, st>>>(p) : k_attend<T, DK, NV, true, false><<<grid, block, 0, st>>>(p);
+  else vec ? k_attend<T, DK, NV, false, true><<<grid, block, 0, st>>>(p) : k_attend<T, DK, NV, false, false><<<grid, block, 0, st>>>(p);
   return hipGetLastError();
 }
 
@@ -508,7 +550,7 @@ hipError_t attend(DecayDev p, int64_t B, bool state, hipStream_t st) {
   const int nv = value_tiles(p.a.width, p.c.width);
   p.blocks = int(ceil_div(p.c.width, 64 * nv));
   p.groups = B * p.H * p.blocks * (state ? p.S - 1 : p.S);
-  p.vec_out = p.c.width % (4 * nv) == 0 && reinterpret_cast<uintptr_t>(p.out) % (4 * nv * sizeof(T)) == 0;
+  p.vec_out = !p.wide && p.c.width % (4 * nv) == 0 && reinterpret_cast<uintptr_t>(p.out) % (4 * nv * sizeof(T)) == 0;
   if (p.a.width <= 64) return nv == 2 ? launch_attend<T, 64, 2>(p, state, st) : launch_attend<T, 64, 1>(p, state, st);
   if (p.a.width <= 128) return nv == 2 ? launch_attend<T, 128, 2>(p, state, st) : launch_attend<T, 128, 1>(p, state, st);
   return launch_attend<T, 256, 1>(p, state, st);

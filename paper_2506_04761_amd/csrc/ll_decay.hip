@@ -46,21 +46,32 @@ __device__ inline int row_of(int t, int i) {
   return sizeof(T) == 2 ? 32 * (t >> 1) + 8 * (i >> 2) + 4 * (t & 1) + (i & 3) : 16 * t + i;
 }
 
-// An LDS tile of rows of W elements: chunk c of 16 bytes at c ^ key(row).  The keys keep apart, over the 256 bytes that
-// the banks span, what is read at once: a chunk of 8 rows (0 - 7, or 0 - 3 and 8 - 11), four chunks of four rows, and
-// (fp32) 16 columns of four rows 4 apart.
+// An LDS tile of rows of W elements: chunk c of 16 bytes at c ^ key(row).  A read serves 256 bytes at a time, 16 lanes of
+// 16 bytes or 32 of 8, which the keys spread over all banks: one chunk of 16 rows (0 - 15, or 0 - 3, 8 - 11, 16 - 19 and
+// 24 - 27), two chunks of 8 rows (0 - 3 and 8 - 11), and in fp32 16 columns of four rows 4 apart.
 template <typename T, int W>
 struct Tile {
   static constexpr int E = 16 / sizeof(T), CH = W / E;
   __device__ static inline int key(int row) {
-    if (sizeof(T) == 4) return (((row >> 2) & 3) << 2 | (row & 3)) & (CH - 1);
-    const int b = ((row >> 2) ^ (row >> 3)) & 1;
-    return CH == 8 ? ((row >> 1) & 1) << 2 | b : (row & 3) << 2 | b;
+    if (sizeof(T) == 4) return row & 15;
+    const int b = ((row >> 2) ^ (row >> 4)) & 1, b1 = (row >> 1) & 1, b3 = (row >> 3) & 1;
+    return CH == 8 ? b | b1 << 1 | b3 << 2 : b | (row & 1) << 1 | b1 << 2 | b3 << 3;
   }
   __device__ static inline int at(int row, int c) { return (row * CH + (c ^ key(row))) * E; }
   // Fragment ks along the row.
   __device__ static inline typename Op<T>::Frag along(const T* s, int row, int ks, int lane) {
     return *reinterpret_cast<const typename Op<T>::Frag*>(s + at(row, 4 * ks + (lane >> 4)));
+  }
+  // The same of a bf16 row with the slots of two stacked results: elements 4 g .. and 16 + 4 g .. of a step's 32.
+  __device__ static inline typename Op<T>::Frag stacked(const T* s, int row, int ks, int lane) {
+    if constexpr (sizeof(T) == 2) {
+      const int g = lane >> 4, half = 4 * (g & 1);
+      const bf16x4 lo = *reinterpret_cast<const bf16x4*>(s + at(row, 4 * ks + (g >> 1)) + half);
+      const bf16x4 hi = *reinterpret_cast<const bf16x4*>(s + at(row, 4 * ks + 2 + (g >> 1)) + half);
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      return along(s, row, ks, lane);
+    }
   }
   // Fragment u down the rows, of column `col` of lane i (four adjacent ones of lanes 4 n .. 4 n + 3; the caller gives
   // the first of lane i & 3's four for bf16, the lane's own for fp32).
@@ -108,6 +119,11 @@ __device__ inline int64_t live_tokens(const int32_t* lengths, int64_t b, int64_t
   const int64_t n = lengths[b];
   return n < 0 ? 0 : (n < T ? n : T);
 }
+// A value that all lanes share, for the compiler to know.
+__device__ inline int64_t uniform64(int64_t v) {
+  const unsigned lo = __builtin_amdgcn_readfirstlane(int(v)), hi = __builtin_amdgcn_readfirstlane(int(v >> 32));
+  return int64_t(uint64_t(hi) << 32 | lo);
+}
 // log2 of a head's decay, finite so that its zeroth power is 1.
 __device__ inline float log2_decay(const float* log_decay, int h) {
   const float v = log_decay[h] * kLog2e;
@@ -117,41 +133,49 @@ __device__ inline float log2_decay(const float* log_decay, int h) {
 __device__ const uint4 kZeros = {0, 0, 0, 0};  // rows before the first token, elements beyond the width
 
 // Copies chunks of C rows of up to W elements to LDS, 16 bytes a thread at a time: straight there (VEC: rows of whole,
-// aligned vectors), or through registers.
-template <typename T, int W, bool VEC>
+// aligned vectors), or through registers.  A chunk's address is the same for all lanes, a lane's offset from it (fewer than
+// 64 rows of less than 2^24 elements) the same for all chunks.
+template <typename T, int W, int NT, bool VEC>
 struct Stage {
   typedef Tile<T, W> Tl;
   typedef typename VecN<T, Tl::E>::type Vec;
-  static constexpr int E = Tl::E, CH = Tl::CH, C = Op<T>::C, ITS = C * CH / 256, ROWS = 256 / CH;
-  const T* at;   // this thread's first piece of the next chunk
-  int64_t step;  // elements between tokens
-  int left;      // elements of a row
-  // `p`: element 0 of the first chunk's row 0
-  __device__ inline void start(const T* p, int64_t step_, int left_) {
-    step = step_, left = left_;
-    const int row = threadIdx.x / CH;
-    at = p + row * step + ((threadIdx.x % CH) ^ Tl::key(row)) * E;
+  static constexpr int E = Tl::E, CH = Tl::CH, C = Op<T>::C, ITS = C * CH / NT, ROWS = NT / CH;
+  const char* base;  // of the next chunk: its row with the lowest address
+  int64_t turn;      // bytes between chunks
+  unsigned off[ITS];
+  int left;          // elements of a row
+  // `p`: element 0 of the first chunk's row 0, tokens `stride` elements apart, later ones lower where `reversed`
+  __device__ inline void start(const T* p, int64_t stride, bool reversed, int left_) {
+    left = left_;
+    base = reinterpret_cast<const char*>(p - (reversed ? (C - 1) * stride : 0));
+    turn = (reversed ? -C : C) * stride * int64_t(sizeof(T));
+#pragma unroll
+    for (int it = 0; it < ITS; ++it) {
+      const int row = threadIdx.x / CH + it * ROWS, c = (threadIdx.x % CH) ^ Tl::key(row);
+      off[it] = (unsigned(reversed ? C - 1 - row : row) * unsigned(stride) + c * E) * unsigned(sizeof(T));
+    }
   }
   // The next chunk, of which rows before `first` are zeros.
   __device__ inline void load(T* s, int first) {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = threadIdx.x / CH;
-    const int c0 = (threadIdx.x % CH) ^ Tl::key(row0);
-    const bool edge = first > 0 || left < W;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    auto copy = [&](auto edge) {
 #pragma unroll
-    for (int it = 0; it < ITS; ++it) {
-      const int row = row0 + it * ROWS, c = (threadIdx.x % CH) ^ Tl::key(row);
-      const T* src = at + it * ROWS * step + (c - c0) * E;
-      T* to = s + (it * 256 + wave * 64) * E;
-      const int k = row < first ? 0 : left - c * E;
-      if constexpr (VEC) {
-        const void* from = src;
-        if (edge && k <= 0) from = &kZeros;
-        __builtin_amdgcn_global_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
-      } else {
-        reinterpret_cast<Vec*>(to)[threadIdx.x & 63] = load_n<T, E>(src, k <= 0 ? 0 : (k < E ? k : E), false);
+      for (int it = 0; it < ITS; ++it) {
+        const int row = threadIdx.x / CH + it * ROWS, c = (threadIdx.x % CH) ^ Tl::key(row);
+        const char* src = base + off[it];
+        T* to = s + (it * NT + wave * 64) * E;
+        const int k = row < first ? 0 : left - c * E;
+        if constexpr (VEC) {
+          if (edge.value) copy16_to_lds(lds_address(to), k > 0 ? static_cast<const void*>(src) : &kZeros);
+          else copy16_to_lds(lds_address(to), base, off[it]);
+        } else {
+          reinterpret_cast<Vec*>(to)[threadIdx.x & 63] = load_n<T, E>(reinterpret_cast<const T*>(src), k <= 0 ? 0 : (k < E ? k : E), false);
+        }
       }
-    }
-    at += C * step;
+    };
+    if (!VEC || first > 0 || left < W) copy(std::true_type{});
+    else copy(std::false_type{});
+    base += turn;
   }
 };
 
@@ -169,23 +193,51 @@ __device__ inline f32x4 pack<float>(const f32x4* v) {
   return v[0];
 }
 
+// v w of a fragment's slots as N bf16 parts, which hold 8 bits each of the products (fp32: the product).
+template <int N>
+__device__ inline void weighted(bf16x8 v, const float* w, bf16x8* part) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int x = 0; x < 8; x += 2) {
+    float a = to_f32(__bf16(v[x])) * w[x], b = to_f32(__bf16(v[x + 1])) * w[x + 1];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const bf16x2 y = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
+      part[k][x] = y[0], part[k][x + 1] = y[1];
+      const unsigned bits = __builtin_bit_cast(unsigned, y);
+      a -= __builtin_bit_cast(float, bits << 16), b -= __builtin_bit_cast(float, bits & 0xffff0000u);
+    }
+  }
+}
+template <int N>
+__device__ inline void weighted(f32x4 v, const float* w, f32x4* part) {
+#pragma unroll
+  for (int x = 0; x < 4; ++x) part[0][x] = v[x] * w[x];
+}
+
+// Whether the next chunk's keys (STATE: and values) have LDS of their own to arrive in while this one's are in use.
+constexpr bool keys_ahead(int dk) { return dk <= 128; }
+
 // One segment of one head, 64 NV values a workgroup: a wave holds the state's rows of its 16 NV columns.  d1 <= DK.
 // Chunks end with the segment: the first may begin with rows of zeros, and powers of the decay are the same in all others.
 template <typename T, int DK, int NV, bool STATE, bool VEC>
 __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
   constexpr int KF = Op<T>::KF, C = Op<T>::C, R = KF / 16, QT = C / 16, US = C / KF, KS = DK / KF, DT = DK / 16;
-  constexpr int DV = 64 * NV, NU = US * QT / 4;  // NU: fragments of P^T that a wave forms
+  constexpr int NW = 4, DV = 16 * NW * NV, NU = QT * US / NW;  // NU: fragments of P^T that a wave forms
+  constexpr bool AHEAD = keys_ahead(DK);
   typedef typename Op<T>::Frag Frag;
   typedef Tile<T, DK> TlK;
   typedef Tile<T, DV> TlV;
-  __shared__ __attribute__((aligned(1024))) T sk[C * DK];
-  __shared__ __attribute__((aligned(1024))) T sv[C * DV];
+  __shared__ __attribute__((aligned(1024))) T sk[AHEAD ? 2 : 1][C * DK];
+  __shared__ __attribute__((aligned(1024))) T sv[AHEAD && STATE ? 2 : 1][C * DV];
   __shared__ __attribute__((aligned(1024))) T sq[STATE ? 8 : C * DK];
   __shared__ Frag sp[STATE ? 1 : QT][US][64];
   __shared__ __attribute__((aligned(16))) float sw[C];  // what a token's product counts in the state after the chunk
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i = lane & 15;
 
+  // the sums of segments go through the input in one order, the results in the other: what was read last is still cached
   unsigned id = unsigned(xcd_remap(blockIdx.x, p.groups));
+  if (!STATE && p.S > 1) id = unsigned(p.groups) - 1 - id;
   const unsigned segs = STATE ? p.S - 1 : p.S;
   const int blk = int(id % unsigned(p.blocks));
   id /= unsigned(p.blocks);
@@ -194,90 +246,113 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
   const int h = int(id % unsigned(p.H));
   const int64_t b = id / unsigned(p.H);
   const int d1 = p.a.width, d2 = p.c.width, col0 = blk * DV;
-  const int64_t live = live_tokens(p.lengths, b, p.T), t0 = seg * p.L;
+  const int64_t live = uniform64(live_tokens(p.lengths, b, p.T)), t0 = seg * p.L;
   int64_t n = live - t0 < p.L ? live - t0 : p.L;  // tokens of this segment
   n = n < 0 ? 0 : n;
   const int64_t chunks = (n + C - 1) / C;
   int first = int(chunks * C - n);  // rows of zeros
+  // the segment whose state a caller may get
+  const bool ends = STATE || seg == (live > 0 ? (live - 1) / p.L : 0);
   const float lg = log2_decay(p.log_decay, h);
   const int rho = p.reversed ? 1 : 0;
 
-  // the wave's columns: value tile v, lane i
-  const int wcol = 16 * NV * wave;
-  auto vcol = [&](int v, int x) { return wcol + (NV == 2 ? 8 * (x >> 2) + 4 * v + (x & 3) : x); };
-
   // tokens by their order in time: that of the first chunk's row 0, and the step between two
   const int64_t tok = p.reversed ? live - 1 - (t0 - first) : t0 - first, dir = p.reversed ? -1 : 1;
-  Stage<T, DK, VEC> lk, lq;
-  Stage<T, DV, VEC> lv;
-  lk.start(static_cast<const T*>(p.b.p) + b * p.b.sb + tok * p.b.st + (h / p.b.group) * d1, dir * p.b.st, d1);
-  lv.start(static_cast<const T*>(p.c.p) + b * p.c.sb + tok * p.c.st + (h / p.c.group) * d2 + col0, dir * p.c.st, d2 - col0);
-  if (!STATE) lq.start(static_cast<const T*>(p.a.p) + b * p.a.sb + tok * p.a.st + (h / p.a.group) * d1, dir * p.a.st, d1);
+  Stage<T, DK, 64 * NW, VEC> lk, lq;
+  Stage<T, DV, 64 * NW, VEC> lv;
+  lk.start(static_cast<const T*>(p.b.p) + b * p.b.sb + tok * p.b.st + (h / p.b.group) * d1, p.b.st, p.reversed, d1);
+  lv.start(static_cast<const T*>(p.c.p) + b * p.c.sb + tok * p.c.st + (h / p.c.group) * d2 + col0, p.c.st, p.reversed, d2 - col0);
+  if (!STATE) lq.start(static_cast<const T*>(p.a.p) + b * p.a.sb + tok * p.a.st + (h / p.a.group) * d1, p.a.st, p.reversed, d1);
   if (n > 0) {
-    lk.load(sk, first);
+    lk.load(sk[0], first);
     if (!STATE) lq.load(sq, first);
-    lv.load(sv, first);
+    lv.load(sv[0], first);
   }
   if (threadIdx.x < C) sw[threadIdx.x] = p.in_scale * fast_exp2(lg * float(C - 1 - int(threadIdx.x) + rho));
 
+  // columns: those of tile v that lane i holds; two tiles interleaved in fours, so that a lane's results are adjacent
+  const int wcol = 16 * NV * wave;
+  auto vcol = [&](int v, int x) { return wcol + (NV == 2 ? 8 * (x >> 2) + 4 * v + (x & 3) : x); };
+  auto element = [&](int row, int col) { return p.transposed ? col * d1 + row : row * d2 + col; };
   f32x4 S[DT][NV] = {};
-  if (!STATE && p.first && n > 0) {
+  if (!STATE && p.first && (n > 0 || ends)) {
     const float* f = p.first + ((b * p.H + h) * p.S + seg) * int64_t(d1) * d2;
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
+    for (int t = 0; t < DT; ++t) {
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int row = row_of<T>(t, 4 * g + r), col = col0 + vcol(v, i);
-          if (row < d1 && col < d2) S[t][v][r] = f[p.transposed ? col * d1 + row : row * d2 + col];
+          const int row = 16 * t + 4 * g + r, col = col0 + vcol(v, i);
+          if (row < d1 && col < d2) S[t][v][r] = f[element(row, col)];
         }
+      if (t % 2) __builtin_amdgcn_sched_barrier(0);  // few addresses at a time: registers
+    }
   }
-  // g^(i-j) of the wave's scores, nothing where j > i
+  // g^(i-j) of the wave's scores, nothing where j > i, with both scales
   float pw[NU][R][4];
-  const int qt0 = wave % QT;
 #pragma unroll
   for (int x = 0; x < NU; ++x)
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int gap = 16 * qt0 + i - row_of<T>(R * (wave / QT + x * (4 / QT)) + r, 4 * g + e);
-        pw[x][r][e] = gap >= 0 ? p.in_scale * fast_exp2(lg * float(gap)) : 0.0f;
+        const int item = wave + x * NW, gap = 16 * (item % QT) + i - row_of<T>(R * (item / QT) + r, 4 * g + e);
+        pw[x][r][e] = gap >= 0 ? p.in_scale * p.out_scale * fast_exp2(lg * float(gap)) : 0.0f;
       }
   const int ocol = col0 + wcol + 4 * NV * g, ocount = d2 - ocol < 4 * NV ? d2 - ocol : 4 * NV;
   int64_t orow = ((b * p.T + tok + dir * i) * p.H + h) * d2 + ocol;
   const int64_t ostep = dir * p.H * d2;
 
   for (int64_t ch = 0; ch < chunks; ++ch) {
-    if (VEC) wait_vmem();
+    const T* k_now = sk[AHEAD ? ch & 1 : 0];
+    const T* v_now = sv[AHEAD && STATE ? ch & 1 : 0];
+    const bool more = ch + 1 < chunks;
+    // opaque at every use: the addresses that depend on it would all be formed, and spilled, before the loop
+    auto opaque = [&] {
+      int ln = lane;
+      asm volatile("" : "+v"(ln));
+      return ln;
+    };
+    auto x4 = [](int ln) { return sizeof(T) == 2 ? 4 * (ln & 3) : ln & 15; };  // a lane's column of those read down
+    if (VEC) copies_done();
     __syncthreads();
+    if (AHEAD && more) {
+      lk.load(sk[~ch & 1], 0);
+      if (STATE) lv.load(sv[~ch & (STATE ? 1 : 0)], 0);
+    }
     Frag vf[NV][US];
+    auto values = [&] {
+      const int ln = opaque();
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
+      for (int v = 0; v < NV; ++v)
 #pragma unroll
-      for (int u = 0; u < US; ++u) vf[v][u] = TlV::down(sv, u, sizeof(T) == 2 ? vcol(v, 4 * (i & 3)) : vcol(v, i), lane);
+        for (int u = 0; u < US; ++u) vf[v][u] = TlV::down(v_now, u, vcol(v, x4(ln)), ln);
+    };
+    if (STATE) values();
 
     if constexpr (!STATE) {
       // P^T of 16 queries and the keys up to them
 #pragma unroll
       for (int x = 0; x < NU; ++x) {
-        const int u = wave / QT + x * (4 / QT);
-        if (u * KF > 16 * qt0 + 15) continue;
+        const int qt = (wave + x * NW) % QT, u = (wave + x * NW) / QT;
+        if (u * KF > 16 * qt + 15) continue;
         f32x4 pt[R] = {};
+        const int ln = opaque();
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          const Frag q = TlK::along(sq, 16 * qt0 + i, ks, lane);
+          const Frag q = TlK::along(sq, 16 * qt + (ln & 15), ks, ln);
 #pragma unroll
-          for (int r = 0; r < R; ++r) pt[r] = Op<T>::mma(TlK::along(sk, row_of<T>(R * u + r, i), ks, lane), q, pt[r]);
+          for (int r = 0; r < R; ++r) pt[r] = Op<T>::mma(TlK::along(k_now, row_of<T>(R * u + r, ln & 15), ks, ln), q, pt[r]);
         }
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
           for (int e = 0; e < 4; ++e) pt[r][e] *= pw[x][r][e];
-        sp[qt0][u][lane] = pack<T>(pt);
+        sp[qt][u][lane] = pack<T>(pt);
       }
       f32x4 o[QT][NV] = {};
+      const int ln = opaque();
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         Frag s[NV];
@@ -290,19 +365,24 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
         }
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
-          const Frag q = TlK::along(sq, 16 * qt + i, ks, lane);
+          const Frag q = TlK::stacked(sq, 16 * qt + (ln & 15), ks, ln);
 #pragma unroll
           for (int v = 0; v < NV; ++v) o[qt][v] = Op<T>::mma(s[v], q, o[qt][v]);
         }
       }
+      values();
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt) {
         const int after = 16 * qt + i + 1 - rho - first;
-        const float w = fast_exp2(lg * float(after > 0 ? after : 0));
+        const float w = p.out_scale * fast_exp2(lg * float(after > 0 ? after : 0));
 #pragma unroll
         for (int v = 0; v < NV; ++v) o[qt][v] *= w;
       }
       __syncthreads();
+      if (more) {
+        lq.load(sq, 0);
+        lv.load(sv[0], 0);
+      }
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt)
 #pragma unroll
@@ -312,23 +392,26 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
 #pragma unroll
           for (int v = 0; v < NV; ++v) o[qt][v] = Op<T>::mma(vf[v][u], pf, o[qt][v]);
         }
+      if (ocount > 0) {
 #pragma unroll
-      for (int qt = 0; qt < QT; ++qt) {
-        if (16 * qt + i < first || ocount <= 0) continue;
-        float f[4 * NV];
+        for (int qt = 0; qt < QT; ++qt) {
+          float f[4 * NV];
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
+          for (int v = 0; v < NV; ++v)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) f[4 * v + r] = o[qt][v][r] * p.out_scale;
-        const int64_t e = orow + 16 * qt * ostep;
-        if (VEC && p.vec_out) store_n<T, 4 * NV>(static_cast<T*>(p.out) + e, f, ocount, true);
-        else if (p.wide) store_n<float, 4 * NV>(static_cast<float*>(p.out) + e, f, ocount, false);
-        else store_n<T, 4 * NV>(static_cast<T*>(p.out) + e, f, ocount, false);
+            for (int r = 0; r < 4; ++r) f[4 * v + r] = o[qt][v][r];
+          const int64_t e = orow + 16 * qt * ostep;
+          const bool in = 16 * qt + i >= first;
+          if (!in) continue;
+          if (p.wide) store_n<float, 4 * NV>(static_cast<float*>(p.out) + e, f, VEC ? 4 * NV : ocount, VEC);
+          else store_n<T, 4 * NV>(static_cast<T*>(p.out) + e, f, VEC ? 4 * NV : ocount, VEC);
+        }
       }
       orow += C * ostep;
     }
 
-    // the state after the chunk; values times powers of the decay in three bf16 parts, which hold all of fp32's bits
+    // the state after the chunk; values times powers of the decay in bf16 parts, three where fp32's bits are wanted and
+    // two (16 bits) where only rounded results come of it
     const float carry = fast_exp2(lg * float(C - first));
 #pragma unroll
     for (int t = 0; t < DT; ++t)
@@ -336,8 +419,6 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
       for (int v = 0; v < NV; ++v) S[t][v] *= carry;
 #pragma unroll
     for (int u = 0; u < US; ++u) {
-      constexpr int PARTS = sizeof(T) == 2 ? 3 : 1;
-      Frag part[NV][PARTS];
       float w[KF / 4];
 #pragma unroll
       for (int x = 0; x < KF / 4; x += 4) {
@@ -345,61 +426,68 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[x + e] = y[e];
       }
+      // adds the parts from `from` on to the state
+      auto add = [&](auto from, auto to) {
+        constexpr int P0 = decltype(from)::value, P1 = decltype(to)::value;
+        Frag part[NV][P1];
 #pragma unroll
-      for (int x = 0; x < KF / 4; ++x)
+        for (int v = 0; v < NV; ++v) weighted<P1>(vf[v][u], w, part[v]);
+        const int ln = opaque();
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-          float f = to_f32(T(vf[v][u][x])) * w[x];
+        for (int t = 0; t < DT; t += 2) {  // several sums at a time: a product does not wait for the one before
+          Frag k[2];
 #pragma unroll
-          for (int k = 0; k < PARTS; ++k) {
-            const T y = from_f32<T>(f);
-            part[v][k][x] = y;
-            f -= to_f32(y);
-          }
+          for (int x = 0; x < 2; ++x) k[x] = TlK::down(k_now, u, 16 * (t + x) + x4(ln), ln);
+#pragma unroll
+          for (int y = P0; y < P1; ++y)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+              for (int v = 0; v < NV; ++v) S[t + x][v] = Op<T>::mma(k[x], part[v][y], S[t + x][v]);
         }
-#pragma unroll
-      for (int t = 0; t < DT; ++t) {
-        const Frag k = TlK::down(sk, u, sizeof(T) == 2 ? row_of<T>(t, 4 * (i & 3)) : row_of<T>(t, i), lane);
-#pragma unroll
-        for (int v = 0; v < NV; ++v)
-#pragma unroll
-          for (int x = 0; x < PARTS; ++x) S[t][v] = Op<T>::mma(k, part[v][x], S[t][v]);
+      };
+      typedef std::integral_constant<int, 0> None;
+      if constexpr (sizeof(T) == 4) {
+        add(None{}, std::integral_constant<int, 1>{});
+      } else if constexpr (STATE) {
+        add(None{}, std::integral_constant<int, 3>{});
+      } else {
+        add(None{}, std::integral_constant<int, 2>{});
+        if (ends) add(std::integral_constant<int, 2>{}, std::integral_constant<int, 3>{});
       }
     }
-    __syncthreads();
-    first = 0;
-    if (ch + 1 < chunks) {
-      lk.load(sk, 0);
-      if (!STATE) lq.load(sq, 0);
-      lv.load(sv, 0);
+    if (!AHEAD) {
+      __syncthreads();
+      if (more) {
+        lk.load(sk[0], 0);
+        if (STATE) lv.load(sv[0], 0);
+      }
     }
+    first = 0;
   }
 
   // STATE: this segment's own sums, where the next one starts.  Else the final state, of the segment that ends there.
   float* to = nullptr;
   if (STATE) to = p.last + ((b * p.H + h) * p.S + seg + 1) * int64_t(d1) * d2;
-  else if (p.last && seg == (live > 0 ? (live - 1) / p.L : 0)) to = p.last + (b * p.H + h) * int64_t(d1) * d2;
+  else if (p.last && ends) to = p.last + (b * p.H + h) * int64_t(d1) * d2;
   if (to) {
-    const bool keep = !STATE && n == 0 && p.first;  // an empty sequence ends where it begins
-    const float* f = p.first + (b * p.H + h) * p.S * int64_t(d1) * d2;
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
+    for (int t = 0; t < DT; ++t) {
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int row = row_of<T>(t, 4 * g + r), col = col0 + vcol(v, i);
-          if (row < d1 && col < d2) {
-            const int e = p.transposed ? col * d1 + row : row * d2 + col;
-            to[e] = keep ? f[e] : S[t][v][r];
-          }
+          const int row = 16 * t + 4 * g + r, col = col0 + vcol(v, i);
+          if (row < d1 && col < d2) to[element(row, col)] = S[t][v][r];
         }
+      if (t % 2) __builtin_amdgcn_sched_barrier(0);
+    }
   }
   // rows after the sequence's end
   if (!STATE) {
     const int64_t end = t0 + p.L < p.T ? t0 + p.L : p.T, from = live > t0 ? live : t0;
     const int cols = d2 - col0 < DV ? d2 - col0 : DV;
-    for (int64_t t = from + wave; t < end; t += 4) {
+    for (int64_t t = from + wave; t < end; t += NW) {
       const int64_t e = ((b * p.T + t) * p.H + h) * d2 + col0;
       for (int c = lane; c < cols; c += 64) {
         if (p.wide) static_cast<float*>(p.out)[e + c] = 0.0f;
@@ -516,9 +604,9 @@ int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 struct Split {
   int64_t L, S;
 };
-// Segments of whole chunks: enough for 1024 workgroups of a head each, of 512 tokens at least.
+// Segments of whole chunks: enough for 512 workgroups of a head each, of 512 tokens at least.
 Split split_of(int64_t B, int64_t T, int64_t H) {
-  int64_t S = ceil_div(1024, B * H);
+  int64_t S = ceil_div(512, B * H);
   S = S < T / 512 ? S : T / 512;
   S = S < 1 ? 1 : S;
   Split q;
@@ -534,12 +622,13 @@ Heads heads_of(const Rows& r, int64_t heads, int64_t H, int64_t width, int esize
   return {r.p, r.sb, r.st, int(width), int(H / heads), rows_aligned(r, esize, n) && width % n == 0};
 }
 
+// Tiles of 16 values that a wave holds: two where it has registers for them.
 int value_tiles(int64_t d1, int64_t d2) { return d1 <= 128 && d2 > 64 ? 2 : 1; }
 
 template <typename T, int DK, int NV>
 hipError_t launch_attend(const DecayDev& p, bool state, hipStream_t st) {
   const dim3 grid(uint32_t(p.groups)), block(256);
-  const bool vec = p.b.vec && p.c.vec && (state || p.a.vec);
+  const bool vec = p.b.vec && p.c.vec && (state || (p.a.vec && p.vec_out));
   if (state) vec ? k_attend<T, DK, NV, true, true><<<grid, block, 0, st>>>(p) : k_attend<T, DK, NV, true, false><<<grid, block, 0, st>>>(p);
   else vec ? k_attend<T, DK, NV, false, true><<<grid, block, 0, st>>>(p) : k_attend<T, DK, NV, false, false><<<grid, block, 0, st>>>(p);
   return hipGetLastError();
@@ -550,7 +639,7 @@ hipError_t attend(DecayDev p, int64_t B, bool state, hipStream_t st) {
   const int nv = value_tiles(p.a.width, p.c.width);
   p.blocks = int(ceil_div(p.c.width, 64 * nv));
   p.groups = B * p.H * p.blocks * (state ? p.S - 1 : p.S);
-  p.vec_out = !p.wide && p.c.width % (4 * nv) == 0 && reinterpret_cast<uintptr_t>(p.out) % (4 * nv * sizeof(T)) == 0;
+  p.vec_out = reinterpret_cast<uintptr_t>(p.out) % 16 == 0 && p.c.width % 8 == 0;  // rows of whole vectors of 4 NV
   if (p.a.width <= 64) return nv == 2 ? launch_attend<T, 64, 2>(p, state, st) : launch_attend<T, 64, 1>(p, state, st);
   if (p.a.width <= 128) return nv == 2 ? launch_attend<T, 128, 2>(p, state, st) : launch_attend<T, 128, 1>(p, state, st);
   return launch_attend<T, 256, 1>(p, state, st);
@@ -679,10 +768,10 @@ int64_t decay_workspace(int64_t B, int64_t T, int64_t H, int64_t Hqk, int64_t dk
 }
 bool decay_launchable(const DecayArgs& a, bool backward) {
   const int64_t S = split_of(a.B, a.T, a.H).S, heads = a.B * a.H;
-  auto blocks = [](int64_t d1, int64_t d2) { return ceil_div(d2, 64 * value_tiles(d1, d2)); };
-  if (!launchable(heads * S * blocks(a.dk, a.dv), 256) || !launchable(ceil_div(heads * a.dk * a.dv, 256), 256)) return false;
+  auto attends = [&](int64_t d1, int64_t d2) { return launchable(heads * S * ceil_div(d2, 64 * value_tiles(d1, d2)), 256); };
+  if (!attends(a.dk, a.dv) || !launchable(ceil_div(heads * a.dk * a.dv, 256), 256)) return false;
   if (!backward) return true;
-  return launchable(heads * S * blocks(a.dv, a.dk), 256) &&
+  return attends(a.dv, a.dk) &&
          (a.Hqk == a.H || launchable(ceil_div(a.B * a.T * a.Hqk * a.dk, 256), 256));
 }
 bool decay_step_launchable(const DecayArgs& a) { return launchable(a.B * a.H, 256); }

@@ -89,6 +89,21 @@ __device__ inline float softplusf(float v) {
   return fmaf(s + s, p, v > 0.0f ? v : 0.0f);
 }
 
+// Direct copies of 16 bytes a lane to LDS, lane l's to `lds` + 16 l.  In inline assembly: before every LDS read the compiler
+// waits for all such copies that it knows of, also those of another buffer that are to arrive meanwhile.  The caller waits
+// for them itself (copies_done, then a barrier) before they are read; a memory barrier for the compiler either way.  M0 takes
+// one wait state between its write and its use.
+// The low half of a pointer into LDS is its address there.
+__device__ inline unsigned lds_address(const void* p) { return __builtin_amdgcn_readfirstlane(unsigned(reinterpret_cast<uintptr_t>(p))); }
+__device__ inline void copy16_to_lds(unsigned lds, const void* from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
+}
+// From a lane's offset to an address that all lanes share.
+__device__ inline void copy16_to_lds(unsigned lds, const void* base, unsigned offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
+}
+__device__ inline void copies_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // The lanes of one wave exchange data through LDS without a workgroup barrier: the LDS serves a
 // wave's accesses in order, so only the compiler has to keep theirs.
 __device__ inline void wave_sync() {

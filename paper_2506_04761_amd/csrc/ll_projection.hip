@@ -125,7 +125,7 @@ struct Copy {
       if constexpr (DIRECT) {
         const void* from = src[it];
         if (left < Tl::BK && ofs[it] >= left) from = &kZeros;
-        __builtin_amdgcn_global_load_lds(from, (__attribute__((address_space(3))) void*)(lds + (it * NT + wave * 64) * E), 16, 0, 0);
+        copy16_to_lds(lds_address(lds + (it * NT + wave * 64) * E), from);
       } else {
         int n = count[it];
         if (left < Tl::BK) {
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm(GemmDev p) {
   for (int st = 0; st < stages; ++st) {
     T* now = s + (st & 1) * kStage;
     T* next = s + (~st & 1) * kStage;
-    if (DIRECT) wait_vmem();
+    if (DIRECT) copies_done();
     __syncthreads();
     left -= BK;
     if (left > 0) {

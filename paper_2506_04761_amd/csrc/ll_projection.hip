@@ -39,34 +39,38 @@ __device__ inline int output_of(int t, int i) { return 32 * (t >> 1) + 8 * (i >>
 
 constexpr int kStageBytes = 128;  // of k
 
-// The LDS tile of TD outputs' stage: 16-byte chunks, chunk c of a row at c ^ key(row), with keys for which the lanes that
-// an LDS read serves together (rows 0 - 3 and 8 - 11 along; four rows of four chunks, or four rows 4 apart, down) touch
-// different banks.
-template <typename T, int TD, bool DOWN>
+// The LDS tile of TD outputs' stage: 16-byte chunks, chunk c of a row at c ^ key(row).  A read serves 256 bytes at a time,
+// 16 lanes of 16 bytes or 32 of 8; with these keys it finds them in different banks: along, a chunk of the 16 rows
+// output_of(t, 0 .. 15); down, two chunks of 8 rows (0 - 3 and 8 - 11) or in fp32 four chunks of four rows 4 apart.
+// PAIRED: outputs in the order of output_of, else 16 t + i (down in bf16 half of a chunk each is read of a pair, so that
+// the banks serve it at half their rate).
+template <typename T, int TD, bool DOWN, bool PAIRED>
 struct Tile {
   static constexpr int E = 16 / sizeof(T);
   static constexpr int BK = kStageBytes / sizeof(T);
   static constexpr int CH = DOWN ? TD / E : 8;  // chunks of a row
   __device__ static inline int key(int row) {
-    if (!DOWN) return (row & 3) | ((row >> 1) & 4);
+    const int b1 = (row >> 1) & 1, b3 = (row >> 3) & 1;
+    if (!DOWN) return b1 | b3 << 1 | ((row >> 4) & 1) << 2;
     if (sizeof(T) == 4) return ((row >> 2) & 1) | (row & 8);
-    return CH == 8 ? 4 * ((row >> 1) & 1) : 4 * (row & 3);
+    return CH == 8 ? b1 << 1 | b3 << 2 : (row & 1) << 1 | b1 << 2 | b3 << 3;
   }
+  __device__ static inline int output(int t, int i) { return PAIRED ? output_of(t, i) : 16 * t + i; }
   // Fragment t of k step ks of the outputs from d0 on.
   __device__ static inline typename Op<T>::Frag frag(const T* s, int d0, int t, int ks, int lane) {
     const int g = lane >> 4, i = lane & 15;
     if constexpr (!DOWN) {
-      const int row = d0 + output_of(t, i);
+      const int row = d0 + output(t, i);
       return *reinterpret_cast<const typename Op<T>::Frag*>(s + (row * CH + ((4 * ks + g) ^ key(row))) * E);
     } else if constexpr (sizeof(T) == 2) {
       // lane 4 j + c of 16 supplies four outputs of row j, see lds_read_tr
-      const int row = 32 * ks + 8 * g + (i >> 2), d = d0 + output_of(t, 4 * (i & 3));
+      const int row = 32 * ks + 8 * g + (i >> 2), d = d0 + output(t, 4 * (i & 3));
       const int at = (d >> 3) ^ key(row);
       const bf16x4 lo = lds_read_tr(s + (row * CH + at) * E + (d & 7));
       const bf16x4 hi = lds_read_tr(s + ((row + 4) * CH + at) * E + (d & 7));
       return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
-      const int row = 16 * ks + 4 * g, d = d0 + output_of(t, i);
+      const int row = 16 * ks + 4 * g, d = d0 + output(t, i);
       const int at = (d >> 2) ^ key(row);
       f32x4 f;
 #pragma unroll
@@ -85,58 +89,51 @@ struct Side {
 __device__ const uint4 kZeros = {0, 0, 0, 0};  // the k beyond the last
 
 // Copies stages of an operand to LDS, 16 bytes a thread at a time: straight there (DIRECT: rows of whole, aligned
-// chunks), or through registers (any rows).
-template <typename T, int TD, bool DOWN, bool DIRECT, int NT>
+// chunks), or through registers (any rows).  A stage's address is the same for all lanes, a lane's offset from it (at most
+// 64 rows of less than 2^24 elements) the same for all stages.
+template <typename T, typename Tl, int TD, bool DOWN, bool DIRECT, int NT>
 struct Copy {
-  typedef Tile<T, TD, DOWN> Tl;
   typedef typename VecN<T, Tl::E>::type Vec;
-  static constexpr int E = Tl::E, ITS = TD * 8 / NT;
-  const T* src[ITS];
-  int ofs[ITS];    // first k of the chunk within a stage
-  int count[ITS];  // outputs (down) or rows (along, 0 or E) that are inputs
+  static constexpr int E = Tl::E, CH = Tl::CH, ITS = TD * 8 / NT, ROWS = NT / CH;
+  const char* base;  // of the next stage
+  int64_t turn, jump;  // bytes between stages, between a lane's rows
+  unsigned off[ITS];
+  int64_t n;         // outputs from the tile's first on
   Vec held[DIRECT ? 1 : ITS];
-  int64_t step;
 
   __device__ inline void start(const Side& s, int64_t d0, int64_t k0) {
-    step = DOWN ? Tl::BK * s.stride : Tl::BK;
+    n = s.n - d0;
+    base = static_cast<const char*>(s.p) + (DOWN ? k0 * s.stride + d0 : d0 * s.stride + k0) * int64_t(sizeof(T));
+    turn = (DOWN ? Tl::BK * s.stride : Tl::BK) * int64_t(sizeof(T));
+    jump = ROWS * s.stride * int64_t(sizeof(T));
 #pragma unroll
     for (int it = 0; it < ITS; ++it) {
-      const int q = it * NT + threadIdx.x, row = q / Tl::CH, c = (q % Tl::CH) ^ Tl::key(row);
-      if (DOWN) {
-        int64_t d = d0 + c * E;
-        ofs[it] = row;
-        count[it] = d >= s.n ? 0 : (s.n - d < E ? int(s.n - d) : E);
-        if (DIRECT && d > s.n - E) d = s.n - E;  // some input, for outputs that are not stored
-        src[it] = static_cast<const T*>(s.p) + (k0 + row) * s.stride + d;
-      } else {
-        int64_t d = d0 + row;
-        ofs[it] = c * E;
-        count[it] = d < s.n ? E : 0;
-        if (DIRECT && d >= s.n) d = s.n - 1;
-        src[it] = static_cast<const T*>(s.p) + d * s.stride + k0 + c * E;
-      }
+      const int row0 = threadIdx.x / CH;
+      off[it] = (unsigned(row0) * unsigned(s.stride) + chunk(row0 + it * ROWS) * E) * unsigned(sizeof(T));
     }
   }
+  __device__ static inline int chunk(int row) { return (threadIdx.x % CH) ^ Tl::key(row); }
   // Begins the copy of the next stage, of which `left` k are inputs.
   __device__ inline void load(T* lds, int64_t left) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (DIRECT && left >= Tl::BK && n >= TD) {
 #pragma unroll
-    for (int it = 0; it < ITS; ++it) {
-      if constexpr (DIRECT) {
-        const void* from = src[it];
-        if (left < Tl::BK && ofs[it] >= left) from = &kZeros;
-        copy16_to_lds(lds_address(lds + (it * NT + wave * 64) * E), from);
-      } else {
-        int n = count[it];
-        if (left < Tl::BK) {
-          const int k = int(left) - ofs[it];
-          if (DOWN) n = k > 0 ? n : 0;
-          else n = n == 0 || k <= 0 ? 0 : (k < E ? k : E);
+      for (int it = 0; it < ITS; ++it) copy16_to_lds(lds_address(lds + (it * NT + wave * 64) * E), base + it * jump, off[it]);
+    } else {
+#pragma unroll
+      for (int it = 0; it < ITS; ++it) {
+        const int row = threadIdx.x / CH + it * ROWS, c = chunk(row);
+        const int64_t k = left - (DOWN ? row : c * E), d = n - (DOWN ? c * E : row);  // what is left from here on
+        const char* src = base + it * jump + off[it];
+        if constexpr (DIRECT) {
+          copy16_to_lds(lds_address(lds + (it * NT + wave * 64) * E), k > 0 && d > 0 ? static_cast<const void*>(src) : &kZeros);
+        } else {
+          const int64_t m = k <= 0 || d <= 0 ? 0 : (DOWN ? d : k);
+          held[it] = load_n<T, E>(reinterpret_cast<const T*>(src), m < E ? int(m) : E, false);
         }
-        held[it] = load_n<T, E>(src[it], n, false);
       }
-      src[it] += step;
     }
+    base += turn;
   }
   // Through registers: ends the copy.
   __device__ inline void store(T* lds) {
@@ -191,10 +188,10 @@ struct GemmDev {
 };
 
 template <typename T, int TM, int TN, int WM, int WN, bool DOWN_M, bool DOWN_N, bool DIRECT>
-__global__ __launch_bounds__(64 * WM * WN) void k_gemm(GemmDev p) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_gemm(GemmDev p) {
   constexpr int NT = 64 * WM * WN, FM = TM / WM / 16, FN = TN / WN / 16;
-  typedef Tile<T, TM, DOWN_M> TlM;
-  typedef Tile<T, TN, DOWN_N> TlN;
+  typedef Tile<T, TM, DOWN_M, !(DOWN_M && sizeof(T) == 2)> TlM;
+  typedef Tile<T, TN, DOWN_N, true> TlN;
   constexpr int BK = TlM::BK, KS = BK / Op<T>::KF;
   constexpr int kStage = (TM + TN) * BK;
   __shared__ __attribute__((aligned(1024))) T s[2 * kStage];
@@ -202,18 +199,18 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm(GemmDev p) {
   const int wm = wave / WN * (TM / WM), wn = wave % WN * (TN / WN);
 
   // an XCD takes adjacent tiles, eight rows of tiles at a time, so that its L2 serves both operands
-  const int64_t tiles = p.m_tiles * p.n_tiles;
-  int64_t id = xcd_remap(blockIdx.x, tiles * p.splits);
-  const int64_t split = id / tiles;
+  const unsigned m_tiles = unsigned(p.m_tiles), n_tiles = unsigned(p.n_tiles), tiles = m_tiles * n_tiles;
+  unsigned id = unsigned(xcd_remap(blockIdx.x, int64_t(tiles) * p.splits));
+  const unsigned split = id / tiles;
   id %= tiles;
-  const int64_t strip = id / (8 * p.n_tiles), rows = p.m_tiles - 8 * strip < 8 ? p.m_tiles - 8 * strip : 8;
-  id %= 8 * p.n_tiles;
-  const int64_t m0 = (8 * strip + id % rows) * TM, n0 = id / rows * TN;
+  const unsigned strip = id / (8 * n_tiles), rows = m_tiles - 8 * strip < 8 ? m_tiles - 8 * strip : 8;
+  id %= 8 * n_tiles;
+  const int64_t m0 = int64_t(8 * strip + id % rows) * TM, n0 = int64_t(id / rows) * TN;
 
   const int64_t k0 = split * p.span;
   int64_t left = p.K - k0 < p.span ? p.K - k0 : p.span;
-  Copy<T, TM, DOWN_M, DIRECT, NT> cm;
-  Copy<T, TN, DOWN_N, DIRECT, NT> cn;
+  Copy<T, TlM, TM, DOWN_M, DIRECT, NT> cm;
+  Copy<T, TlN, TN, DOWN_N, DIRECT, NT> cn;
   cm.start(p.b, m0, k0);
   cn.start(p.a, n0, k0);
   f32x4 acc[FM][FN] = {};
@@ -251,7 +248,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_gemm(GemmDev p) {
   }
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
-    const int64_t m = m0 + wm + output_of(i, lane & 15);
+    const int64_t m = m0 + wm + TlM::output(i, lane & 15);
 #pragma unroll
     for (int j = 0; j < FN; j += 2) {
       const int64_t n = n0 + wn + 16 * j + 8 * (lane >> 4);
@@ -393,7 +390,7 @@ GemmPlan plan(int64_t M, int64_t N, int64_t K, int dtype, Product what) {
     return q;
   }
   auto tiles = [&](int t) { return ceil_div(M, t) * ceil_div(N, t); };
-  q.tile = tiles(128) >= 256 ? 128 : 64;
+  q.tile = tiles(256) >= 256 ? 256 : tiles(128) >= 256 ? 128 : 64;
   q.m_tiles = ceil_div(M, q.tile), q.n_tiles = ceil_div(N, q.tile);
   const int64_t n = q.m_tiles * q.n_tiles;
   if (n < 256) {
@@ -447,7 +444,8 @@ bool direct(const Side& s, bool down, int64_t K, int esize) {
 
 template <typename T, int TILE, bool DM, bool DN, bool DIRECT>
 void launch_tiles(const GemmDev& p, int64_t workgroups, hipStream_t st) {
-  k_gemm<T, TILE, TILE, 2, 2, DM, DN, DIRECT><<<dim3(uint32_t(workgroups)), dim3(256), 0, st>>>(p);
+  constexpr int WM = 2, WN = TILE == 256 ? 4 : 2;
+  k_gemm<T, TILE, TILE, WM, WN, DM, DN, DIRECT><<<dim3(uint32_t(workgroups)), dim3(64 * WM * WN), 0, st>>>(p);
 }
 
 template <typename T, bool DM, bool DN>
@@ -455,7 +453,8 @@ hipError_t launch_product(GemmDev p, const GemmPlan& q, float* part, hipStream_t
   p.m_tiles = q.m_tiles, p.n_tiles = q.n_tiles, p.splits = q.splits, p.span = q.span;
   p.part = q.splits > 1 ? part : nullptr;
   const bool dir = direct(p.b, DM, p.K, sizeof(T)) && direct(p.a, DN, p.K, sizeof(T));
-  if (q.tile == 128) dir ? launch_tiles<T, 128, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 128, DM, DN, false>(p, q.workgroups, st);
+  if (q.tile == 256) dir ? launch_tiles<T, 256, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 256, DM, DN, false>(p, q.workgroups, st);
+  else if (q.tile == 128) dir ? launch_tiles<T, 128, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 128, DM, DN, false>(p, q.workgroups, st);
   else dir ? launch_tiles<T, 64, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 64, DM, DN, false>(p, q.workgroups, st);
   if (q.splits > 1) {
     p.part = part;
@@ -528,7 +527,7 @@ int64_t projection_workspace(int64_t M, int64_t K, int64_t N, int act, int dtype
 
 bool projection_launchable(int64_t M, int64_t K, int64_t N, int act, int dtype, bool backward) {
   auto ok = [](const GemmPlan& q, int64_t m, int64_t n) {
-    return launchable(q.workgroups, q.few ? 64 * kFewWaves : 256) && (q.splits == 1 || launchable(ceil_div(m * ceil_div(n, 4), 256), 256));
+    return launchable(q.workgroups, 64 * kFewWaves) && (q.splits == 1 || launchable(ceil_div(m * ceil_div(n, 4), 256), 256));
   };
   if (!backward) return ok(plan(M, N, K, dtype, kForward), M, N);
   const BwdPlan q = bwd_plan(M, K, N, dtype, act != 0);

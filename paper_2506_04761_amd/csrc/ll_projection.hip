@@ -380,7 +380,19 @@ struct GemmPlan {
   int64_t bytes = 0;       // of partial sums
 };
 
-// out [M, N] over K.
+// What a stage takes on a compute unit that holds n workgroups (at most `most`) of a tile, and a workgroup's results, in
+// us: fitted to products of 128 to 65536 rows in 1 to 32 splits (the choice is within 15 % of the best of those).
+struct TileCost {
+  int tile, most;
+  double stage, each, results;
+};
+constexpr TileCost kCosts[2][3] = {{{64, 5, 0.1, 0.6, 1.0}, {128, 2, 0.2, 2.1, 1.5}, {0, 0, 0, 0, 0}},
+                                   {{64, 5, 0.35, 0.09, 1.0}, {128, 2, 0.39, 0.35, 1.5}, {256, 1, 0, 1.65, 5.0}}};
+
+// out [M, N] over K: the tile and the splits of K that take the least time by those costs.  Larger tiles read less from
+// LDS (8192 x 1024 over 8192 in bf16: tiles of 64 202 us, of 128 152, of 256 in two splits 133), smaller ones and splits
+// fill more compute units (1024 x 1024 over 1024: 11.6, 15.2 and 26.6 us; 1024 x 2048 over 8064: 128 without splits 68, in
+// four 49).
 GemmPlan plan(int64_t M, int64_t N, int64_t K, int dtype, Product what) {
   GemmPlan q;
   const int64_t BK = kStageBytes / elem(dtype), stages = ceil_div(K, BK);
@@ -389,18 +401,23 @@ GemmPlan plan(int64_t M, int64_t N, int64_t K, int dtype, Product what) {
     q.workgroups = ceil_div(N, 16);
     return q;
   }
-  auto tiles = [&](int t) { return ceil_div(M, t) * ceil_div(N, t); };
-  q.tile = tiles(256) >= 256 ? 256 : tiles(128) >= 256 ? 128 : 64;
-  q.m_tiles = ceil_div(M, q.tile), q.n_tiles = ceil_div(N, q.tile);
-  const int64_t n = q.m_tiles * q.n_tiles;
-  if (n < 256) {
-    q.splits = 512 / n < stages / 4 ? 512 / n : stages / 4;
-    q.splits = q.splits < 1 ? 1 : (q.splits > 32 ? 32 : q.splits);
+  double best = 0;
+  for (const TileCost& c : kCosts[dtype]) {
+    if (!c.tile) continue;
+    const int64_t m_tiles = ceil_div(M, c.tile), n_tiles = ceil_div(N, c.tile);
+    for (const int64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+      const int64_t each = ceil_div(stages, want), splits = ceil_div(stages, each);
+      if (want > 1 && (want > stages / 2 || m_tiles * n_tiles * want > 2304)) break;
+      const int64_t a_unit = ceil_div(m_tiles * n_tiles * splits, 256), rounds = a_unit / c.most, rest = a_unit % c.most;
+      auto round = [&](int64_t n) { return n ? each * (c.stage + n * c.each) + c.results : 0.0; };
+      const double join = splits > 1 ? 3 + double(splits) * M * N * 8 / 7e6 : 0;
+      const double us = rounds * round(c.most) + round(rest) + join;
+      if (q.tile && us >= best) continue;
+      best = us;
+      q.tile = c.tile, q.m_tiles = m_tiles, q.n_tiles = n_tiles, q.splits = splits, q.span = each * BK;
+    }
   }
-  const int64_t each = ceil_div(stages, q.splits);
-  q.span = each * BK;
-  q.splits = ceil_div(stages, each);
-  q.workgroups = n * q.splits;
+  q.workgroups = q.m_tiles * q.n_tiles * q.splits;
   q.bytes = q.splits > 1 ? q.splits * M * N * 4 : 0;
   return q;
 }
@@ -453,9 +470,11 @@ hipError_t launch_product(GemmDev p, const GemmPlan& q, float* part, hipStream_t
   p.m_tiles = q.m_tiles, p.n_tiles = q.n_tiles, p.splits = q.splits, p.span = q.span;
   p.part = q.splits > 1 ? part : nullptr;
   const bool dir = direct(p.b, DM, p.K, sizeof(T)) && direct(p.a, DN, p.K, sizeof(T));
-  if (q.tile == 256) dir ? launch_tiles<T, 256, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 256, DM, DN, false>(p, q.workgroups, st);
-  else if (q.tile == 128) dir ? launch_tiles<T, 128, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 128, DM, DN, false>(p, q.workgroups, st);
-  else dir ? launch_tiles<T, 64, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 64, DM, DN, false>(p, q.workgroups, st);
+  if constexpr (sizeof(T) == 2) {
+    if (q.tile == 256) dir ? launch_tiles<T, 256, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 256, DM, DN, false>(p, q.workgroups, st);
+  }
+  if (q.tile == 128) dir ? launch_tiles<T, 128, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 128, DM, DN, false>(p, q.workgroups, st);
+  else if (q.tile == 64) dir ? launch_tiles<T, 64, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 64, DM, DN, false>(p, q.workgroups, st);
   if (q.splits > 1) {
     p.part = part;
     k_gemm_join<T><<<dim3(uint32_t(ceil_div(p.f.M * ceil_div(p.f.N, 4), 256))), dim3(256), 0, st>>>(p);

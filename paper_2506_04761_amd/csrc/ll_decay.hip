@@ -52,30 +52,61 @@ __device__ inline int row_of(int t, int i) {
 template <typename T, int W>
 struct Tile {
   static constexpr int E = 16 / sizeof(T), CH = W / E;
-  __device__ static inline int key(int row) {
+  __device__ static inline constexpr int key(int row) {
     if (sizeof(T) == 4) return row & 15;
     const int b = ((row >> 2) ^ (row >> 4)) & 1, b1 = (row >> 1) & 1, b3 = (row >> 3) & 1;
     return CH == 8 ? b | b1 << 1 | b3 << 2 : b | (row & 1) << 1 | b1 << 2 | b3 << 3;
   }
   __device__ static inline int at(int row, int c) { return (row * CH + (c ^ key(row))) * E; }
-  // Fragment ks along the row.
-  __device__ static inline typename Op<T>::Frag along(const T* s, int row, int ks, int lane) {
-    return *reinterpret_cast<const typename Op<T>::Frag*>(s + at(row, 4 * ks + (lane >> 4)));
+  // Addresses of fragments in LDS: a lane's of the first, which the others' differ from by exclusive ors and sums of
+  // constants.  (Their keys differ by the constant rows' own, as no sum of a row carries, and a tile begins at a multiple
+  // of 1024.)
+  __device__ static inline unsigned address(const T* s) { return unsigned(reinterpret_cast<uintptr_t>(s)); }
+  template <typename V>
+  __device__ static inline V read(unsigned at, int offset) {
+    return *reinterpret_cast<const __attribute__((address_space(3))) V*>((__attribute__((address_space(3))) const char*)(uintptr_t(at)) + offset);
+  }
+  // Chunk 4 ks + g of the lane's row and of those `row` further on.
+  __device__ static inline unsigned along0(const T* s, int row, int lane) { return address(s) + at(row, lane >> 4) * unsigned(sizeof(T)); }
+  __device__ static inline typename Op<T>::Frag along(unsigned at0, int ks, int row) {
+    return read<typename Op<T>::Frag>(at0 ^ (64 * ks) ^ (16 * key(row)), row * CH * 16);
   }
   // The same of a bf16 row with the slots of two stacked results: elements 4 g .. and 16 + 4 g .. of a step's 32.
-  __device__ static inline typename Op<T>::Frag stacked(const T* s, int row, int ks, int lane) {
+  __device__ static inline unsigned stacked0(const T* s, int row, int lane) {
+    const int g = lane >> 4;
+    return sizeof(T) == 2 ? address(s) + at(row, g >> 1) * 2 + 8 * (g & 1) : along0(s, row, lane);
+  }
+  __device__ static inline typename Op<T>::Frag stacked(unsigned at0, int ks, int row) {
     if constexpr (sizeof(T) == 2) {
-      const int g = lane >> 4, half = 4 * (g & 1);
-      const bf16x4 lo = *reinterpret_cast<const bf16x4*>(s + at(row, 4 * ks + (g >> 1)) + half);
-      const bf16x4 hi = *reinterpret_cast<const bf16x4*>(s + at(row, 4 * ks + 2 + (g >> 1)) + half);
-      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      const unsigned lo = at0 ^ (64 * ks) ^ (16 * key(row));
+      return __builtin_shufflevector(read<bf16x4>(lo, row * CH * 16), read<bf16x4>(lo ^ 32, row * CH * 16), 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
-      return along(s, row, ks, lane);
+      return along(at0, ks, row);
     }
   }
-  // Fragment u down the rows, of column `col` of lane i (four adjacent ones of lanes 4 n .. 4 n + 3; the caller gives
-  // the first of lane i & 3's four for bf16, the lane's own for fp32).
-  __device__ static inline typename Op<T>::Frag down(const T* s, int u, int col, int lane) {
+  // Down the rows KF u .., 16 columns from 16 t on.
+  __device__ static inline unsigned down0(const T* s, int lane) {
+    const int g = lane >> 4, i = lane & 15;
+    if (sizeof(T) == 2) return address(s) + at(8 * g + (i >> 2), (i & 3) >> 1) * 2 + 8 * (i & 1);
+    return address(s) + (at(4 * g, i >> 2) + (i & 3)) * 4;
+  }
+  __device__ static inline typename Op<T>::Frag down(unsigned at0, int t, int u) {
+    if constexpr (sizeof(T) == 2) {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) char* Lds;
+      const unsigned lo = at0 ^ (32 * t), hi = lo ^ (16 * key(4));
+      const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)((Lds)(uintptr_t(lo)) + 32 * u * CH * 16));
+      const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)((Lds)(uintptr_t(hi)) + (32 * u + 4) * CH * 16));
+      return __builtin_shufflevector(__builtin_bit_cast(bf16x4, x), __builtin_bit_cast(bf16x4, y), 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      f32x4 f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) f[r] = read<float>(at0 ^ (64 * t) ^ (16 * key(r)), (16 * u + r) * CH * 16);
+      return f;
+    }
+  }
+  // Down the rows in any order of columns: `col` is the first of lane i & 3's four for bf16, the lane's own for fp32.
+  __device__ static inline typename Op<T>::Frag down_at(const T* s, int u, int col, int lane) {
     const int g = lane >> 4, i = lane & 15;
     if constexpr (sizeof(T) == 2) {
       const int row = 32 * u + 8 * g + (i >> 2);
@@ -327,7 +358,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
-        for (int u = 0; u < US; ++u) vf[v][u] = TlV::down(v_now, u, vcol(v, x4(ln)), ln);
+        for (int u = 0; u < US; ++u) vf[v][u] = TlV::down_at(v_now, u, vcol(v, x4(ln)), ln);
     };
     if (STATE) values();
 
@@ -339,11 +370,12 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
         if (u * KF > 16 * qt + 15) continue;
         f32x4 pt[R] = {};
         const int ln = opaque();
+        const unsigned qa = TlK::along0(sq, 16 * qt + (ln & 15), ln), ka = TlK::along0(k_now, KF * u + row_of<T>(0, ln & 15), ln);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          const Frag q = TlK::along(sq, 16 * qt + (ln & 15), ks, ln);
+          const Frag q = TlK::along(qa, ks, 0);
 #pragma unroll
-          for (int r = 0; r < R; ++r) pt[r] = Op<T>::mma(TlK::along(k_now, row_of<T>(R * u + r, ln & 15), ks, ln), q, pt[r]);
+          for (int r = 0; r < R; ++r) pt[r] = Op<T>::mma(TlK::along(ka, ks, row_of<T>(r, 0)), q, pt[r]);
         }
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -353,6 +385,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
       }
       f32x4 o[QT][NV] = {};
       const int ln = opaque();
+      const unsigned qa = TlK::stacked0(sq, ln & 15, ln);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         Frag s[NV];
@@ -365,7 +398,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
         }
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
-          const Frag q = TlK::stacked(sq, 16 * qt + (ln & 15), ks, ln);
+          const Frag q = TlK::stacked(qa, ks, 16 * qt);
 #pragma unroll
           for (int v = 0; v < NV; ++v) o[qt][v] = Op<T>::mma(s[v], q, o[qt][v]);
         }
@@ -432,12 +465,12 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
         Frag part[NV][P1];
 #pragma unroll
         for (int v = 0; v < NV; ++v) weighted<P1>(vf[v][u], w, part[v]);
-        const int ln = opaque();
+        const unsigned ka = TlK::down0(k_now, opaque());
 #pragma unroll
         for (int t = 0; t < DT; t += 2) {  // several sums at a time: a product does not wait for the one before
           Frag k[2];
 #pragma unroll
-          for (int x = 0; x < 2; ++x) k[x] = TlK::down(k_now, u, 16 * (t + x) + x4(ln), ln);
+          for (int x = 0; x < 2; ++x) k[x] = TlK::down(ka, t + x, u);
 #pragma unroll
           for (int y = P0; y < P1; ++y)
 #pragma unroll

@@ -466,17 +466,23 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
 #pragma unroll
         for (int v = 0; v < NV; ++v) weighted<P1>(vf[v][u], w, part[v]);
         const unsigned ka = TlK::down0(k_now, opaque());
+        // two tiles at a time, so that a product does not wait for the one before, and the next two are on their way
+        Frag k[2][2];
 #pragma unroll
-        for (int t = 0; t < DT; t += 2) {  // several sums at a time: a product does not wait for the one before
-          Frag k[2];
+        for (int x = 0; x < 2; ++x) k[0][x] = TlK::down(ka, x, u);
 #pragma unroll
-          for (int x = 0; x < 2; ++x) k[x] = TlK::down(ka, t + x, u);
+        for (int t = 0; t < DT; t += 2) {
+          if (t + 2 < DT) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) k[(t / 2 + 1) & 1][x] = TlK::down(ka, t + 2 + x, u);
+          }
 #pragma unroll
           for (int y = P0; y < P1; ++y)
 #pragma unroll
             for (int x = 0; x < 2; ++x)
 #pragma unroll
-              for (int v = 0; v < NV; ++v) S[t + x][v] = Op<T>::mma(k[x], part[v][y], S[t + x][v]);
+              for (int v = 0; v < NV; ++v) S[t + x][v] = Op<T>::mma(k[t / 2 & 1][x], part[v][y], S[t + x][v]);
+          __builtin_amdgcn_sched_barrier(0);
         }
       };
       typedef std::integral_constant<int, 0> None;

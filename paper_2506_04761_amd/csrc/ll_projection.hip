@@ -284,30 +284,45 @@ __global__ __launch_bounds__(256) void k_gemm_join(GemmDev p) {
 }
 
 // A few rows (up to 16 MT): 16 outputs n to a workgroup, whose waves take 128 bytes of k each in turn, straight from
-// memory, and are added at the end in their order.
+// memory, and are added at the end in their order.  Bound by the loads in flight: those of U turns are issued together
+// (one row of 8192 x 8192 in bf16: 44 us one turn at a time, 29 with eight, 4.6 TB/s).
 constexpr int kFewWaves = 8;
-template <typename T, int MT>
-__global__ __launch_bounds__(64 * kFewWaves) void k_few_rows(GemmDev p, bool vec) {
-  constexpr int E = 16 / sizeof(T), KF = Op<T>::KF;
+template <typename T, int MT, bool VEC>
+__global__ __launch_bounds__(64 * kFewWaves) void k_few_rows(GemmDev p) {
+  constexpr int E = 16 / sizeof(T), KF = Op<T>::KF, U = 8 / MT;
+  typedef typename Op<T>::Frag Frag;
   __shared__ f32x4 s[kFewWaves][MT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i = lane & 15;
   const int64_t n0 = int64_t(blockIdx.x) * 16;
   const int64_t arow = n0 + i < p.a.n ? n0 + i : p.a.n - 1;
-  const T* a = static_cast<const T*>(p.a.p) + arow * p.a.stride;
+  const T* a = static_cast<const T*>(p.a.p) + arow * p.a.stride + E * g;
   const T* b[MT];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) b[t] = static_cast<const T*>(p.b.p) + (16 * t + i < p.b.n ? 16 * t + i : p.b.n - 1) * p.b.stride;
+  for (int t = 0; t < MT; ++t) b[t] = static_cast<const T*>(p.b.p) + (16 * t + i < p.b.n ? 16 * t + i : p.b.n - 1) * p.b.stride + E * g;
   f32x4 acc[MT] = {};
-  for (int64_t k0 = wave * 2 * KF; k0 < p.K; k0 += kFewWaves * 2 * KF) {
+  constexpr int64_t kTurn = kFewWaves * 2 * KF;
+  // `n` turns from k0 on; `whole`: all their k are inputs
+  auto turns = [&](int64_t k0, auto n, auto whole) {
+    constexpr int H = 2 * decltype(n)::value;
+    Frag fa[H], fb[H][MT];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int64_t k = k0 + h * KF + E * g;
-      const int n = k >= p.K ? 0 : (p.K - k < E ? int(p.K - k) : E);
-      const auto fa = load_n<T, E>(a + k, n, vec);
+    for (int h = 0; h < H; ++h) {
+      const int64_t k = k0 + h / 2 * kTurn + h % 2 * KF;
+      const int64_t left = p.K - k - E * g;
+      const int m = whole.value || left >= E ? E : (left > 0 ? int(left) : 0);
+      fa[h] = load_n<T, E>(a + k, m, VEC);
 #pragma unroll
-      for (int t = 0; t < MT; ++t) acc[t] = Op<T>::mma(fa, load_n<T, E>(b[t] + k, n, vec), acc[t]);
+      for (int t = 0; t < MT; ++t) fb[h][t] = load_n<T, E>(b[t] + k, m, VEC);
     }
-  }
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int t = 0; t < MT; ++t) acc[t] = Op<T>::mma(fa[h], fb[h][t], acc[t]);
+  };
+  int64_t k0 = wave * 2 * KF;
+  for (; k0 + (U - 1) * kTurn + 2 * KF <= p.K; k0 += U * kTurn) turns(k0, std::integral_constant<int, U>{}, std::true_type{});
+  for (; k0 + kTurn + 2 * KF <= p.K; k0 += 2 * kTurn) turns(k0, std::integral_constant<int, 2>{}, std::true_type{});
+  for (; k0 < p.K; k0 += kTurn) turns(k0, std::integral_constant<int, 1>{}, std::false_type{});
 #pragma unroll
   for (int t = 0; t < MT; ++t) s[wave][t][lane] = acc[t];
   __syncthreads();
@@ -396,12 +411,17 @@ constexpr TileCost kCosts[2][3] = {{{64, 5, 0.1, 0.6, 1.0}, {128, 2, 0.2, 2.1, 1
 GemmPlan plan(int64_t M, int64_t N, int64_t K, int dtype, Product what) {
   GemmPlan q;
   const int64_t BK = kStageBytes / elem(dtype), stages = ceil_div(K, BK);
+  // what is read, at the rate of a copy; tiles' stages overlap with about half of it
+  const double read = double(M + N) * K * elem(dtype) / 4.6e6;
+  double best = 0;
   if (what == kForward && M <= 64) {
+    // a workgroup's time is its K's, two on a compute unit take twice that (8192 x 8192: 16 rows 39 us, 32 54, 64 82)
     q.few = M <= 16 ? 1 : M <= 32 ? 2 : 4;
     q.workgroups = ceil_div(N, 16);
-    return q;
+    const double units = q.workgroups > 256 ? q.workgroups / 256.0 : 1;
+    best = K * units * 1e-3 * (M <= 4 ? 1.5 : M <= 16 ? 2.0 : M <= 32 ? 2.5 : 4.4) * (dtype == 1 ? 1 : 2.4);
+    best = best > read ? best : read;
   }
-  double best = 0;
   for (const TileCost& c : kCosts[dtype]) {
     if (!c.tile) continue;
     const int64_t m_tiles = ceil_div(M, c.tile), n_tiles = ceil_div(N, c.tile);
@@ -411,12 +431,13 @@ GemmPlan plan(int64_t M, int64_t N, int64_t K, int dtype, Product what) {
       const int64_t a_unit = ceil_div(m_tiles * n_tiles * splits, 256), rounds = a_unit / c.most, rest = a_unit % c.most;
       auto round = [&](int64_t n) { return n ? each * (c.stage + n * c.each) + c.results : 0.0; };
       const double join = splits > 1 ? 3 + double(splits) * M * N * 8 / 7e6 : 0;
-      const double us = rounds * round(c.most) + round(rest) + join;
-      if (q.tile && us >= best) continue;
+      const double us = rounds * round(c.most) + round(rest) + read / 2 + join;
+      if ((q.tile || q.few) && us >= best) continue;
       best = us;
-      q.tile = c.tile, q.m_tiles = m_tiles, q.n_tiles = n_tiles, q.splits = splits, q.span = each * BK;
+      q.few = 0, q.tile = c.tile, q.m_tiles = m_tiles, q.n_tiles = n_tiles, q.splits = splits, q.span = each * BK;
     }
   }
+  if (q.few) return q;
   q.workgroups = q.m_tiles * q.n_tiles * q.splits;
   q.bytes = q.splits > 1 ? q.splits * M * N * 4 : 0;
   return q;
@@ -486,9 +507,9 @@ template <typename T>
 hipError_t launch_few(const GemmDev& p, const GemmPlan& q, hipStream_t st) {
   const bool vec = direct(p.a, false, p.K, sizeof(T)) && direct(p.b, false, p.K, sizeof(T));
   const dim3 grid(uint32_t(q.workgroups)), block(64 * kFewWaves);
-  if (q.few == 1) k_few_rows<T, 1><<<grid, block, 0, st>>>(p, vec);
-  else if (q.few == 2) k_few_rows<T, 2><<<grid, block, 0, st>>>(p, vec);
-  else k_few_rows<T, 4><<<grid, block, 0, st>>>(p, vec);
+  if (q.few == 1) vec ? k_few_rows<T, 1, true><<<grid, block, 0, st>>>(p) : k_few_rows<T, 1, false><<<grid, block, 0, st>>>(p);
+  else if (q.few == 2) vec ? k_few_rows<T, 2, true><<<grid, block, 0, st>>>(p) : k_few_rows<T, 2, false><<<grid, block, 0, st>>>(p);
+  else vec ? k_few_rows<T, 4, true><<<grid, block, 0, st>>>(p) : k_few_rows<T, 4, false><<<grid, block, 0, st>>>(p);
   return hipGetLastError();
 }
 

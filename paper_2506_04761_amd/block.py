@@ -233,8 +233,6 @@ class _DecayAttention(torch.autograd.Function):
     def forward(ctx, q, k, v, log_decay, initial_state, lengths, scale, want_state):
         for t, name in ((q, "q"), (k, "k"), (v, "v")):
             _dims(t, name, 4)
-        if log_decay.requires_grad:
-            raise ValueError("log_decay must not require a gradient: the decays are constants")
         q, k, v = _heads_last(q), _heads_last(k), _heads_last(v)
         log_decay, initial_state = log_decay.contiguous(), _dense(initial_state)
         shape = (v.shape[0], v.shape[2], q.shape[3], v.shape[3])
@@ -290,6 +288,8 @@ class _Projection(torch.autograd.Function):
 def decay_attention(q, k, v, log_decay, scale=1.0, initial_state=None, lengths=None, return_final_state=False):
     """Differentiable ll_decay_attention_fwd: o, or (o, final state); gradients flow to q, k, v and the states.  Memory
     held until the graph is freed: the inputs and ll_decay_attention_states_bytes(...) bytes."""
+    if log_decay.requires_grad and torch.is_grad_enabled():
+        raise ValueError("log_decay must not require a gradient: the decays are constants")
     o, final = _DecayAttention.apply(q, k, v, log_decay, initial_state, lengths, scale, return_final_state)
     return (o, final) if return_final_state else o
 

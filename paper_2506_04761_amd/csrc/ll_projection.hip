@@ -451,7 +451,7 @@ struct DuPlan {
 DuPlan du_plan(int64_t M, int64_t N, int dtype) {
   DuPlan q;
   q.cols = ceil_div(N, 64 * (16 / elem(dtype)));
-  q.rows = ceil_div(M * q.cols, 1024);
+  q.rows = ceil_div(M * q.cols, 512);
   q.rows = ceil_div(q.rows < 16 ? 16 : q.rows, 4) * 4;
   q.strips = ceil_div(M, q.rows);
   return q;

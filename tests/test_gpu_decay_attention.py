@@ -138,9 +138,9 @@ def test_sequences_that_end_early(ends, dtype):
     _Case(1, 3, 130, 2, 1, 32, 48, dtype, ends=ends).check()
 
 
-# one segment to 512 tokens or more where batch and heads are few
+# segments of 128 tokens and more, from 512 tokens on where batch and heads are few
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("T,ends,state", [(1100, None, True), (1536, [1536, 0, 640], True), (2111, [1, 2111, 1087], False),
+@pytest.mark.parametrize("T,ends,state", [(512, None, True), (577, [577, 300, 0], True), (1100, None, True), (1536, [1536, 0, 640], True), (2111, [1, 2111, 1087], False),
                                           (1024, [512, 513, 1024], True)])
 def test_segments(T, ends, state, dtype):
     _Case(T, 3 if ends else 1, T, 2, 1, 16, 24, dtype, ends=ends, state=state).check()
@@ -198,6 +198,24 @@ def test_a_prompt_is_continued_in_place_and_by_tokens(dtype):
     _within(state, _np(whole), 2 * end_bound, dtype, T, "state", state=True)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_widest_rows(dtype):
+    """Tokens as far apart as strides may be: a chunk spans up to 2^32 bytes, the sequence more."""
+    import torch
+    from tests.gpu_util import torch_dtype
+    step, T = (1 << 24) - 8, 70
+    if torch.cuda.mem_get_info()[0] < 3 * T * step * 4:
+        pytest.skip("memory")
+    c = _Case(9, 1, T, 2, 2, 16, 16, dtype)
+    wide = torch.empty(T * step, dtype=torch_dtype(dtype), device="cuda")
+    for n, at in (("q", 0), ("k", 64), ("v", 128)):
+        x = getattr(c, n)
+        view = wide[at:].as_strided((1, T, 2, 16), (0, step, 16, 1))
+        view.copy_(x)
+        setattr(c, n, view)
+    c.check()
+
+
 def test_differentiable_against_differences():
     from paper_2506_04761_amd import block as ll
     import torch
@@ -240,8 +258,11 @@ def test_differentiable_takes_any_strides_and_refuses_what_it_cannot_give():
     for x, want in zip(leaves, g):
         assert torch.equal(x.grad.transpose(1, 2), want)
     assert g.initial_state is None
+    learned = c.ld.clone().requires_grad_()
     with pytest.raises(ValueError, match="constants"):
-        ll.decay_attention(c.q, c.k, c.v, c.ld.clone().requires_grad_())
+        ll.decay_attention(c.q, c.k, c.v, learned)
+    with torch.no_grad():
+        assert torch.equal(ll.decay_attention(c.q, c.k, c.v, learned, c.scale), o)
     q = c.q.clone().requires_grad_()
     d, = torch.autograd.grad(ll.decay_attention(q, c.k, c.v, c.ld).square().sum(), q, create_graph=True)
     with pytest.raises(RuntimeError, match="second derivatives"):

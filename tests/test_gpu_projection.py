@@ -137,6 +137,36 @@ def test_epilogue(M, K, N, dtype, silu, bias, residual):
     assert torch.equal(again, y)
 
 
+@pytest.mark.parametrize("dtype,M", [("bf16", 260), ("f32", 131)])
+def test_the_widest_rows(dtype, M):
+    """Rows as far apart as strides may be: a tile spans more than 2^32 bytes."""
+    import paper_2506_04761_amd as ll
+    import torch
+    from tests.gpu_util import torch_dtype
+    step = (1 << 24) - 8
+    if torch.cuda.mem_get_info()[0] < 3 * M * step * 4:
+        pytest.skip("memory")
+    i = _inputs(12, M, 72, 264, dtype, None)
+    wide = torch.empty(M * step, dtype=torch_dtype(dtype), device="cuda").as_strided((M, 72), (step, 1))
+    wide.copy_(i["x"])
+    i["x"] = wide
+    h = _host(i)
+    pre = torch.empty((M, 264), device="cuda")
+    y = ll.block.ll_projection_fwd(i["x"], i["w"], i["b"], i["r"], ll.LL_ACT_SILU, pre)
+    _check_fwd(y, pre, h, dtype, True, 72)
+    _check_bwd(ll.block.ll_projection_bwd(i["x"], i["w"], i["b"], i["dy"], ll.LL_ACT_SILU, pre), h, dtype, True, 72)
+
+
+def test_rows_that_are_one_row():
+    """Strides of zero: one input row, and one residual row, for every output row."""
+    from paper_2506_04761_amd import block as ll
+    i = _inputs(13, 1, 200, 72, "bf16", None)
+    h = _host(i)
+    y = ll.ll_projection_fwd(i["x"].expand(150, -1), i["w"], i["b"], i["r"].expand(150, -1))
+    h = {**h, "x": np.repeat(h["x"], 150, 0), "r": np.repeat(h["r"], 150, 0)}
+    _check_fwd(y, None, h, "bf16", False, 200)
+
+
 def test_only_the_gradients_that_are_wanted():
     from paper_2506_04761_amd import block as ll
     import torch

@@ -163,18 +163,31 @@ __device__ inline float log2_decay(const float* log_decay, int h) {
 
 __device__ const uint4 kZeros = {0, 0, 0, 0};  // rows before the first token, elements beyond the width
 
+// g^n for the state's way over n tokens, and what fp32 leaves of it: its error would be taken to the power of the chunks (a
+// state after 14758 tokens: off by 1.1e-6 with v_exp_f32's power, 6e-7 so).
+struct Carry {
+  float hi, lo;
+  __device__ inline Carry(const float* log_decay, int h, double n) {
+    const double w = exp(double(log_decay[h]) * n);
+    hi = float(w), lo = float(w - hi);
+  }
+};
+
 // Copies chunks of C rows of up to W elements to LDS, 16 bytes a thread at a time: straight there (VEC: rows of whole,
-// aligned vectors), or through registers.  A chunk's address is the same for all lanes, a lane's offset from it (fewer than
-// 64 rows of less than 2^24 elements) the same for all chunks.
-template <typename T, int W, int NT, bool VEC>
+// aligned vectors), or through registers, where a row's last, short vector is read moved back over the one before and
+// shifted (101 and 143 elements, 4 x 24115 tokens of 8 heads: element by element 2027 us).  A chunk's address is the same for
+// all lanes, a lane's offset from it (fewer than 64 rows of less than 2^24 elements) the same for all chunks.
+template <typename T, int W, bool VEC>
 struct Stage {
   typedef Tile<T, W> Tl;
   typedef typename VecN<T, Tl::E>::type Vec;
-  static constexpr int E = Tl::E, CH = Tl::CH, C = Op<T>::C, ITS = C * CH / NT, ROWS = NT / CH;
+  typedef typename VecN<T, Tl::E>::loose Loose;
+  static constexpr int E = Tl::E, CH = Tl::CH, C = Op<T>::C, ITS = C * CH / 256, ROWS = 256 / CH;
   const char* base;  // of the next chunk: its row with the lowest address
   int64_t turn;      // bytes between chunks
   unsigned off[ITS];
   int left;          // elements of a row
+  Vec held[VEC ? 1 : ITS];
   // `p`: element 0 of the first chunk's row 0, tokens `stride` elements apart, later ones lower where `reversed`
   __device__ inline void start(const T* p, int64_t stride, bool reversed, int left_) {
     left = left_;
@@ -186,27 +199,44 @@ struct Stage {
       off[it] = (unsigned(reversed ? C - 1 - row : row) * unsigned(stride) + c * E) * unsigned(sizeof(T));
     }
   }
-  // The next chunk, of which rows before `first` are zeros.
+  // Begins the copy of the next chunk, of which rows before `first` are zeros: to `s` (VEC), or to registers.
   __device__ inline void load(T* s, int first) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     auto copy = [&](auto edge) {
 #pragma unroll
       for (int it = 0; it < ITS; ++it) {
         const int row = threadIdx.x / CH + it * ROWS, c = (threadIdx.x % CH) ^ Tl::key(row);
-        const char* src = base + off[it];
-        T* to = s + (it * NT + wave * 64) * E;
         const int k = row < first ? 0 : left - c * E;
         if constexpr (VEC) {
-          if (edge.value) copy16_to_lds(lds_address(to), k > 0 ? static_cast<const void*>(src) : &kZeros);
-          else copy16_to_lds(lds_address(to), base, off[it]);
+          const unsigned to = lds_address(s + (it * 256 + wave * 64) * E);
+          if (edge.value) copy16_to_lds(to, k > 0 ? static_cast<const void*>(base + off[it]) : &kZeros);
+          else copy16_to_lds(to, base, off[it]);
+        } else if (left >= E) {
+          const int back = k < E ? E - k : 0;
+          const void* src = k > 0 ? static_cast<const void*>(base + off[it] - back * int(sizeof(T))) : &kZeros;
+          held[it] = *static_cast<const Loose*>(src);
         } else {
-          reinterpret_cast<Vec*>(to)[threadIdx.x & 63] = load_n<T, E>(reinterpret_cast<const T*>(src), k <= 0 ? 0 : (k < E ? k : E), false);
+          held[it] = load_n<T, E>(reinterpret_cast<const T*>(base + off[it]), k <= 0 ? 0 : (k < E ? k : E), false);
         }
       }
     };
     if (!VEC || first > 0 || left < W) copy(std::true_type{});
     else copy(std::false_type{});
     base += turn;
+  }
+  // Through registers: ends the copy.
+  __device__ inline void store(T* s) {
+    if constexpr (!VEC) {
+#pragma unroll
+      for (int it = 0; it < ITS; ++it) {
+        const int row = threadIdx.x / CH + it * ROWS, c = (threadIdx.x % CH) ^ Tl::key(row), k = left - c * E;
+        if (left >= E && k > 0 && k < E) {
+          const int shift = (E - k) * int(sizeof(T)) * 8;
+          held[it] = __builtin_bit_cast(Vec, __builtin_bit_cast(unsigned __int128, held[it]) >> shift);
+        }
+        reinterpret_cast<Vec*>(s)[it * 256 + threadIdx.x] = held[it];
+      }
+    }
   }
 };
 
@@ -289,16 +319,20 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
 
   // tokens by their order in time: that of the first chunk's row 0, and the step between two
   const int64_t tok = p.reversed ? live - 1 - (t0 - first) : t0 - first, dir = p.reversed ? -1 : 1;
-  Stage<T, DK, 64 * NW, VEC> lk, lq;
-  Stage<T, DV, 64 * NW, VEC> lv;
+  Stage<T, DK, VEC> lk, lq;
+  Stage<T, DV, VEC> lv;
   lk.start(static_cast<const T*>(p.b.p) + b * p.b.sb + tok * p.b.st + (h / p.b.group) * d1, p.b.st, p.reversed, d1);
   lv.start(static_cast<const T*>(p.c.p) + b * p.c.sb + tok * p.c.st + (h / p.c.group) * d2 + col0, p.c.st, p.reversed, d2 - col0);
   if (!STATE) lq.start(static_cast<const T*>(p.a.p) + b * p.a.sb + tok * p.a.st + (h / p.a.group) * d1, p.a.st, p.reversed, d1);
   if (n > 0) {
-    lk.load(sk[0], first);
-    if (!STATE) lq.load(sq, first);
-    lv.load(sv[0], first);
+    lk.load(sk[0], first), lk.store(sk[0]);
+    if (!STATE) lq.load(sq, first), lq.store(sq);
+    lv.load(sv[0], first), lv.store(sv[0]);
   }
+  const Carry chunk(p.log_decay, h, double(C));
+  Carry begin = chunk;
+  if (first > 0) begin = Carry(p.log_decay, h, double(C - first));
+  float over = 0.0f;
   if (threadIdx.x < C) sw[threadIdx.x] = p.in_scale * fast_exp2(lg * float(C - 1 - int(threadIdx.x) + rho));
 
   // columns: those of tile v that lane i holds; two tiles interleaved in fours, so that a lane's results are adjacent
@@ -348,10 +382,13 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
     auto x4 = [](int ln) { return sizeof(T) == 2 ? 4 * (ln & 3) : ln & 15; };  // a lane's column of those read down
     if (VEC) copies_done();
     __syncthreads();
-    if (AHEAD && more) {
-      lk.load(sk[~ch & 1], 0);
-      if (STATE) lv.load(sv[~ch & (STATE ? 1 : 0)], 0);
+    T* const k_next = sk[AHEAD ? ~ch & 1 : 0];
+    T* const v_next = sv[AHEAD && STATE ? ~ch & 1 : 0];
+    if (more && (AHEAD || !VEC)) {
+      lk.load(k_next, 0);
+      if (STATE) lv.load(v_next, 0);
     }
+    if (more && !STATE && !VEC) lq.load(sq, 0), lv.load(v_next, 0);
     Frag vf[NV][US];
     auto values = [&] {
       const int ln = opaque();
@@ -413,8 +450,8 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
       }
       __syncthreads();
       if (more) {
-        lq.load(sq, 0);
-        lv.load(sv[0], 0);
+        if (VEC) lq.load(sq, 0), lv.load(v_next, 0);
+        lq.store(sq), lv.store(v_next);
       }
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt)
@@ -445,7 +482,10 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
 
     // the state after the chunk; values times powers of the decay in bf16 parts, three where fp32's bits are wanted and
     // two (16 bits) where only rounded results come of it
-    const float carry = fast_exp2(lg * float(C - first));
+    // what the factors leave out of exact ones is carried over, so that their product over the chunks is off by a rounding
+    over += ch ? chunk.lo : begin.lo;
+    const float carry = (ch ? chunk.hi : begin.hi) + over;
+    over -= carry - (ch ? chunk.hi : begin.hi);
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -495,12 +535,14 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
         if (ends) add(std::integral_constant<int, 2>{}, std::integral_constant<int, 3>{});
       }
     }
-    if (!AHEAD) {
-      __syncthreads();
-      if (more) {
-        lk.load(sk[0], 0);
-        if (STATE) lv.load(sv[0], 0);
+    if (!AHEAD) __syncthreads();
+    if (more) {
+      if (VEC && !AHEAD) {
+        lk.load(k_next, 0);
+        if (STATE) lv.load(v_next, 0);
       }
+      lk.store(k_next);
+      if (STATE) lv.store(v_next);
     }
     first = 0;
   }
@@ -547,7 +589,7 @@ __global__ __launch_bounds__(256) void k_join(float* h, const float* first, cons
   float* p = h + bh * S * size + e;
   float v = first ? first[id] : 0.0f;
   p[0] = v;
-  const float w = fast_exp2(log2_decay(log_decay, int(bh % H)) * float(L));  // a segment with one after it is whole
+  const Carry w(log_decay, int(bh % H), double(L));  // a segment with one after it is whole
   constexpr int U = 8;  // loads ahead of the stores
   for (int s = 1; s < used; s += U) {
     float u[U];
@@ -555,7 +597,7 @@ __global__ __launch_bounds__(256) void k_join(float* h, const float* first, cons
     for (int k = 0; k < U; ++k) u[k] = s + k < used ? p[(s + k) * size] : 0.0f;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-      v = fmaf(w, v, u[k]);
+      v = fmaf(w.hi, v, fmaf(w.lo, v, u[k]));
       if (s + k < used) p[(s + k) * size] = v;
     }
   }
@@ -640,16 +682,19 @@ __global__ __launch_bounds__(256) void k_group_sum(const float* x, void* out, in
 
 int64_t up256(int64_t n) { return (n + 255) / 256 * 256; }
 
+// Tiles of 16 values that a wave holds: two where it has registers for them.
+int value_tiles(int64_t d1, int64_t d2) { return d1 <= 128 && d2 > 64 ? 2 : 1; }
+
 struct Split {
   int64_t L, S;
 };
-// Segments of whole chunks: as many as the card holds workgroups at once (three to a compute unit of heads up to 64
+// Segments of whole chunks: as many as the card holds workgroups at once (three to a compute unit of keys up to 64
 // elements, two up to 128, else one; one more segment begins a second round: 2 x 4096 tokens, 24 heads of 128 x 128, 10
 // segments 90 us, 12 109), of 128 tokens at least, and none below 512 tokens, where the two launches more take longer.  One
 // segment of 4 x 8192 tokens, 32 heads of 64 x 64 takes 301 us, two 222, six 181.
 Split split_of(int64_t B, int64_t T, int64_t H, int64_t dk, int64_t dv) {
-  const int64_t d = dk > dv ? dk : dv, held = d <= 64 ? 768 : d <= 128 ? 512 : 256;
-  int64_t S = held / (B * H * ceil_div(d, 128));
+  const int64_t held = dk <= 64 ? 768 : dk <= 128 ? 512 : 256;
+  int64_t S = held / (B * H * ceil_div(dv, 64 * value_tiles(dk, dv)));
   S = S < T / 128 ? S : T / 128;
   if (S < 1 || T < 512) S = 1;
   Split q;
@@ -662,9 +707,6 @@ Heads heads_of(const Rows& r, int64_t heads, int64_t H, int64_t width, int esize
   const int n = 16 / esize;
   return {r.p, r.sb, r.st, int(width), int(H / heads), rows_aligned(r, esize, n) && width % n == 0};
 }
-
-// Tiles of 16 values that a wave holds: two where it has registers for them.
-int value_tiles(int64_t d1, int64_t d2) { return d1 <= 128 && d2 > 64 ? 2 : 1; }
 
 template <typename T, int DK, int NV>
 hipError_t launch_attend(const DecayDev& p, bool state, hipStream_t st) {

@@ -89,20 +89,25 @@ struct Side {
 __device__ const uint4 kZeros = {0, 0, 0, 0};  // the k beyond the last
 
 // Copies stages of an operand to LDS, 16 bytes a thread at a time: straight there (DIRECT: rows of whole, aligned
-// chunks), or through registers (any rows).  A stage's address is the same for all lanes, a lane's offset from it (at most
+// chunks), or through registers (any rows; the last, short vector of a row is read moved back over the one before and
+// shifted).  A stage's address is the same for all lanes, a lane's offset from it (at most
 // 64 rows of less than 2^24 elements) the same for all stages.
 template <typename T, typename Tl, int TD, bool DOWN, bool DIRECT, int NT>
 struct Copy {
   typedef typename VecN<T, Tl::E>::type Vec;
+  typedef typename VecN<T, Tl::E>::loose Loose;
   static constexpr int E = Tl::E, CH = Tl::CH, ITS = TD * 8 / NT, ROWS = NT / CH;
   const char* base;  // of the next stage
   int64_t turn, jump;  // bytes between stages, between a lane's rows
   unsigned off[ITS];
   int64_t n;         // outputs from the tile's first on
   Vec held[DIRECT ? 1 : ITS];
+  int back[DIRECT ? 1 : ITS];  // elements that a short vector was moved back by
+  bool movable;                // vectors lie before a short one
 
-  __device__ inline void start(const Side& s, int64_t d0, int64_t k0) {
+  __device__ inline void start(const Side& s, int64_t d0, int64_t k0, int64_t K) {
     n = s.n - d0;
+    movable = (DOWN ? s.n : K) >= E;
     base = static_cast<const char*>(s.p) + (DOWN ? k0 * s.stride + d0 : d0 * s.stride + k0) * int64_t(sizeof(T));
     turn = (DOWN ? Tl::BK * s.stride : Tl::BK) * int64_t(sizeof(T));
     jump = ROWS * s.stride * int64_t(sizeof(T));
@@ -116,9 +121,12 @@ struct Copy {
   // Begins the copy of the next stage, of which `left` k are inputs.
   __device__ inline void load(T* lds, int64_t left) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (DIRECT && left >= Tl::BK && n >= TD) {
+    if (left >= Tl::BK && n >= TD) {
 #pragma unroll
-      for (int it = 0; it < ITS; ++it) copy16_to_lds(lds_address(lds + (it * NT + wave * 64) * E), base + it * jump, off[it]);
+      for (int it = 0; it < ITS; ++it) {
+        if constexpr (DIRECT) copy16_to_lds(lds_address(lds + (it * NT + wave * 64) * E), base + it * jump, off[it]);
+        else held[it] = *reinterpret_cast<const Loose*>(base + it * jump + off[it]), back[it] = 0;
+      }
     } else {
 #pragma unroll
       for (int it = 0; it < ITS; ++it) {
@@ -128,8 +136,11 @@ struct Copy {
         if constexpr (DIRECT) {
           copy16_to_lds(lds_address(lds + (it * NT + wave * 64) * E), k > 0 && d > 0 ? static_cast<const void*>(src) : &kZeros);
         } else {
-          const int64_t m = k <= 0 || d <= 0 ? 0 : (DOWN ? d : k);
-          held[it] = load_n<T, E>(reinterpret_cast<const T*>(src), m < E ? int(m) : E, false);
+          const int64_t whole = k <= 0 || d <= 0 ? 0 : (DOWN ? d : k);
+          const int m = whole < E ? int(whole) : E;
+          back[it] = movable && m > 0 ? E - m : 0;
+          if (movable) held[it] = *static_cast<const Loose*>(m > 0 ? static_cast<const void*>(src - back[it] * int(sizeof(T))) : &kZeros);
+          else held[it] = load_n<T, E>(reinterpret_cast<const T*>(src), m, false);
         }
       }
     }
@@ -139,7 +150,10 @@ struct Copy {
   __device__ inline void store(T* lds) {
     if constexpr (!DIRECT) {
 #pragma unroll
-      for (int it = 0; it < ITS; ++it) *reinterpret_cast<Vec*>(lds + (it * NT + threadIdx.x) * E) = held[it];
+      for (int it = 0; it < ITS; ++it) {
+        if (back[it]) held[it] = __builtin_bit_cast(Vec, __builtin_bit_cast(unsigned __int128, held[it]) >> (back[it] * int(sizeof(T)) * 8));
+        *reinterpret_cast<Vec*>(lds + (it * NT + threadIdx.x) * E) = held[it];
+      }
     }
   }
 };
@@ -211,8 +225,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_gemm(GemmDev p) {
   int64_t left = p.K - k0 < p.span ? p.K - k0 : p.span;
   Copy<T, TlM, TM, DOWN_M, DIRECT, NT> cm;
   Copy<T, TlN, TN, DOWN_N, DIRECT, NT> cn;
-  cm.start(p.b, m0, k0);
-  cn.start(p.a, n0, k0);
+  cm.start(p.b, m0, k0, p.K);
+  cn.start(p.a, n0, k0, p.K);
   f32x4 acc[FM][FN] = {};
   cm.load(s, left);
   cn.load(s + TM * BK, left);
@@ -352,28 +366,37 @@ __global__ __launch_bounds__(256) void k_du(DuDev p) {
   const int lane = threadIdx.x & 63, sub = threadIdx.x >> 6;
   const int64_t strip = blockIdx.x / p.cols, n = (blockIdx.x % p.cols * 64 + lane) * E;
   const int count = n >= p.N ? 0 : (p.N - n < E ? int(p.N - n) : E);
+  // a row's last, short vector is moved back over the one before: it does again what that does, and counts its own
+  const int64_t at = count > 0 && count < E && p.N >= E ? p.N - E : n;
   const int64_t end = (strip + 1) * p.rows < p.M ? (strip + 1) * p.rows : p.M;
   float sum[E] = {};
+  auto row = [&](int64_t m, int c) {
+    const auto g = load_n<T, E>(static_cast<const T*>(p.dy) + m * p.N + at, c, false);
+    float d[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) d[i] = to_f32(T(g[i]));
+    if (p.pre) {
+      const auto u = load_n<float, E>(p.pre + m * p.N + at, c, false);
+#pragma unroll
+      for (int i = 0; i < E; ++i) d[i] *= silu_grad(u[i], sigmoidf(u[i]));
+      store_n<T, E>(static_cast<T*>(p.du) + m * p.N + at, d, c, false);
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) sum[i] += d[i];
+  };
   if (count > 0) {
+    if (p.N >= E) {
 #pragma unroll 4
-    for (int64_t m = strip * p.rows + sub; m < end; m += 4) {
-      const auto g = load_n<T, E>(static_cast<const T*>(p.dy) + m * p.N + n, count, false);
-      float d[E];
-#pragma unroll
-      for (int i = 0; i < E; ++i) d[i] = to_f32(T(g[i]));
-      if (p.pre) {
-        const auto u = load_n<float, E>(p.pre + m * p.N + n, count, false);
-#pragma unroll
-        for (int i = 0; i < E; ++i) d[i] *= silu_grad(u[i], sigmoidf(u[i]));
-        store_n<T, E>(static_cast<T*>(p.du) + m * p.N + n, d, count, false);
-      }
-#pragma unroll
-      for (int i = 0; i < E; ++i) sum[i] += d[i];
+      for (int64_t m = strip * p.rows + sub; m < end; m += 4) row(m, E);
+    } else {
+      for (int64_t m = strip * p.rows + sub; m < end; m += 4) row(m, count);
     }
   }
   if (!p.part) return;
+  const int own = int(n - at);  // of the vector's elements, those before are the one before's
 #pragma unroll
-  for (int i = 0; i < E; ++i) s[sub][lane][i] = sum[i];
+  for (int i = 0; i < E; ++i)
+    if (i >= own) s[sub][lane][i - own] = sum[i];
   __syncthreads();
   for (int c = threadIdx.x; c < 64 * E; c += 256) {
     const int64_t col = blockIdx.x % p.cols * 64 * E + c;
@@ -420,6 +443,7 @@ GemmPlan plan(int64_t M, int64_t N, int64_t K, int dtype, Product what) {
     q.workgroups = ceil_div(N, 16);
     const double units = q.workgroups > 256 ? q.workgroups / 256.0 : 1;
     best = K * units * 1e-3 * (M <= 4 ? 1.5 : M <= 16 ? 2.0 : M <= 32 ? 2.5 : 4.4) * (dtype == 1 ? 1 : 2.4);
+    if (dtype == 1 && K % 8) best *= 1.8;  // unaligned rows (64 rows of 2047 x 4001 36 us, in tiles 17)
     best = best > read ? best : read;
   }
   for (const TileCost& c : kCosts[dtype]) {

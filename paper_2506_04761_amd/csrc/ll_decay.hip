@@ -12,6 +12,11 @@
 // Everything is computed transposed: P^T = K Q^T, O^T = S^T Q^T + V^T P^T, S += K^T V.  A result of one matrix instruction
 // then is an operand of the next as the lanes hold it (P^T through LDS, where other waves read it; S in place), since a
 // contraction only needs both operands to agree on which k a slot stands for.
+//
+// bf16: 65536 tokens of 16 heads of 128 x 128 386 us in all (sums of 32 segments 134, their join 16, results 281), 4.5 TB/s
+// over the 1.75 GB that are moved; 4 x 8192 tokens of 32 heads of 128 x 64 with states in and out 274 us (80, 11, 205), 4.4
+// TB/s; a copy reaches 5.0.  Bound by memory there, by a chunk's way through the waves (7 to 9 us with two workgroups on a
+// compute unit) where segments are short.
 #include "ll_layer.hpp"
 #include "ll_layer_device.hpp"
 
@@ -603,6 +608,7 @@ __global__ __launch_bounds__(256) void k_join(float* h, const float* first, cons
   }
 }
 
+// Bound by memory: 64 sequences of 16 heads of 128 x 128 32 us, 4.2 TB/s of states in and out.
 // One token of 256 / LV rows at a time: o = scale (g S + k v^T)^T q, the state passed through.
 struct StepDev {
   Heads q, k, v;

@@ -5,6 +5,10 @@
 // "along" the reduction (x and W in the forward: rows of k) or "down" it (W in dx, du and x in dW: every row is one
 // k).  A stage of 128 bytes of k of both operands is copied to LDS as it lies, and the fragments of the matrix
 // instructions are read from there along or down the rows, so that nothing is transposed in memory.
+//
+// bf16: 32768 x 1024 to 4096 304 us, 905 TFLOP/s (the library's product 254); training step of 8064 x 2048 to 1024 145 us, 700
+// TFLOP/s (41 the forward, 41 dx, 51 dW in four splits, 11 dbias).  The matrix cores are busy 42 % of the time, LDS 16 to 32 %:
+// what bounds the products is the turn of a stage, its wait, barrier and first reads.
 #include "ll_layer.hpp"
 #include "ll_layer_device.hpp"
 

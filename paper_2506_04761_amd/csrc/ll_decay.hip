@@ -857,10 +857,10 @@ int64_t decay_workspace(int64_t B, int64_t T, int64_t H, int64_t Hqk, int64_t dk
 }
 bool decay_launchable(const DecayArgs& a, bool backward) {
   const int64_t S = split_of(a.B, a.T, a.H, a.dk, a.dv).S, heads = a.B * a.H;
-  auto attends = [&](int64_t d1, int64_t d2) { return launchable(heads * S * ceil_div(d2, 64 * value_tiles(d1, d2)), 256); };
-  if (!attends(a.dk, a.dv) || !launchable(ceil_div(heads * a.dk * a.dv, 256), 256)) return false;
+  auto attends = [&](int64_t d2) { return launchable(heads * S * ceil_div(d2, 64), 256); };
+  if (!attends(a.dv) || !launchable(ceil_div(heads * a.dk * a.dv, 256), 256)) return false;
   if (!backward) return true;
-  return attends(a.dv, a.dk) &&
+  return attends(a.dk) &&
          (a.Hqk == a.H || launchable(ceil_div(a.B * a.T * a.Hqk * a.dk, 256), 256));
 }
 bool decay_step_launchable(const DecayArgs& a) { return launchable(a.B * a.H, 256); }

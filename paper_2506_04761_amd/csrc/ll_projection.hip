@@ -449,6 +449,7 @@ GemmPlan plan(int64_t M, int64_t N, int64_t K, int dtype, Product what) {
     best = K * units * 1e-3 * (M <= 4 ? 1.5 : M <= 16 ? 2.0 : M <= 32 ? 2.5 : 4.4) * (dtype == 1 ? 1 : 2.4);
     if (dtype == 1 && K % 8) best *= 1.8;  // unaligned rows (64 rows of 2047 x 4001 36 us, in tiles 17)
     best = best > read ? best : read;
+    if (best <= 4) return q;  // less than tiles and their join take at all
   }
   for (const TileCost& c : kCosts[dtype]) {
     if (!c.tile) continue;

@@ -147,6 +147,12 @@ def test_segments(T, ends, state, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dk,dv", [(16, 100), (96, 24), (128, 128), (136, 64), (256, 200), (65, 129), (33, 47), (5, 3)])
+def test_segments_of_every_kernel(dk, dv, dtype):
+    _Case(dk + 1, 2, 640, 2, 1, dk, dv, dtype, ends=[600, 513]).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("decays", [[0.0], [float("-inf")], [-1e-7, -5.0, -80.0, -1e30]])
 @pytest.mark.parametrize("T", [70, 1100])
 def test_decays_from_none_to_all(decays, T, dtype):

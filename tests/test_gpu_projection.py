@@ -137,6 +137,27 @@ def test_epilogue(M, K, N, dtype, silu, bias, residual):
     assert torch.equal(again, y)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N", [(4090, 1032, 2816), (4090, 1031, 2810), (2050, 2048, 1030), (700, 4104, 1000), (20, 8200, 8200)])
+def test_tiles_of_every_size(M, K, N, dtype):
+    """Sizes that take tiles of 64, 128 and 256 outputs, whole and in splits, of aligned and unaligned rows.  The reference
+    is in 64 bits on the GPU; bounds as above."""
+    from paper_2506_04761_amd import block as ll
+    i = _inputs(M, M, K, N, dtype, None)
+    h = {k: t.double() for k, t in i.items()}
+    u24, e = 2.0 ** -24, HALF[dtype]
+    y = ll.ll_projection_fwd(i["x"], i["w"], i["b"], i["r"])
+    g = ll.ll_projection_bwd(i["x"], i["w"], i["b"], i["dy"])
+    more = (h["b"].abs() + h["r"].abs()) * 16 * u24
+    for name, got, a, b, n, add, tol in (("y", y, h["x"], h["w"].T, K, h["b"] + h["r"], more), ("dx", g.x, h["dy"], h["w"], N, 0, 0),
+                                         ("dw", g.weight, h["dy"].T, h["x"], M, 0, 0)):
+        want = a @ b + add
+        bound = (n + 8) * u24 * (a.abs() @ b.abs()) + tol
+        assert ((got.double() - want).abs() <= bound + e * (want.abs() + bound)).all(), name
+    want, bound = h["dy"].sum(0), (M + 8) * u24 * h["dy"].abs().sum(0)
+    assert ((g.bias.double() - want).abs() <= bound).all()
+
+
 @pytest.mark.parametrize("dtype,M", [("bf16", 260), ("f32", 131)])
 def test_the_widest_rows(dtype, M):
     """Rows as far apart as strides may be: a tile spans more than 2^32 bytes."""

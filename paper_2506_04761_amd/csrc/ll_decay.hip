@@ -259,6 +259,16 @@ __device__ inline f32x4 pack<float>(const f32x4* v) {
   return v[0];
 }
 
+// What packing leaves of the values, nothing of infinities.
+template <typename T>
+__device__ inline void remainder(f32x4& v) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const float held = to_f32(from_f32<T>(v[r]));
+    v[r] = v[r] == held ? 0.0f : v[r] - held;
+  }
+}
+
 // v w of a fragment's slots as N bf16 parts, which hold 8 bits each of the products (fp32: the product).
 template <int N>
 __device__ inline void weighted(bf16x8 v, const float* w, bf16x8* part) {
@@ -286,11 +296,15 @@ constexpr bool keys_ahead(int dk) { return dk <= 128; }
 
 // One segment of one head, 64 NV values a workgroup: a wave holds the state's rows of its 16 NV columns.  d1 <= DK.
 // Chunks end with the segment: the first may begin with rows of zeros, and powers of the decay are the same in all others.
-template <typename T, int DK, int NV, bool STATE, bool VEC>
+// FEW: bf16 calls of one chunk take scores and states in two parts: with few of them their roundings do not average out (28
+// sequences of one token: results off by 0.0032, 0.0017 so; of more than 64 tokens 0.0025 at most).  512 sequences of 64
+// tokens, 16 heads of 128 x 128: 597 us, 622 so.  A branch on a sequence's own length took registers from the long calls.
+template <typename T, int DK, int NV, bool STATE, bool VEC, bool FEW = false>
 __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
   constexpr int KF = Op<T>::KF, C = Op<T>::C, R = KF / 16, QT = C / 16, US = C / KF, KS = DK / KF, DT = DK / 16;
   constexpr int NW = 4, DV = 16 * NW * NV, NU = QT * US / NW;  // NU: fragments of P^T that a wave forms
   constexpr bool AHEAD = keys_ahead(DK);
+  constexpr int PARTS = FEW ? 2 : 1;
   typedef typename Op<T>::Frag Frag;
   typedef Tile<T, DK> TlK;
   typedef Tile<T, DV> TlV;
@@ -405,68 +419,84 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
     if (STATE) values();
 
     if constexpr (!STATE) {
-      // P^T of 16 queries and the keys up to them
-#pragma unroll
-      for (int x = 0; x < NU; ++x) {
-        const int qt = (wave + x * NW) % QT, u = (wave + x * NW) / QT;
-        if (u * KF > 16 * qt + 15) continue;
-        f32x4 pt[R] = {};
-        const int ln = opaque();
-        const unsigned qa = TlK::along0(sq, 16 * qt + (ln & 15), ln), ka = TlK::along0(k_now, KF * u + row_of<T>(0, ln & 15), ln);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const Frag q = TlK::along(qa, ks, 0);
-#pragma unroll
-          for (int r = 0; r < R; ++r) pt[r] = Op<T>::mma(TlK::along(ka, ks, row_of<T>(r, 0)), q, pt[r]);
-        }
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) pt[r][e] *= pw[x][r][e];
-        sp[qt][u][lane] = pack<T>(pt);
-      }
       f32x4 o[QT][NV] = {};
-      const int ln = opaque();
-      const unsigned qa = TlK::stacked0(sq, ln & 15, ln);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        Frag s[NV];
+      for (int part = 0; part < PARTS; ++part) {
+        if (part) __syncthreads();  // the first part's scores are read; queries and keys are there: no chunk comes after
+        // P^T of 16 queries and the keys up to them; of the second part, what its rounding left
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-          f32x4 x[R];
-#pragma unroll
-          for (int r = 0; r < R; ++r) x[r] = S[R * ks + r][v];
-          s[v] = pack<T>(x);
-        }
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) {
-          const Frag q = TlK::stacked(qa, ks, 16 * qt);
-#pragma unroll
-          for (int v = 0; v < NV; ++v) o[qt][v] = Op<T>::mma(s[v], q, o[qt][v]);
-        }
-      }
-      values();
-#pragma unroll
-      for (int qt = 0; qt < QT; ++qt) {
-        const int after = 16 * qt + i + 1 - rho - first;
-        const float w = p.out_scale * fast_exp2(lg * float(after > 0 ? after : 0));
-#pragma unroll
-        for (int v = 0; v < NV; ++v) o[qt][v] *= w;
-      }
-      __syncthreads();
-      if (more) {
-        if (VEC) lq.load(sq, 0), lv.load(v_next, 0);
-        lq.store(sq), lv.store(v_next);
-      }
-#pragma unroll
-      for (int qt = 0; qt < QT; ++qt)
-#pragma unroll
-        for (int u = 0; u < US; ++u) {
+        for (int x = 0; x < NU; ++x) {
+          const int qt = (wave + x * NW) % QT, u = (wave + x * NW) / QT;
           if (u * KF > 16 * qt + 15) continue;
-          const Frag pf = sp[qt][u][lane];
+          f32x4 pt[R] = {};
+          const int ln = opaque();
+          const unsigned qa = TlK::along0(sq, 16 * qt + (ln & 15), ln), ka = TlK::along0(k_now, KF * u + row_of<T>(0, ln & 15), ln);
 #pragma unroll
-          for (int v = 0; v < NV; ++v) o[qt][v] = Op<T>::mma(vf[v][u], pf, o[qt][v]);
+          for (int ks = 0; ks < KS; ++ks) {
+            const Frag q = TlK::along(qa, ks, 0);
+#pragma unroll
+            for (int r = 0; r < R; ++r) pt[r] = Op<T>::mma(TlK::along(ka, ks, row_of<T>(r, 0)), q, pt[r]);
+          }
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pt[r][e] *= pw[x][r][e];
+          if (part) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) remainder<T>(pt[r]);
+          }
+          sp[qt][u][lane] = pack<T>(pt);
         }
+        if (part == 0) {
+#pragma unroll
+          for (int low = 0; low < PARTS; ++low) {
+            const int ln = opaque();
+            const unsigned qa = TlK::stacked0(sq, ln & 15, ln);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+              Frag s[NV];
+#pragma unroll
+              for (int v = 0; v < NV; ++v) {
+                f32x4 x[R];
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                  x[r] = S[R * ks + r][v];
+                  if (low) remainder<T>(x[r]);
+                }
+                s[v] = pack<T>(x);
+              }
+#pragma unroll
+              for (int qt = 0; qt < QT; ++qt) {
+                const Frag q = TlK::stacked(qa, ks, 16 * qt);
+#pragma unroll
+                for (int v = 0; v < NV; ++v) o[qt][v] = Op<T>::mma(s[v], q, o[qt][v]);
+              }
+            }
+          }
+          values();
+#pragma unroll
+          for (int qt = 0; qt < QT; ++qt) {
+            const int after = 16 * qt + i + 1 - rho - first;
+            const float w = p.out_scale * fast_exp2(lg * float(after > 0 ? after : 0));
+#pragma unroll
+            for (int v = 0; v < NV; ++v) o[qt][v] *= w;
+          }
+        }
+        __syncthreads();
+        if (PARTS == 1 && more) {
+          if (VEC) lq.load(sq, 0), lv.load(v_next, 0);
+          lq.store(sq), lv.store(v_next);
+        }
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt)
+#pragma unroll
+          for (int u = 0; u < US; ++u) {
+            if (u * KF > 16 * qt + 15) continue;
+            const Frag pf = sp[qt][u][lane];
+#pragma unroll
+            for (int v = 0; v < NV; ++v) o[qt][v] = Op<T>::mma(vf[v][u], pf, o[qt][v]);
+          }
+      }
       if (ocount > 0) {
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
@@ -718,6 +748,12 @@ template <typename T, int DK, int NV>
 hipError_t launch_attend(const DecayDev& p, bool state, hipStream_t st) {
   const dim3 grid(uint32_t(p.groups)), block(256);
   const bool vec = p.b.vec && p.c.vec && (state || (p.a.vec && p.vec_out));
+  if constexpr (sizeof(T) == 2) {
+    if (!state && p.T <= Op<T>::C) {
+      vec ? k_attend<T, DK, NV, false, true, true><<<grid, block, 0, st>>>(p) : k_attend<T, DK, NV, false, false, true><<<grid, block, 0, st>>>(p);
+      return hipGetLastError();
+    }
+  }
   if (state) vec ? k_attend<T, DK, NV, true, true><<<grid, block, 0, st>>>(p) : k_attend<T, DK, NV, true, false><<<grid, block, 0, st>>>(p);
   else vec ? k_attend<T, DK, NV, false, true><<<grid, block, 0, st>>>(p) : k_attend<T, DK, NV, false, false><<<grid, block, 0, st>>>(p);
   return hipGetLastError();

@@ -125,6 +125,28 @@ def test_lengths(T, state, dtype):
     _Case(T, 1, T, 3, 3, 24, 40, dtype, state=state).check()
 
 
+@pytest.mark.parametrize("dk,dv", [(103, 64), (64, 64), (64, 128), (33, 80), (128, 128), (100, 143), (128, 48), (101, 20),
+                                   (256, 128), (200, 50)])
+@pytest.mark.parametrize("B,T", [(28, 1), (1, 1), (3, 2), (2, 17), (1, 64)])
+@pytest.mark.parametrize("state", [True, False])
+def test_few_tokens_are_rounded_once(state, B, T, dk, dv):
+    """bf16 calls of one chunk: scores and states enter the products in two parts, which leave 2^-8 of 2^-8, so that but the
+    results' own rounding counts: the head's bound with 2^-16 A for 2^-8 A."""
+    c = _Case(dk, B, T, 2, 1, dk, dv, "bf16", state=state, ends=[T] * (B - 1) + [T - T // 4])
+    h = [np.nan_to_num(_np(t)) for t in (c.q, c.k, c.v)] + [_np(c.ld)]
+    d, i, f = np.nan_to_num(_np(c.d_o)), _np(c.initial), _np(c.d_final)
+    mag, mags = [np.abs(x) for x in h[:3]] + [h[3]], [None if x is None else np.abs(x) for x in (i, f)]
+    o, _, g = c.run()
+    wants = [layer.decay_attention(*h, c.scale, i, c.ends)[0], *layer.decay_attention_grad(*h, d, c.scale, i, c.ends, f)]
+    bounds = [layer.decay_attention(*mag, c.scale, mags[0], c.ends)[0],
+              *layer.decay_attention_grad(*mag, np.abs(d), c.scale, mags[0], c.ends, mags[1])]
+    for name, got, want, bound in zip(("o", "dq", "dk", "dv"), (o, *g), wants, bounds):
+        tol = ((2 * T + 64) * 2.0 ** -24 + 2.0 ** -16) * bound
+        tol += HALF["bf16"] * (np.abs(want) + tol)
+        bad = ~(np.abs(_np(got) - want) <= tol + 1e-36)
+        assert not bad.any(), (name, int(bad.sum()), float(np.nanmax(np.abs(_np(got) - want) / (tol + 1e-36))))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("off", [8, 3])
 @pytest.mark.parametrize("dk,dv", [(64, 64), (20, 36), (7, 9)])

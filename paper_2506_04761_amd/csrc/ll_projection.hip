@@ -360,6 +360,7 @@ struct DuDev {
   const void* dy;
   const float* pre;  // null: du = dy, only the sums
   void* du;
+  void* low;         // what du's rounding leaves; may be null
   float* part;       // [strips, N]; may be null
   int64_t M, N, rows, cols;  // rows of a strip, workgroups over the columns
 };
@@ -384,6 +385,15 @@ __global__ __launch_bounds__(256) void k_du(DuDev p) {
 #pragma unroll
       for (int i = 0; i < E; ++i) d[i] *= silu_grad(u[i], sigmoidf(u[i]));
       store_n<T, E>(static_cast<T*>(p.du) + m * p.N + at, d, c, false);
+      if (p.low) {
+        float left[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          const float held = to_f32(from_f32<T>(d[i]));
+          left[i] = d[i] == held ? 0.0f : d[i] - held;  // nothing of infinities
+        }
+        store_n<T, E>(static_cast<T*>(p.low) + m * p.N + at, left, c, false);
+      }
     }
 #pragma unroll
     for (int i = 0; i < E; ++i) sum[i] += d[i];
@@ -489,14 +499,21 @@ DuPlan du_plan(int64_t M, int64_t N, int dtype) {
 struct BwdPlan {
   GemmPlan dx, dw;
   DuPlan du;
-  int64_t o_du = 0, o_part = 0, total = 0;  // du; partial sums of whichever kernel runs
+  bool two = false;  // du in two bf16 parts
+  int64_t o_du = 0, o_low = 0, o_part = 0, total = 0;  // du; its second part; partial sums of whichever kernel runs
 };
 BwdPlan bwd_plan(int64_t M, int64_t K, int64_t N, int dtype, bool act) {
   BwdPlan q;
   q.dx = plan(M, K, N, dtype, kDx);
   q.dw = plan(N, K, M, dtype, kDw);
   q.du = du_plan(M, N, dtype);
-  q.o_part = act ? up256(M * N * elem(dtype)) : 0;
+  // The roundings of few values of du do not average out (256 values: the gradient of the weight off by up to 1.55 times what
+  // its own rounding takes, with 1024 by 1.48 as with many).  Such a call has the products of what they leave as more splits,
+  // whose sums stay below 512 MB (1 x 2048 x 64 13.8 us, 23.2 so; 1 x 8192 x 1023 19.5 and 52.8).
+  q.two = act && dtype == 1 && M * N < 1024 && K <= 65536;
+  if (q.two) q.dx.bytes = 2 * q.dx.splits * M * K * 4, q.dw.bytes = 2 * q.dw.splits * N * K * 4;
+  q.o_low = act ? up256(M * N * elem(dtype)) : 0;
+  q.o_part = q.two ? 2 * q.o_low : q.o_low;
   int64_t part = q.du.strips * N * 4;
   part = part < q.dx.bytes ? q.dx.bytes : part;
   part = part < q.dw.bytes ? q.dw.bytes : part;
@@ -516,16 +533,27 @@ void launch_tiles(const GemmDev& p, int64_t workgroups, hipStream_t st) {
 }
 
 template <typename T, bool DM, bool DN>
-hipError_t launch_product(GemmDev p, const GemmPlan& q, float* part, hipStream_t st) {
-  p.m_tiles = q.m_tiles, p.n_tiles = q.n_tiles, p.splits = q.splits, p.span = q.span;
-  p.part = q.splits > 1 ? part : nullptr;
+void launch_tile(const GemmDev& p, const GemmPlan& q, hipStream_t st) {
   const bool dir = direct(p.b, DM, p.K, sizeof(T)) && direct(p.a, DN, p.K, sizeof(T));
   if constexpr (sizeof(T) == 2) {
     if (q.tile == 256) dir ? launch_tiles<T, 256, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 256, DM, DN, false>(p, q.workgroups, st);
   }
   if (q.tile == 128) dir ? launch_tiles<T, 128, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 128, DM, DN, false>(p, q.workgroups, st);
   else if (q.tile == 64) dir ? launch_tiles<T, 64, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 64, DM, DN, false>(p, q.workgroups, st);
-  if (q.splits > 1) {
+}
+
+// A product by its plan; with `low`, a second part of operand b, its products' sums come after the others.
+template <typename T, bool DM, bool DN>
+hipError_t launch_product(GemmDev p, const GemmPlan& q, float* part, hipStream_t st, const void* low = nullptr) {
+  p.m_tiles = q.m_tiles, p.n_tiles = q.n_tiles, p.splits = q.splits, p.span = q.span;
+  p.part = q.bytes ? part : nullptr;
+  launch_tile<T, DM, DN>(p, q, st);
+  if (low) {
+    p.b.p = low, p.part = part + q.splits * p.f.M * p.f.N;
+    launch_tile<T, DM, DN>(p, q, st);
+    p.splits = 2 * q.splits;
+  }
+  if (q.bytes) {
     p.part = part;
     k_gemm_join<T><<<dim3(uint32_t(ceil_div(p.f.M * ceil_div(p.f.N, 4), 256))), dim3(256), 0, st>>>(p);
   }
@@ -558,9 +586,11 @@ hipError_t bwd(const ProjArgs& a, const ProjGrads& g, hipStream_t st) {
   char* ws = static_cast<char*>(a.workspace);
   float* part = reinterpret_cast<float*>(ws + q.o_part);
   const void* du = a.act ? ws + q.o_du : g.dy;
+  void* const low = q.two ? ws + q.o_low : nullptr;  // may be null
   hipError_t e = hipSuccess;
   if (a.act || g.dbias) {
-    const DuDev d = {g.dy, a.act ? a.pre : nullptr, ws + q.o_du, g.dbias ? part : nullptr, a.M, a.N, q.du.rows, q.du.cols};
+    const DuDev d = {g.dy, a.act ? a.pre : nullptr, ws + q.o_du, low, g.dbias ? part : nullptr,
+                      a.M, a.N, q.du.rows, q.du.cols};
     k_du<T><<<dim3(uint32_t(q.du.cols * q.du.strips)), dim3(256), 0, st>>>(d);
     e = hipGetLastError();
     if (e == hipSuccess && g.dbias) {
@@ -574,13 +604,13 @@ hipError_t bwd(const ProjArgs& a, const ProjGrads& g, hipStream_t st) {
     GemmDev p = {};
     p.a = {a.weight, a.K, a.K}, p.b = {du, a.N, a.M}, p.K = a.N;
     p.f = {g.dx, nullptr, nullptr, 0, nullptr, a.M, a.K, 0};
-    e = launch_product<T, false, true>(p, q.dx, part, st);
+    e = launch_product<T, false, true>(p, q.dx, part, st, low);
   }
   if (e == hipSuccess && g.dweight) {
     GemmDev p = {};
     p.a = {a.x, a.x_stride, a.K}, p.b = {du, a.N, a.N}, p.K = a.M;
     p.f = {g.dweight, nullptr, nullptr, 0, nullptr, a.N, a.K, 0};
-    e = launch_product<T, true, true>(p, q.dw, part, st);
+    e = launch_product<T, true, true>(p, q.dw, part, st, low);
   }
   return e;
 }
@@ -596,7 +626,7 @@ int64_t projection_workspace(int64_t M, int64_t K, int64_t N, int act, int dtype
 
 bool projection_launchable(int64_t M, int64_t K, int64_t N, int act, int dtype, bool backward) {
   auto ok = [](const GemmPlan& q, int64_t m, int64_t n) {
-    return launchable(q.workgroups, 64 * kFewWaves) && (q.splits == 1 || launchable(ceil_div(m * ceil_div(n, 4), 256), 256));
+    return launchable(q.workgroups, 64 * kFewWaves) && (!q.bytes || launchable(ceil_div(m * ceil_div(n, 4), 256), 256));
   };
   if (!backward) return ok(plan(M, N, K, dtype, kForward), M, N);
   const BwdPlan q = bwd_plan(M, K, N, dtype, act != 0);

@@ -78,8 +78,9 @@ def _check_fwd(y, pre, h, dtype, silu, K):
     _within(y, want, tol + HALF[dtype] * (np.abs(want) + tol), "y")
 
 
-def _check_bwd(g, h, dtype, silu, K):
+def _check_bwd(g, h, dtype, silu, K, into_e=None):
     e = HALF[dtype]
+    into_e = e if into_e is None else into_e
     M, N = h["dy"].shape
     dx, dw, db = layer.projection_grad(h["x"], h["w"], h["dy"], h["b"], silu)
     u = layer.projection(h["x"], h["w"], h["b"])[1]
@@ -87,7 +88,7 @@ def _check_bwd(g, h, dtype, silu, K):
     off = np.zeros_like(du)  # of du in fp32
     if silu:
         off = np.abs(h["dy"]) * (0.5 * _sum_tol(h["x"], h["w"].T, K) + (8 + np.abs(u)) * 2.0 ** -23)
-    into = off + (e * (du + off) if silu else 0)  # of du in the products
+    into = off + (into_e * (du + off) if silu else 0)  # of du in the products
     for name, got, want, a, b, n in (("dx", g[0], dx, du, h["w"], N), ("dw", g[1], dw, du.T, h["x"], M)):
         d = into if name == "dx" else into.T
         tol = (n + 8) * 2.0 ** -24 * ((a + d) @ np.abs(b)) + d @ np.abs(b)
@@ -114,6 +115,24 @@ def test_sizes(M, K, N, dtype, off):
     y = ll.ll_projection_fwd(i["x"], i["w"], i["b"], i["r"], ll.LL_ACT_SILU, pre)
     _check_fwd(y, pre, h, dtype, True, K)
     _check_bwd(ll.ll_projection_bwd(i["x"], i["w"], i["b"], i["dy"], ll.LL_ACT_SILU, pre), h, dtype, True, K)
+
+
+@pytest.mark.parametrize("M,K,N", [(1, 8, 8), (1, 2048, 40), (1, 100, 1023), (7, 257, 130), (31, 64, 33), (3, 8192, 64),
+                                   (1000, 65, 1), (15, 1000, 64)])
+@pytest.mark.parametrize("off", [None, 3])
+def test_few_gradients_are_rounded_once(off, M, K, N):
+    """bf16, fewer than 1024 values of du: du enters its products in two parts, which leave 2^-8 of 2^-8, so the head's
+    bounds with 2^-16 |du| for 2^-8 |du|."""
+    from paper_2506_04761_amd import block as ll
+    i = _inputs(M + N, M, K, N, "bf16", off, residual=False)
+    h = _host(i)
+    import torch
+    pre = torch.empty((M, N), device="cuda")
+    ll.ll_projection_fwd(i["x"], i["w"], i["b"], None, ll.LL_ACT_SILU, pre)
+    ws = ll.ll_projection_workspace(i["x"], i["w"], ll.LL_ACT_SILU, True)
+    ws.fill_(255)
+    _check_bwd(ll.ll_projection_bwd(i["x"], i["w"], i["b"], i["dy"], ll.LL_ACT_SILU, pre, workspace=ws), h, "bf16", True, K,
+               into_e=2.0 ** -16)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

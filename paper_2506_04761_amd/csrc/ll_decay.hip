@@ -259,29 +259,34 @@ __device__ inline f32x4 pack<float>(const f32x4* v) {
   return v[0];
 }
 
-// What packing leaves of the values, nothing of infinities.
-template <typename T>
-__device__ inline void remainder(f32x4& v) {
+// One of two parts of values that are not -0.  The upper one is formed again for the rest: kept, those of a state spill.
+__device__ inline f32x4 part_of(f32x4 v, int part) {
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    const float held = to_f32(from_f32<T>(v[r]));
-    v[r] = v[r] == held ? 0.0f : v[r] - held;
+    if (part) asm volatile("" : "+v"(v[r]));
+    const float hi = upper_part(v[r]);
+    v[r] = part ? v[r] - hi : hi;
   }
+  return v;
 }
 
-// v w of a fragment's slots as N bf16 parts, which hold 8 bits each of the products (fp32: the product).
+// v w of a fragment's slots as N bf16 parts, upper ones but for the third: three are off by 2^-24 of a product, two by 2^-14.
+// fp32: the product.
 template <int N>
 __device__ inline void weighted(bf16x8 v, const float* w, bf16x8* part) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
   for (int x = 0; x < 8; x += 2) {
-    float a = to_f32(__bf16(v[x])) * w[x], b = to_f32(__bf16(v[x + 1])) * w[x + 1];
+    float a = fmaf(to_f32(__bf16(v[x])), w[x], kNoZero), b = fmaf(to_f32(__bf16(v[x + 1])), w[x + 1], kNoZero);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-      const bf16x2 y = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
+      bf16x2 y = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
+      if (k < 2) {
+        const float ha = upper_part(a), hb = upper_part(b);
+        y = __builtin_bit_cast(bf16x2, __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, hb), __builtin_bit_cast(unsigned, ha), 0x07060302u));
+        a -= ha, b -= hb;
+      }
       part[k][x] = y[0], part[k][x + 1] = y[1];
-      const unsigned bits = __builtin_bit_cast(unsigned, y);
-      a -= __builtin_bit_cast(float, bits << 16), b -= __builtin_bit_cast(float, bits & 0xffff0000u);
     }
   }
 }
@@ -423,7 +428,7 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
 #pragma unroll
       for (int part = 0; part < PARTS; ++part) {
         if (part) __syncthreads();  // the first part's scores are read; queries and keys are there: no chunk comes after
-        // P^T of 16 queries and the keys up to them; of the second part, what its rounding left
+        // P^T of 16 queries and the keys up to them
 #pragma unroll
         for (int x = 0; x < NU; ++x) {
           const int qt = (wave + x * NW) % QT, u = (wave + x * NW) / QT;
@@ -440,10 +445,10 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
 #pragma unroll
           for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) pt[r][e] *= pw[x][r][e];
-          if (part) {
+            for (int e = 0; e < 4; ++e) pt[r][e] = FEW ? fmaf(pt[r][e], pw[x][r][e], kNoZero) : pt[r][e] * pw[x][r][e];
+          if (FEW) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) remainder<T>(pt[r]);
+            for (int r = 0; r < R; ++r) pt[r] = part_of(pt[r], part);
           }
           sp[qt][u][lane] = pack<T>(pt);
         }
@@ -460,8 +465,9 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
                 f32x4 x[R];
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
+                  if (FEW && !low) S[R * ks + r][v] += kNoZero;
                   x[r] = S[R * ks + r][v];
-                  if (low) remainder<T>(x[r]);
+                  if (FEW) x[r] = part_of(x[r], low);
                 }
                 s[v] = pack<T>(x);
               }
@@ -515,8 +521,8 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
       orow += C * ostep;
     }
 
-    // the state after the chunk; values times powers of the decay in bf16 parts, three where fp32's bits are wanted and
-    // two (16 bits) where only rounded results come of it
+    // the state after the chunk; values times powers of the decay in bf16 parts, three where fp32's bits are wanted and two
+    // where only rounded results come of it (the state itself is rounded to 8 bits there, an operand of the next chunk)
     // what the factors leave out of exact ones is carried over, so that their product over the chunks is off by a rounding
     over += ch ? chunk.lo : begin.lo;
     const float carry = (ch ? chunk.hi : begin.hi) + over;
@@ -537,6 +543,10 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
       // adds the parts from `from` on to the state
       auto add = [&](auto from, auto to) {
         constexpr int P0 = decltype(from)::value, P1 = decltype(to)::value;
+        if (P0 && DK <= 64 && NV == 2) {  // formed again: kept from the parts before, they take the registers of a third workgroup
+#pragma unroll
+          for (int x = 0; x < KF / 4; ++x) asm volatile("" : "+v"(w[x]));
+        }
         Frag part[NV][P1];
 #pragma unroll
         for (int v = 0; v < NV; ++v) weighted<P1>(vf[v][u], w, part[v]);

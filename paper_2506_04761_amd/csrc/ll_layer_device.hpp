@@ -89,6 +89,16 @@ __device__ inline float softplusf(float v) {
   return fmaf(s + s, p, v > 0.0f ? v : 0.0f);
 }
 
+// A value in two addends: its upper part, the upper 16 bits of the float before it (towards zero), which bf16 holds, and the
+// rest, below 2^-7 of it.  Both have the value's sign and neither is zero where the value is not (powers of two away from
+// the smallest float), an infinity's rest is infinite: so an infinity on either side of a product is one in the sum of the
+// parts' products, where a rounded part would leave 0 times it, or two of opposite signs.  -0 has no float before it: kNoZero,
+// which is too little for bf16, is added first where it may come.
+constexpr float kNoZero = 0x1p-149f;
+__device__ inline float upper_part(float v) {
+  return __builtin_bit_cast(float, __builtin_elementwise_sub_sat(__builtin_bit_cast(unsigned, v), 1u) & 0xffff0000u);
+}
+
 // Direct copies of 16 bytes a lane to LDS, lane l's to `lds` + 16 l.  In inline assembly: before every LDS read the compiler
 // waits for all such copies that it knows of, also those of another buffer that are to arrive meanwhile.  The caller waits
 // for them itself (copies_done, then a barrier) before they are read; a memory barrier for the compiler either way.  M0 takes

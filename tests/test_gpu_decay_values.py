@@ -1,0 +1,83 @@
+"""The decay attention's infinities and NaN, on the GPU against the float64 oracle: a state is infinite where the formulas
+have it so, and what a token's infinity or NaN does not reach by the formulas keeps its bits, but for outputs of up to 63
+tokens before it (of the gradients of k and v, up to 63 after it), which may be NaN.
+
+Tolerances of what stays finite are bounds: (2 T + 64) 2^-24 times the same sums of absolute values, for states that keep
+fp32's bits."""
+
+import numpy as np
+import pytest
+
+from oracle import layer
+from tests.gpu_util import to_dev
+
+pytestmark = pytest.mark.gpu
+
+INF = float("inf")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _device():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2506_04761_amd  # noqa: F401  (fails loudly if the library is missing)
+
+
+def _np(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def _inputs(seed, T, dk, dv, dtype, B=1, H=2):
+    r = np.random.default_rng(seed)
+    q, k = (to_dev(r.standard_normal((B, T, H, dk)), dtype) for _ in "qk")
+    v = to_dev(r.standard_normal((B, T, H, dv)), dtype)
+    # 600 tokens away a power of the decay is still 2^-19
+    return q, k, v, to_dev(np.array([-0.02, -0.004])[:H]), to_dev(r.standard_normal((B, H, dk, dv)))
+
+
+def _same_states(got, q, k, v, ld, initial, ends=None):
+    """The states of the formulas: infinities and NaN where they have them, the others within their bound."""
+    h = [_np(t) for t in (q, k, v, ld)]
+    with np.errstate(all="ignore"):
+        _, want = layer.decay_attention(*h, 1.0, _np(initial), ends)
+        clean = [np.nan_to_num(np.abs(x), posinf=0.0) for x in h[:3]]
+        _, bound = layer.decay_attention(*clean, h[3], 1.0, np.nan_to_num(np.abs(_np(initial)), posinf=0.0), ends)
+        got, T = _np(got), v.shape[1]
+        assert np.isinf(want).any()
+        assert np.array_equal(np.isnan(got), np.isnan(want))
+        assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)])
+        assert not np.isinf(got[np.isfinite(want)]).any()
+        off = np.abs(got - want)
+        assert (off[np.isfinite(want)] <= ((2 * T + 64) * 2.0 ** -24 * bound)[np.isfinite(want)]).all()
+
+
+# head sizes of every kernel, whole vectors and not
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dk,dv", [(24, 40), (64, 128), (33, 65), (128, 64), (128, 128), (101, 143), (256, 72), (200, 50)])
+@pytest.mark.parametrize("T,at", [(1, 0), (40, 17), (64, 63), (150, 3), (150, 140)])
+def test_a_state_is_infinite_where_a_token_makes_it_so(T, at, dk, dv, dtype):
+    from paper_2506_04761_amd import block as ll
+    import torch
+    q, k, v, ld, initial = _inputs(T + dk, T, dk, dv, dtype)
+    k[0, at, 0, dk // 2] = INF
+    v[0, at, 1, dv // 3] = -INF
+    final = torch.full_like(initial, float("nan"))
+    ll.ll_decay_attention_fwd(q, k, v, ld, 1.0, initial, final)
+    _same_states(final, q, k, v, ld, initial)
+
+
+@pytest.mark.parametrize("dk,dv", [(24, 40), (128, 128), (101, 143)])
+@pytest.mark.parametrize("T", [1, 40, 64])
+def test_an_infinite_token_in_one_chunk_of_bf16(T, dk, dv):
+    """The scores' second parts do not make NaN of what the first have made infinite: the last token's outputs, all of the
+    tokens of the chunk before it, are infinities of the sign of its score times the value's."""
+    from paper_2506_04761_amd import block as ll
+    q, k, v, ld, _ = _inputs(T, T, dk, dv, "bf16")
+    v[0, T - 1, 0, 1] = INF
+    k[0, T - 1, 1, 0] = -INF
+    o = _np(ll.ll_decay_attention_fwd(q, k, v, ld))[0, T - 1]
+    qn, kn, vn = (_np(t)[0, T - 1] for t in (q, k, v))
+    assert o[0, 1] == np.sign((qn[0] * kn[0]).sum()) * INF
+    assert np.isfinite(np.delete(o[0], 1)).all()
+    assert np.array_equal(o[1], np.where(qn[1, 0] * vn[1] > 0, -INF, INF))

@@ -176,6 +176,11 @@ struct Carry {
     const double w = exp(double(log_decay[h]) * n);
     hi = float(w), lo = float(w - hi);
   }
+  // g^n v + u; an infinite v meets lo as the largest number, or 0 or a negative lo times it would make NaN of it
+  __device__ inline float times_plus(float v, float u) const {
+    constexpr float kMost = 0x1.fffffep127f;
+    return fmaf(hi, v, fmaf(lo, __builtin_amdgcn_fmed3f(v, -kMost, kMost), u));
+  }
 };
 
 // Copies chunks of C rows of up to W elements to LDS, 16 bytes a thread at a time: straight there (VEC: rows of whole,
@@ -642,7 +647,7 @@ __global__ __launch_bounds__(256) void k_join(float* h, const float* first, cons
     for (int k = 0; k < U; ++k) u[k] = s + k < used ? p[(s + k) * size] : 0.0f;
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-      v = fmaf(w.hi, v, fmaf(w.lo, v, u[k]));
+      v = w.times_plus(v, u[k]);
       if (s + k < used) p[(s + k) * size] = v;
     }
   }

@@ -81,3 +81,25 @@ def test_an_infinite_token_in_one_chunk_of_bf16(T, dk, dv):
     assert o[0, 1] == np.sign((qn[0] * kn[0]).sum()) * INF
     assert np.isfinite(np.delete(o[0], 1)).all()
     assert np.array_equal(o[1], np.where(qn[1, 0] * vn[1] > 0, -INF, INF))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dk,dv", [(24, 40), (64, 128), (33, 65), (128, 128), (256, 72)])
+@pytest.mark.parametrize("T,ends", [(600, None), (1100, [1100, 513])])
+@pytest.mark.parametrize("decays", [[0.0, -0.01], [-0.0051, -0.0073]])
+def test_an_infinite_state_passes_the_segments(decays, T, ends, dk, dv, dtype):
+    """Segments' states are joined: infinities of the initial state and of a token of the first segment reach the end, also
+    where a power of the decay is a float (its rounding leaves 0) or below its float (a negative rest)."""
+    from paper_2506_04761_amd import block as ll
+    import torch
+    B = 1 if ends is None else len(ends)
+    q, k, v, ld, initial = _inputs(T + dk, T, dk, dv, dtype, B=B)
+    ld = to_dev(np.array(decays))
+    initial[:, 0, 1, 2] = INF
+    initial[:, 1, 3, 4] = -INF
+    k[0, 30, 0, dk // 2] = -INF
+    v[0, 31, 1, dv // 3] = INF
+    lengths = None if ends is None else torch.tensor(ends, dtype=torch.int32, device="cuda")
+    final = torch.full_like(initial, float("nan"))
+    ll.ll_decay_attention_fwd(q, k, v, ld, 1.0, initial, final, lengths)
+    _same_states(final, q, k, v, ld, initial, ends)

@@ -169,18 +169,18 @@ __device__ inline float log2_decay(const float* log_decay, int h) {
 __device__ const uint4 kZeros = {0, 0, 0, 0};  // rows before the first token, elements beyond the width
 
 // g^n for the state's way over n tokens, and what fp32 leaves of it: its error would be taken to the power of the chunks (a
-// state after 14758 tokens: off by 1.1e-6 with v_exp_f32's power, 6e-7 so).
+// state after 14758 tokens: off by 1.1e-6 with v_exp_f32's power, 6e-7 so).  `hi` is the float towards zero and `lo` not
+// zero where g^n is not: an infinite state stays one (0 or a negative rest times it would make NaN of it).
 struct Carry {
   float hi, lo;
   __device__ inline Carry(const float* log_decay, int h, double n) {
     const double w = exp(double(log_decay[h]) * n);
-    hi = float(w), lo = float(w - hi);
+    hi = float(w);
+    if (hi > w) hi = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, hi) - 1);
+    const double rest = w - hi, least = w * 0x1p-60;
+    lo = float(rest > least ? rest : least);
   }
-  // g^n v + u; an infinite v meets lo as the largest number, or 0 or a negative lo times it would make NaN of it
-  __device__ inline float times_plus(float v, float u) const {
-    constexpr float kMost = 0x1.fffffep127f;
-    return fmaf(hi, v, fmaf(lo, __builtin_amdgcn_fmed3f(v, -kMost, kMost), u));
-  }
+  __device__ inline float times_plus(float v, float u) const { return fmaf(hi, v, fmaf(lo, v, u)); }  // g^n v + u
 };
 
 // Copies chunks of C rows of up to W elements to LDS, 16 bytes a thread at a time: straight there (VEC: rows of whole,
@@ -655,6 +655,8 @@ __global__ __launch_bounds__(256) void k_join(float* h, const float* first, cons
 
 // Bound by memory: 64 sequences of 16 heads of 128 x 128 32 us, 4.2 TB/s of states in and out.
 // One token of 256 / LV rows at a time: o = scale (g S + k v^T)^T q, the state passed through.
+// g with what its rounding leaves, as the prompts' kernels have it: g in fp32 alone moves a state by up to 2^-25 a token, all
+// to one side (4096 tokens of 1 - g = 2^-12.5: by 7e-5).
 struct StepDev {
   Heads q, k, v;
   const float* state;
@@ -676,7 +678,7 @@ __global__ __launch_bounds__(256) void k_decay_step(StepDev p) {
   const T* q = static_cast<const T*>(p.q.p) + b * p.q.sb + (h / p.q.group) * p.dk;
   const T* k = static_cast<const T*>(p.k.p) + b * p.k.sb + (h / p.k.group) * p.dk;
   const T* v = static_cast<const T*>(p.v.p) + b * p.v.sb + h * p.dv + col;
-  const float decay = fast_exp2(log2_decay(p.log_decay, h));
+  const Carry decay(p.log_decay, h, 1.0);
   const auto vr = load_n<T, 4>(v, count, false);
   float vf[4], o[4] = {};
 #pragma unroll
@@ -699,7 +701,7 @@ __global__ __launch_bounds__(256) void k_decay_step(StepDev p) {
         float x[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          x[i] = fmaf(decay, st[u][i], kr[u] * vf[i]);
+          x[i] = decay.times_plus(st[u][i], kr[u] * vf[i]);
           o[i] = fmaf(qr[u], x[i], o[i]);
         }
         store_n<float, 4>(p.next + base + int64_t(r + u * RS) * p.dv, x, r + u * RS < p.dk ? count : 0, p.vec);

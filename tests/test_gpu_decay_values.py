@@ -33,7 +33,7 @@ def _inputs(seed, T, dk, dv, dtype, B=1, H=2):
     q, k = (to_dev(r.standard_normal((B, T, H, dk)), dtype) for _ in "qk")
     v = to_dev(r.standard_normal((B, T, H, dv)), dtype)
     # 600 tokens away a power of the decay is still 2^-19
-    return q, k, v, to_dev(np.array([-0.02, -0.004])[:H]), to_dev(r.standard_normal((B, H, dk, dv)))
+    return q, k, v, to_dev(np.resize([-0.02, -0.004], H)), to_dev(r.standard_normal((B, H, dk, dv)))
 
 
 def _same_states(got, q, k, v, ld, initial, ends=None):
@@ -103,3 +103,18 @@ def test_an_infinite_state_passes_the_segments(decays, T, ends, dk, dv, dtype):
     final = torch.full_like(initial, float("nan"))
     ll.ll_decay_attention_fwd(q, k, v, ld, 1.0, initial, final, lengths)
     _same_states(final, q, k, v, ld, initial, ends)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_an_infinite_state_stays_so_over_tokens(dtype):
+    from paper_2506_04761_amd import block as ll
+    import torch
+    q, k, v, _, state = _inputs(3, 5, 40, 72, dtype, H=4)
+    ld = to_dev(np.array([0.0, -0.01, -0.0051, -0.0073]))
+    k[0, 2, 2, 7] = INF
+    state[0, :, 1, 2] = INF
+    state[0, 1, 3, 4] = -INF
+    first = state.clone()
+    for t in range(5):
+        ll.ll_decay_attention_step(q[:, t], k[:, t], v[:, t], ld, state)
+    _same_states(state, q, k, v, ld, first)

@@ -306,11 +306,12 @@ constexpr bool keys_ahead(int dk) { return dk <= 128; }
 
 // One segment of one head, 64 NV values a workgroup: a wave holds the state's rows of its 16 NV columns.  d1 <= DK.
 // Chunks end with the segment: the first may begin with rows of zeros, and powers of the decay are the same in all others.
-// FEW: bf16 calls of one chunk take scores and states in two parts: with few of them their roundings do not average out (28
-// sequences of one token: results off by 0.0032, 0.0017 so; of more than 64 tokens 0.0025 at most).  512 sequences of 64
-// tokens, 16 heads of 128 x 128: 597 us, 622 so.  A branch on a sequence's own length took registers from the long calls.
-template <typename T, int DK, int NV, bool STATE, bool VEC, bool FEW = false>
-__global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
+// FEW: bf16 sequences of one chunk take scores and states in two parts: with few of them their roundings do not average out
+// (28 sequences of one token: results off by 0.0032, 0.0017 so; of more than 64 tokens 0.0025 at most).  512 sequences of 64
+// tokens, 16 heads of 128 x 128: 597 us, 622 so.
+template <typename T, int DK, int NV, bool STATE, bool VEC, bool FEW, typename Keys, typename Values, typename Queries, typename Scores>
+__device__ __attribute__((always_inline)) inline void attend_segment(const DecayDev& p, int64_t b, int h, int seg, int blk, int64_t live,
+                                                                     Keys& sk, Values& sv, Queries& sq, Scores& sp, float* sw) {
   constexpr int KF = Op<T>::KF, C = Op<T>::C, R = KF / 16, QT = C / 16, US = C / KF, KS = DK / KF, DT = DK / 16;
   constexpr int NW = 4, DV = 16 * NW * NV, NU = QT * US / NW;  // NU: fragments of P^T that a wave forms
   constexpr bool AHEAD = keys_ahead(DK);
@@ -318,25 +319,9 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
   typedef typename Op<T>::Frag Frag;
   typedef Tile<T, DK> TlK;
   typedef Tile<T, DV> TlV;
-  __shared__ __attribute__((aligned(1024))) T sk[AHEAD ? 2 : 1][C * DK];
-  __shared__ __attribute__((aligned(1024))) T sv[AHEAD && STATE ? 2 : 1][C * DV];
-  __shared__ __attribute__((aligned(1024))) T sq[STATE ? 8 : C * DK];
-  __shared__ Frag sp[STATE ? 1 : QT][US][64];
-  __shared__ __attribute__((aligned(16))) float sw[C];  // what a token's product counts in the state after the chunk
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i = lane & 15;
-
-  // the sums of segments go through the input in one order, the results in the other: what was read last is still cached
-  unsigned id = unsigned(xcd_remap(blockIdx.x, p.groups));
-  if (!STATE && p.S > 1) id = unsigned(p.groups) - 1 - id;
-  const unsigned segs = STATE ? p.S - 1 : p.S;
-  const int blk = int(id % unsigned(p.blocks));
-  id /= unsigned(p.blocks);
-  const int seg = int(id % segs);
-  id /= segs;
-  const int h = int(id % unsigned(p.H));
-  const int64_t b = id / unsigned(p.H);
   const int d1 = p.a.width, d2 = p.c.width, col0 = blk * DV;
-  const int64_t live = uniform64(live_tokens(p.lengths, b, p.T)), t0 = seg * p.L;
+  const int64_t t0 = seg * p.L;
   int64_t n = live - t0 < p.L ? live - t0 : p.L;  // tokens of this segment
   n = n < 0 ? 0 : n;
   const int64_t chunks = (n + C - 1) / C;
@@ -628,6 +613,35 @@ __global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
   }
 }
 
+// SHORT: there may be sequences of one chunk, which take the FEW way whatever stands beside them in the batch.  (A launch of
+// its own for them: 32 sequences of up to 512 tokens, 16 heads of 128 x 128, 74 -> 95 us, 75 so.  Without the instances that
+// lack it: 320 tokens, 8 heads of 64 x 64, 17.0 -> 17.8.)
+template <typename T, int DK, int NV, bool STATE, bool VEC, bool SHORT = false>
+__global__ __launch_bounds__(256, 2) void k_attend(DecayDev p) {
+  constexpr int KF = Op<T>::KF, C = Op<T>::C, DV = 64 * NV;
+  constexpr bool AHEAD = keys_ahead(DK);
+  __shared__ __attribute__((aligned(1024))) T sk[AHEAD ? 2 : 1][C * DK];
+  __shared__ __attribute__((aligned(1024))) T sv[AHEAD && STATE ? 2 : 1][C * DV];
+  __shared__ __attribute__((aligned(1024))) T sq[STATE ? 8 : C * DK];
+  __shared__ typename Op<T>::Frag sp[STATE ? 1 : C / 16][C / KF][64];
+  __shared__ __attribute__((aligned(16))) float sw[C];  // what a token's product counts in the state after the chunk
+  // the sums of segments go through the input in one order, the results in the other: what was read last is still cached
+  unsigned id = unsigned(xcd_remap(blockIdx.x, p.groups));
+  if (!STATE && p.S > 1) id = unsigned(p.groups) - 1 - id;
+  const unsigned segs = STATE ? p.S - 1 : p.S;
+  const int blk = int(id % unsigned(p.blocks));
+  id /= unsigned(p.blocks);
+  const int seg = int(id % segs);
+  id /= segs;
+  const int h = int(id % unsigned(p.H));
+  const int64_t b = id / unsigned(p.H);
+  const int64_t live = uniform64(live_tokens(p.lengths, b, p.T));
+  if constexpr (SHORT) {
+    if (live <= C) return attend_segment<T, DK, NV, STATE, VEC, true>(p, b, h, seg, blk, live, sk, sv, sq, sp, sw);
+  }
+  attend_segment<T, DK, NV, STATE, VEC, false>(p, b, h, seg, blk, live, sk, sv, sq, sp, sw);
+}
+
 // The states at the segments' starts, in place of the segments' own sums: h_0 = first, h_(s+1) = g^(n_s) h_s + u_s.
 __global__ __launch_bounds__(256) void k_join(float* h, const float* first, const float* log_decay, const int32_t* lengths,
                                               int64_t T, int64_t L, int H, int S, int64_t size, int64_t total) {
@@ -766,7 +780,7 @@ hipError_t launch_attend(const DecayDev& p, bool state, hipStream_t st) {
   const dim3 grid(uint32_t(p.groups)), block(256);
   const bool vec = p.b.vec && p.c.vec && (state || (p.a.vec && p.vec_out));
   if constexpr (sizeof(T) == 2) {
-    if (!state && p.T <= Op<T>::C) {
+    if (!state && (p.T <= Op<T>::C || p.lengths)) {
       vec ? k_attend<T, DK, NV, false, true, true><<<grid, block, 0, st>>>(p) : k_attend<T, DK, NV, false, false, true><<<grid, block, 0, st>>>(p);
       return hipGetLastError();
     }

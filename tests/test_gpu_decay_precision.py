@@ -8,7 +8,8 @@ import numpy as np
 import pytest
 
 from oracle import layer
-from tests.gpu_util import to_dev, torch_dtype
+from tests.gpu_util import to_dev
+from tests.test_gpu_decay_attention import HALF, _Case
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +53,29 @@ def test_decoding_forgets_at_the_rate_of_the_decay(inplace, dtype):
     assert (np.abs(off) <= 2 * n * U).all()
     # two roundings a token (of lo S, which is none to speak of, and of the sum), and 2 u
     assert (np.abs(off.mean(1)) <= 2 * U + 6 * U * np.sqrt(n / off.shape[1])).all(), off.mean(1) / U
+
+
+@pytest.mark.parametrize("dk,dv", [(64, 64), (64, 128), (33, 80), (128, 128), (101, 143), (128, 48), (256, 128), (200, 50)])
+@pytest.mark.parametrize("T", [65, 150, 600])
+def test_short_sequences_of_a_longer_batch_are_rounded_once(T, dk, dv):
+    """bf16 sequences of one chunk (64 tokens) take scores and states in two parts, which leave 2^-16 of them, whatever
+    stands beside them in the batch: (2 n + 64) u A for the sums, 2^-16 A for the operands, the results' own rounding."""
+    ends = [1, T, 3, 64, 0, 17, 65]
+    c = _Case(dk + T, len(ends), T, 2, 1, dk, dv, "bf16", ends=ends)
+    h = [np.nan_to_num(_np(t)) for t in (c.q, c.k, c.v)] + [_np(c.ld)]
+    d, i, f = np.nan_to_num(_np(c.d_o)), _np(c.initial), _np(c.d_final)
+    mag = [np.abs(x) for x in h[:3]] + [h[3]]
+    o, final, g = c.run()
+    wants = [*layer.decay_attention(*h, c.scale, i, ends), *layer.decay_attention_grad(*h, d, c.scale, i, ends, f)]
+    bounds = [*layer.decay_attention(*mag, c.scale, np.abs(i), ends),
+              *layer.decay_attention_grad(*mag, np.abs(d), c.scale, np.abs(i), ends, np.abs(f))]
+    for name, got, want, bound in zip(("o", "final", "dq", "dk", "dv", "dinitial"), (o, final, *g), wants, bounds):
+        got = _np(got)
+        for b, n in enumerate(ends):
+            if n > 64:
+                continue
+            tol = (2 * n + 64) * U * bound[b]
+            if name not in ("final", "dinitial"):
+                tol += 2.0 ** -16 * bound[b]
+                tol += HALF["bf16"] * (np.abs(want[b]) + tol)
+            assert (np.abs(got[b] - want[b]) <= tol + 1e-36).all(), (name, n)

@@ -199,13 +199,15 @@ __device__ inline void finish(const Finish& f, float* v, int64_t m, int64_t n) {
 
 struct GemmDev {
   Side a, b;               // outputs n, outputs m
+  const void* low;         // TWO: what b's rounding leaves, laid out as b
   int64_t K, span;         // span: k of a split, whole stages
   int64_t m_tiles, n_tiles, splits;
   float* part;             // several splits: [splits, M, N] partial sums
   Finish f;
 };
 
-template <typename T, int TM, int TN, int WM, int WN, bool DOWN_M, bool DOWN_N, bool DIRECT>
+// TWO: the products of b's second part come after those of the first, into the same sums.
+template <typename T, int TM, int TN, int WM, int WN, bool DOWN_M, bool DOWN_N, bool DIRECT, bool TWO = false>
 __global__ __launch_bounds__(64 * WM * WN, 2) void k_gemm(GemmDev p) {
   constexpr int NT = 64 * WM * WN, FM = TM / WM / 16, FN = TN / WN / 16;
   typedef Tile<T, TM, DOWN_M, !(DOWN_M && sizeof(T) == 2)> TlM;
@@ -226,7 +228,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_gemm(GemmDev p) {
   const int64_t m0 = int64_t(8 * strip + id % rows) * TM, n0 = int64_t(id / rows) * TN;
 
   const int64_t k0 = split * p.span;
-  int64_t left = p.K - k0 < p.span ? p.K - k0 : p.span;
+  const int64_t own = p.K - k0 < p.span ? p.K - k0 : p.span;
+  int64_t left = own;
   Copy<T, TlM, TM, DOWN_M, DIRECT, NT> cm;
   Copy<T, TlN, TN, DOWN_N, DIRECT, NT> cn;
   cm.start(p.b, m0, k0, p.K);
@@ -237,12 +240,17 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_gemm(GemmDev p) {
   cm.store(s);
   cn.store(s + TM * BK);
   const int stages = int((left + BK - 1) / BK);
-  for (int st = 0; st < stages; ++st) {
+  for (int st = 0; st < (TWO ? 2 : 1) * stages; ++st) {
     T* now = s + (st & 1) * kStage;
     T* next = s + (~st & 1) * kStage;
     if (DIRECT) copies_done();
     __syncthreads();
     left -= BK;
+    if (TWO && st + 1 == stages) {
+      cm.start({p.low, p.b.stride, p.b.n}, m0, k0, p.K);
+      cn.start(p.a, n0, k0, p.K);
+      left = own;
+    }
     if (left > 0) {
       cm.load(next, left);
       cn.load(next + TM * BK, left);
@@ -445,7 +453,7 @@ constexpr TileCost kCosts[2][3] = {{{64, 5, 0.1, 0.6, 1.0}, {128, 2, 0.2, 2.1, 1
 // LDS (8192 x 1024 over 8192 in bf16: tiles of 64 202 us, of 128 152, of 256 in two splits 133), smaller ones and splits
 // fill more compute units (1024 x 1024 over 1024: 11.6, 15.2 and 26.6 us; 1024 x 2048 over 8064: 128 without splits 68, in
 // four 49).
-GemmPlan plan(int64_t M, int64_t N, int64_t K, int dtype, Product what) {
+GemmPlan plan(int64_t M, int64_t N, int64_t K, int dtype, Product what, int largest = 256) {
   GemmPlan q;
   const int64_t BK = kStageBytes / elem(dtype), stages = ceil_div(K, BK);
   // what is read, at the rate of a copy; tiles' stages overlap with about half of it
@@ -462,7 +470,7 @@ GemmPlan plan(int64_t M, int64_t N, int64_t K, int dtype, Product what) {
     if (best <= 4) return q;  // less than tiles and their join take at all
   }
   for (const TileCost& c : kCosts[dtype]) {
-    if (!c.tile) continue;
+    if (!c.tile || c.tile > largest) continue;
     const int64_t m_tiles = ceil_div(M, c.tile), n_tiles = ceil_div(N, c.tile);
     for (const int64_t want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
       const int64_t each = ceil_div(stages, want), splits = ceil_div(stages, each);
@@ -499,19 +507,18 @@ DuPlan du_plan(int64_t M, int64_t N, int dtype) {
 struct BwdPlan {
   GemmPlan dx, dw;
   DuPlan du;
-  bool two = false;  // du in two bf16 parts
+  bool two = false;  // du in two bf16 parts, tiles of 64
   int64_t o_du = 0, o_low = 0, o_part = 0, total = 0;  // du; its second part; partial sums of whichever kernel runs
 };
 BwdPlan bwd_plan(int64_t M, int64_t K, int64_t N, int dtype, bool act) {
   BwdPlan q;
-  q.dx = plan(M, K, N, dtype, kDx);
-  q.dw = plan(N, K, M, dtype, kDw);
-  q.du = du_plan(M, N, dtype);
   // The roundings of few values of du do not average out (256 values: the gradient of the weight off by up to 1.55 times what
-  // its own rounding takes, with 1024 by 1.48 as with many).  Such a call has the products of what they leave as more splits,
-  // whose sums stay below 512 MB (1 x 2048 x 64 13.8 us, 23.2 so; 1 x 8192 x 1023 19.5 and 52.8).
-  q.two = act && dtype == 1 && M * N < 1024 && K <= 65536;
-  if (q.two) q.dx.bytes = 2 * q.dx.splits * M * K * 4, q.dw.bytes = 2 * q.dw.splits * N * K * 4;
+  // its own rounding takes, with 1024 by 1.48 as with many), and few are cheap to take twice: 1 x 2048 to 64 13.6 us either
+  // way, 1 x 8192 to 1023 20.0 and 26.4.  Many are not: twice the products of 4096 x 1024 to 2816, 83 us.
+  q.two = act && dtype == 1 && M * N < 1024;
+  q.dx = plan(M, K, N, dtype, kDx, q.two ? 64 : 256);
+  q.dw = plan(N, K, M, dtype, kDw, q.two ? 64 : 256);
+  q.du = du_plan(M, N, dtype);
   q.o_low = act ? up256(M * N * elem(dtype)) : 0;
   q.o_part = q.two ? 2 * q.o_low : q.o_low;
   int64_t part = q.du.strips * N * 4;
@@ -526,37 +533,32 @@ bool direct(const Side& s, bool down, int64_t K, int esize) {
   return reinterpret_cast<uintptr_t>(s.p) % 16 == 0 && s.stride % e == 0 && (down ? s.n : K) % e == 0;
 }
 
-template <typename T, int TILE, bool DM, bool DN, bool DIRECT>
+template <typename T, int TILE, bool DM, bool DN, bool DIRECT, bool TWO = false>
 void launch_tiles(const GemmDev& p, int64_t workgroups, hipStream_t st) {
   constexpr int WM = 2, WN = TILE == 256 ? 4 : 2;
-  k_gemm<T, TILE, TILE, WM, WN, DM, DN, DIRECT><<<dim3(uint32_t(workgroups)), dim3(64 * WM * WN), 0, st>>>(p);
+  k_gemm<T, TILE, TILE, WM, WN, DM, DN, DIRECT, TWO><<<dim3(uint32_t(workgroups)), dim3(64 * WM * WN), 0, st>>>(p);
 }
 
 template <typename T, bool DM, bool DN>
 void launch_tile(const GemmDev& p, const GemmPlan& q, hipStream_t st) {
   const bool dir = direct(p.b, DM, p.K, sizeof(T)) && direct(p.a, DN, p.K, sizeof(T));
   if constexpr (sizeof(T) == 2) {
+    if constexpr (DN) {
+      if (p.low) return dir ? launch_tiles<T, 64, DM, DN, true, true>(p, q.workgroups, st) : launch_tiles<T, 64, DM, DN, false, true>(p, q.workgroups, st);
+    }
     if (q.tile == 256) dir ? launch_tiles<T, 256, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 256, DM, DN, false>(p, q.workgroups, st);
   }
   if (q.tile == 128) dir ? launch_tiles<T, 128, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 128, DM, DN, false>(p, q.workgroups, st);
   else if (q.tile == 64) dir ? launch_tiles<T, 64, DM, DN, true>(p, q.workgroups, st) : launch_tiles<T, 64, DM, DN, false>(p, q.workgroups, st);
 }
 
-// A product by its plan; with `low`, a second part of operand b, its products' sums come after the others.
+// A product by its plan.
 template <typename T, bool DM, bool DN>
-hipError_t launch_product(GemmDev p, const GemmPlan& q, float* part, hipStream_t st, const void* low = nullptr) {
+hipError_t launch_product(GemmDev p, const GemmPlan& q, float* part, hipStream_t st) {
   p.m_tiles = q.m_tiles, p.n_tiles = q.n_tiles, p.splits = q.splits, p.span = q.span;
   p.part = q.bytes ? part : nullptr;
   launch_tile<T, DM, DN>(p, q, st);
-  if (low) {
-    p.b.p = low, p.part = part + q.splits * p.f.M * p.f.N;
-    launch_tile<T, DM, DN>(p, q, st);
-    p.splits = 2 * q.splits;
-  }
-  if (q.bytes) {
-    p.part = part;
-    k_gemm_join<T><<<dim3(uint32_t(ceil_div(p.f.M * ceil_div(p.f.N, 4), 256))), dim3(256), 0, st>>>(p);
-  }
+  if (q.bytes) k_gemm_join<T><<<dim3(uint32_t(ceil_div(p.f.M * ceil_div(p.f.N, 4), 256))), dim3(256), 0, st>>>(p);
   return hipGetLastError();
 }
 
@@ -602,15 +604,15 @@ hipError_t bwd(const ProjArgs& a, const ProjGrads& g, hipStream_t st) {
   }
   if (e == hipSuccess && g.dx) {
     GemmDev p = {};
-    p.a = {a.weight, a.K, a.K}, p.b = {du, a.N, a.M}, p.K = a.N;
+    p.a = {a.weight, a.K, a.K}, p.b = {du, a.N, a.M}, p.low = low, p.K = a.N;
     p.f = {g.dx, nullptr, nullptr, 0, nullptr, a.M, a.K, 0};
-    e = launch_product<T, false, true>(p, q.dx, part, st, low);
+    e = launch_product<T, false, true>(p, q.dx, part, st);
   }
   if (e == hipSuccess && g.dweight) {
     GemmDev p = {};
-    p.a = {a.x, a.x_stride, a.K}, p.b = {du, a.N, a.N}, p.K = a.M;
+    p.a = {a.x, a.x_stride, a.K}, p.b = {du, a.N, a.N}, p.low = low, p.K = a.M;
     p.f = {g.dweight, nullptr, nullptr, 0, nullptr, a.N, a.K, 0};
-    e = launch_product<T, true, true>(p, q.dw, part, st, low);
+    e = launch_product<T, true, true>(p, q.dw, part, st);
   }
   return e;
 }

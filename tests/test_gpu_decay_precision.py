@@ -79,3 +79,52 @@ def test_short_sequences_of_a_longer_batch_are_rounded_once(T, dk, dv):
                 tol += 2.0 ** -16 * bound[b]
                 tol += HALF["bf16"] * (np.abs(want[b]) + tol)
             assert (np.abs(got[b] - want[b]) <= tol + 1e-36).all(), (name, n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,B,H,dk,dv", [(16384, 1, 8, 64, 48), (16400, 1, 8, 128, 128), (8192, 50, 8, 16, 16)])
+def test_prompts_forget_at_the_rate_of_the_decay(T, B, H, dk, dv, dtype):
+    """Tokens whose keys are zero, in 128 segments and in one: the state times g^T.  A rounding for each chunk or segment,
+    not for a factor's error in each."""
+    from paper_2506_04761_amd import block as ll
+    import torch
+    r = np.random.default_rng(2)
+    k = torch.zeros((B, T, H, dk), device="cuda", dtype=torch.float32 if dtype == "f32" else torch.bfloat16)
+    v = torch.ones((B, T, H, dv), device="cuda", dtype=k.dtype)
+    ld, first = to_dev(DECAYS), to_dev(r.standard_normal((B, H, dk, dv)))
+    final = torch.empty_like(first)
+    ll.ll_decay_attention_fwd(k, k, v, ld, 1.0, first, final)
+    want = _np(first) * np.exp(_np(ld) * T)[None, :, None, None]
+    off = (_np(final) / want - 1).swapaxes(0, 1).reshape(H, -1)
+    steps = T // 32 + 2
+    assert (np.abs(off) <= 2 * steps * U).all()
+    assert (np.abs(off.mean(1)) <= 2 * U + 6 * U * np.sqrt(steps / off.shape[1])).all(), off.mean(1) / U
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dk,dv", [(16, 24), (33, 47), (64, 128), (128, 128), (101, 143), (256, 200)])
+@pytest.mark.parametrize("T", [64, 400, 640, 1100])
+def test_states_of_few_tokens_keep_the_bits_of_fp32(T, dk, dv, dtype):
+    """States, and gradients of states, that a few tokens make.  In u of the same sums of absolute values A: a power of the
+    decay 5 (exp2's 2, its exponent of up to 1.3), the products with it, with the scale and in parts 3, their sums 3 for each
+    of two tokens of a chunk, a chunk's factor 1 and a segment's 1: 24 + T / 32.  (Two parts of bf16 would leave 2^-14.)"""
+    from paper_2506_04761_amd import block as ll
+    import torch
+    c = _Case(T + dk, 2, T, 2, 1, dk, dv, dtype, decays=[-0.003, -0.02], state=False)
+    at = sorted({3 % T, 40 % T, T // 3, T // 2, T - 70 if T > 70 else 0, T - 1})
+    keep = torch.zeros(T, dtype=torch.bool, device="cuda")
+    keep[at] = True
+    c.k = c.k.masked_fill(~keep[None, :, None, None], 0)
+    c.d_o = c.d_o.masked_fill(~keep[None, :, None, None], 0)
+    final = torch.empty((2, 2, dk, dv), device="cuda")
+    states = ll.ll_decay_attention_states(c.q, c.v)
+    a = (c.q, c.k, c.v, c.ld)
+    ll.ll_decay_attention_fwd(*a, c.scale, None, final, states=states)
+    g = ll.ll_decay_attention_bwd(*a, states, c.d_o, c.scale, initial_state_grad=True)
+    h, d = [_np(t) for t in a], _np(c.d_o)
+    mag = [np.abs(x) for x in h[:3]] + [h[3]]
+    wants = layer.decay_attention(*h, c.scale)[1], layer.decay_attention_grad(*h, d, c.scale)[3]
+    bounds = layer.decay_attention(*mag, c.scale)[1], layer.decay_attention_grad(*mag, np.abs(d), c.scale)[3]
+    for name, got, want, bound in zip(("final", "d_initial"), (final, g.initial_state), wants, bounds):
+        off = np.abs(_np(got) - want) / ((24 + T / 32) * U * bound + 1e-36)
+        assert (off <= 1).all(), (name, float(off.max()))

@@ -118,3 +118,42 @@ def test_an_infinite_state_stays_so_over_tokens(dtype):
     for t in range(5):
         ll.ll_decay_attention_step(q[:, t], k[:, t], v[:, t], ld, state)
     _same_states(state, q, k, v, ld, first)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [float("nan"), INF])
+@pytest.mark.parametrize("what", ["q", "k", "v", "d_o"])
+@pytest.mark.parametrize("T,dk,dv", [(300, 24, 40), (640, 128, 128), (640, 33, 65)])
+def test_what_a_token_does_not_reach_keeps_its_bits(T, dk, dv, what, value, dtype):
+    """One token of one head without a finite element.  By the formulas a key or value reaches the outputs and gradients of
+    queries from its token on, a query or a gradient of an output the gradients of keys and values up to its token, each its
+    own gradient's partner at its token; in chunks also up to 63 tokens to the other side.  Everything else keeps its bits."""
+    from paper_2506_04761_amd import block as ll
+    import torch
+    q, k, v, ld, initial = _inputs(T, T, dk, dv, dtype)
+    d_o = to_dev(np.random.default_rng(3).standard_normal((1, T, 2, dv)), dtype)
+    t = T // 2 + 5
+
+    def run():
+        states, final = ll.ll_decay_attention_states(q, v), torch.empty_like(initial)
+        o = ll.ll_decay_attention_fwd(q, k, v, ld, 1.0, initial, final, states=states)
+        g = ll.ll_decay_attention_bwd(q, k, v, ld, states, d_o, initial_state_grad=True)
+        return {"o": o, "final": final, "q": g.q, "k": g.k, "v": g.v, "initial": g.initial_state}
+
+    clean = run()
+    {"q": q, "k": k, "v": v, "d_o": d_o}[what][0, t, 0] = value
+    dirty = run()
+    onward, back, own, none = range(max(t - 63, 0), T), range(min(t + 64, T)), range(t, t + 1), range(0)
+    reach = {"q": {"o": own, "q": none, "k": back, "v": back}, "k": {"o": onward, "q": onward, "k": none, "v": own},
+             "v": {"o": onward, "q": onward, "k": own, "v": none}, "d_o": {"o": none, "q": own, "k": back, "v": back}}[what]
+    for name, x in dirty.items():
+        assert torch.equal(x[:, :, 1] if name in reach else x[:, 1], clean[name][:, :, 1] if name in reach else clean[name][:, 1]), name
+    for name, tokens in reach.items():
+        out = torch.ones(T, dtype=torch.bool, device="cuda")
+        out[list(tokens)] = False
+        assert torch.equal(dirty[name][0, out, 0], clean[name][0, out, 0]), name
+        # of an infinity, sums of both signs are NaN and others infinite
+        formula = [s for s in tokens if (s >= t if tokens is onward else s <= t)]
+        assert not dirty[name][0, formula, 0].isfinite().any(), name
+    for name, by in (("final", "kv"), ("initial", ("q", "d_o"))):
+        assert torch.equal(dirty[name], clean[name]) if what not in by else not dirty[name][0, 0].isfinite().any(), name

@@ -441,8 +441,11 @@ ll_status ll_group_norm_bwd(const void* x, int64_t x_batch_stride, int64_t x_tok
  * elements, >= 0, a token's below 2^24, heads adjacent.  o and the gradients are dense, states
  * [batch, heads, d_k, d_v] float32.  d_k, d_v <= 256, any T; qk_heads divides heads (LL_ERR_BAD_SHAPE).
  * Lengths, states, sums, rows and limits are as for the operators around a token mixer.  Sums and states are
- * float32; for bf16 the scores and the states' values enter the products with v and q rounded to bf16.  A NaN or
- * an infinity in a token may reach outputs of up to 63 tokens before it. */
+ * float32; for bf16 the scores and the states' values enter the products with v and q rounded to bf16, those of
+ * sequences of up to 64 tokens in two bf16 parts (off by 2^-16).  What a NaN or an infinity in a token reaches by
+ * the formulas is NaN or infinite, states as the formulas have it while the powers of g do not underflow; beside
+ * that, outputs and gradients of q of up to 63 tokens before it, and gradients of k and v of up to 63 tokens after
+ * it, may be NaN.  Nothing else changes. */
 typedef struct ll_decay_inputs {
   const void *q, *k, *v;
   int64_t q_strides[2], k_strides[2], v_strides[2];  /* batch, token */
@@ -492,7 +495,8 @@ ll_status ll_decay_attention_bwd(const ll_decay_inputs* in, const float* states,
  * from d_y [M, N]:
  *   du = d_y act'(u),   dx = du W,   dW = du^T x,   dbias = sum over the rows of du   (residual: d_y itself),
  * dx, dW and dbias each NULL where not wanted, pre not used without an activation.  du enters the products
- * rounded to the storage dtype, dbias as it is.  The workspace is ll_projection_workspace_size(...) bytes
+ * rounded to the storage dtype (fewer than 1024 bf16 values of it in two parts, off by 2^-16), dbias as it is.
+ * The workspace is ll_projection_workspace_size(...) bytes
  * (0: NULL is accepted; 0 for invalid arguments too); the backward's is at least the forward's. */
 size_t ll_projection_workspace_size(int32_t dtype, int64_t M, int64_t K, int64_t N, int32_t act,
                                     int32_t backward);

@@ -13,10 +13,10 @@
 // then is an operand of the next as the lanes hold it (P^T through LDS, where other waves read it; S in place), since a
 // contraction only needs both operands to agree on which k a slot stands for.
 //
-// bf16: 65536 tokens of 16 heads of 128 x 128 386 us in all (sums of 32 segments 134, their join 16, results 281), 4.5 TB/s
-// over the 1.75 GB that are moved; 4 x 8192 tokens of 32 heads of 128 x 64 with states in and out 274 us (80, 11, 205), 4.4
-// TB/s; a copy reaches 5.0.  Bound by memory there, by a chunk's way through the waves (7 to 9 us with two workgroups on a
-// compute unit) where segments are short.
+// bf16: 65536 tokens of 16 heads of 128 x 128 387 us a call, 4.5 TB/s over the 1.75 GB that are moved; 4 x 8192 tokens of 32
+// heads of 128 x 64 with states in and out 274 us, 4.4 TB/s; a copy reaches 5.0.  (In a kernel trace, which runs one launch
+// at a time and slower: sums of 32 segments 137, their join 16, results 268; and 79, 12, 206.)  Bound by memory there, by a
+// chunk's way through the waves (7 to 9 us with two workgroups on a compute unit) where segments are short.
 #include "ll_layer.hpp"
 #include "ll_layer_device.hpp"
 
@@ -53,7 +53,9 @@ __device__ inline int row_of(int t, int i) {
 
 // An LDS tile of rows of W elements: chunk c of 16 bytes at c ^ key(row).  A read serves 256 bytes at a time, 16 lanes of
 // 16 bytes or 32 of 8, which the keys spread over all banks: one chunk of 16 rows (0 - 15, or 0 - 3, 8 - 11, 16 - 19 and
-// 24 - 27), two chunks of 8 rows (0 - 3 and 8 - 11), and in fp32 16 columns of four rows 4 apart.
+// 24 - 27), two chunks of 8 rows (0 - 3 and 8 - 11), and in fp32 16 columns of four rows 4 apart.  The values of paired
+// columns (NV = 2) are read in halves of four chunks of 8 rows, which the banks serve at half their rate.  All in all 39 % of
+// the cycles of LDS reads and copies in k_attend's results of 128 x 128 are conflicts (LDS is active a third of the time).
 template <typename T, int W>
 struct Tile {
   static constexpr int E = 16 / sizeof(T), CH = W / E;
@@ -308,7 +310,7 @@ constexpr bool keys_ahead(int dk) { return dk <= 128; }
 // Chunks end with the segment: the first may begin with rows of zeros, and powers of the decay are the same in all others.
 // FEW: bf16 sequences of one chunk take scores and states in two parts: with few of them their roundings do not average out
 // (28 sequences of one token: results off by 0.0032, 0.0017 so; of more than 64 tokens 0.0025 at most).  512 sequences of 64
-// tokens, 16 heads of 128 x 128: 597 us, 622 so.
+// tokens, 16 heads of 128 x 128: 597 us, 626 so.
 template <typename T, int DK, int NV, bool STATE, bool VEC, bool FEW, typename Keys, typename Values, typename Queries, typename Scores>
 __device__ __attribute__((always_inline)) inline void attend_segment(const DecayDev& p, int64_t b, int h, int seg, int blk, int64_t live,
                                                                      Keys& sk, Values& sv, Queries& sq, Scores& sp, float* sw) {

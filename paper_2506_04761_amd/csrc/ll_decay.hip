@@ -284,7 +284,7 @@ __device__ inline void weighted(bf16x8 v, const float* w, bf16x8* part) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
   for (int x = 0; x < 8; x += 2) {
-    float a = fmaf(to_f32(__bf16(v[x])), w[x], kNoZero), b = fmaf(to_f32(__bf16(v[x + 1])), w[x + 1], kNoZero);
+    float a = product(to_f32(__bf16(v[x])), w[x]), b = product(to_f32(__bf16(v[x + 1])), w[x + 1]);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
       bf16x2 y = {static_cast<__bf16>(a), static_cast<__bf16>(b)};
@@ -437,7 +437,7 @@ __device__ __attribute__((always_inline)) inline void attend_segment(const Decay
 #pragma unroll
           for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) pt[r][e] = FEW ? fmaf(pt[r][e], pw[x][r][e], kNoZero) : pt[r][e] * pw[x][r][e];
+            for (int e = 0; e < 4; ++e) pt[r][e] = FEW ? product(pt[r][e], pw[x][r][e]) : pt[r][e] * pw[x][r][e];
           if (FEW) {
 #pragma unroll
             for (int r = 0; r < R; ++r) pt[r] = part_of(pt[r], part);
@@ -457,7 +457,10 @@ __device__ __attribute__((always_inline)) inline void attend_segment(const Decay
                 f32x4 x[R];
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                  if (FEW && !low) S[R * ks + r][v] += kNoZero;
+                  if (FEW && !low) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) S[R * ks + r][v][e] = positive(S[R * ks + r][v][e]);
+                  }
                   x[r] = S[R * ks + r][v];
                   if (FEW) x[r] = part_of(x[r], low);
                 }

@@ -90,13 +90,19 @@ __device__ inline float softplusf(float v) {
 }
 
 // A value in two addends: its upper part, the upper 16 bits of the float before it (towards zero), which bf16 holds, and the
-// rest, below 2^-7 of it.  Both have the value's sign and neither is zero where the value is not (powers of two away from
+// rest, at most 2^-7 of it.  Both have the value's sign and neither is zero where the value is not (powers of two away from
 // the smallest float), an infinity's rest is infinite: so an infinity on either side of a product is one in the sum of the
-// parts' products, where a rounded part would leave 0 times it, or two of opposite signs.  -0 has no float before it: kNoZero,
-// which is too little for bf16, is added first where it may come.
-constexpr float kNoZero = 0x1p-149f;
+// parts' products, where a rounded part would leave 0 times it, or two of opposite signs.  +0 is +0 and +0, but -0 has no
+// float before it: positive() and product() are without it.
 __device__ inline float upper_part(float v) {
   return __builtin_bit_cast(float, __builtin_elementwise_sub_sat(__builtin_bit_cast(unsigned, v), 1u) & 0xffff0000u);
+}
+// v, and a b rounded, with +0 for -0.  Not in one fused product and sum: its sum may be rounded to -0.
+__device__ inline float positive(float v) { return v + 0.0f; }
+__device__ inline float product(float a, float b) {
+#pragma clang fp contract(off)
+  const float v = a * b;
+  return v + 0.0f;
 }
 
 // Direct copies of 16 bytes a lane to LDS, lane l's to `lds` + 16 l.  In inline assembly: before every LDS read the compiler

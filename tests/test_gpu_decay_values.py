@@ -157,3 +157,33 @@ def test_what_a_token_does_not_reach_keeps_its_bits(T, dk, dv, what, value, dtyp
         assert not dirty[name][0, formula, 0].isfinite().any(), name
     for name, by in (("final", "kv"), ("initial", ("q", "d_o"))):
         assert torch.equal(dirty[name], clean[name]) if what not in by else not dirty[name][0, 0].isfinite().any(), name
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [64, 128, 700])
+def test_products_about_the_smallest_float_are_nothing(T, dtype):
+    """Values times powers of the decay, and scores times them, of -4 to 0 times 2^-149, whose roundings are -0 among others:
+    states, outputs and gradients are what the other tokens make, and finite."""
+    from paper_2506_04761_amd import block as ll
+    import torch
+    H, dk, dv = 4, 16, 64
+    # g^63 is 2^-125 times 2^(h / 4)
+    ld = to_dev(np.log(2.0) * (np.arange(H) / 4 - 125) / 63)
+    small = -2.0 ** -24 * 2.0 ** (np.arange(dv) / 16 - 2)  # -2^-26 to -2^-22
+    q, k = (to_dev(np.ones((1, T, H, dk)), dtype) for _ in "qk")
+    v = to_dev(np.broadcast_to(small, (1, T, H, dv)), dtype)
+    d_o = v.clone()
+    # the first token's scores are small, not its values
+    q[0, :, 2:], k[0, 0, 2:] = 2.0 ** -4, to_dev(small[:dk], dtype)
+    final = torch.empty((1, H, dk, dv), device="cuda")
+    states = ll.ll_decay_attention_states(q, v)
+    o = ll.ll_decay_attention_fwd(q, k, v, ld, 1.0, None, final, states=states)
+    g = ll.ll_decay_attention_bwd(q, k, v, ld, states, d_o, initial_state_grad=True)
+    h = [_np(t) for t in (q, k, v, ld)]
+    want, end = layer.decay_attention(*h)
+    wants = layer.decay_attention_grad(*h, _np(d_o))
+    for name, got, ref in zip(("o", "final", "dq", "dk", "dv", "dinitial"), (o, final, *g), (want, end, *wants)):
+        e = 2.0 ** -8 if dtype == "bf16" and name not in ("final", "dinitial") else 0
+        # all terms of a sum have one sign: bounds relative to it; scores and states rounded once, and the result
+        assert np.isfinite(_np(got)).all(), name
+        assert (np.abs(_np(got) - ref) <= (2.1 * e + (2 * T + 64) * 2.0 ** -24) * np.abs(ref) + 1e-36).all(), name

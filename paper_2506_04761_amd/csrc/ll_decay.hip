@@ -13,7 +13,7 @@
 // then is an operand of the next as the lanes hold it (P^T through LDS, where other waves read it; S in place), since a
 // contraction only needs both operands to agree on which k a slot stands for.
 //
-// bf16: 65536 tokens of 16 heads of 128 x 128 387 us a call, 4.5 TB/s over the 1.75 GB that are moved; 4 x 8192 tokens of 32
+// bf16: 65536 tokens of 16 heads of 128 x 128 386 us a call, 4.5 TB/s over the 1.75 GB that are moved; 4 x 8192 tokens of 32
 // heads of 128 x 64 with states in and out 274 us, 4.4 TB/s; a copy reaches 5.0.  (In a kernel trace, which runs one launch
 // at a time and slower: sums of 32 segments 137, their join 16, results 268; and 79, 12, 206.)  Bound by memory there, by a
 // chunk's way through the waves (7 to 9 us with two workgroups on a compute unit) where segments are short.

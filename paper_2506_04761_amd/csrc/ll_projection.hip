@@ -6,7 +6,7 @@
 // k).  A stage of 128 bytes of k of both operands is copied to LDS as it lies, and the fragments of the matrix
 // instructions are read from there along or down the rows, so that nothing is transposed in memory.
 //
-// bf16: 32768 x 1024 to 4096 308 us, 892 TFLOP/s (the library's product 254); training step of 8064 x 2048 to 1024 146 us, 695
+// bf16: 32768 x 1024 to 4096 299 us, 919 TFLOP/s (the library's product 254); training step of 8064 x 2048 to 1024 143 us, 710
 // TFLOP/s (in a kernel trace 41 the forward, 40 dx, 51 dW in four splits, 12 dbias).  The matrix cores are busy 42 % of the time, LDS 16 to 32 %:
 // what bounds the products is the turn of a stage, its wait, barrier and first reads.
 #include "ll_layer.hpp"
